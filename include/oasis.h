@@ -13,15 +13,18 @@
  * compressed keys the scorer reads (§4.2.1, "Look-ahead attention" figure; §5.1)
  * for the whole context or for the blocks completed since the last call;
  * oasis_copy_blocks, which moves blocks between the GPU pages and the full host
- * tier (§4.3, dense-to-sparse transition and appends); and oasis_pipeline_*,
- * the native issuer of the layer-pipelined step (§4.2.2).
+ * tier (§4.3, dense-to-sparse transition and appends); oasis_tree_attn,
+ * oasis_sparse_tree_attn, oasis_verify_drafts and oasis_append_tokens, the
+ * speculative step of a drafted token tree; and oasis_pipeline_*, the native
+ * issuer of the layer-pipelined step (§4.2.2).
  *
  * General conventions
  * -------------------
  * - Every pointer is owned by the caller. The single-call entry points
- *   (oasis_build_summaries ... oasis_sparse_decode_attn) allocate no memory;
- *   the scratch the attention call needs is a caller-provided workspace whose
- *   size comes from oasis_attn_workspace_bytes. The step issuer does allocate,
+ *   (oasis_build_summaries ... oasis_append_tokens) allocate no memory; the
+ *   scratch that the attention calls and the verification need is a
+ *   caller-provided workspace whose size comes from the call's
+ *   *_workspace_bytes. The step issuer does allocate,
  *   outside its steps: oasis_pipeline_create (its counter array, and the two
  *   background streams unless the caller passes them), oasis_pipeline_set_layer
  *   and oasis_pipeline_set_plan_stream (a plan workspace per layer when the plan
@@ -324,6 +327,122 @@ OASIS_API oasis_status oasis_sparse_decode_attn_noalloc(const oasis_dims* dims, 
                                               const uint16_t* pool_v, const int32_t* slot_map, int32_t k_slots,
                                               const int32_t* ctx_len, float scale, uint16_t* out, float* lse,
                                               void* stream);
+
+/*
+ * Speculative step: attention of a tree of drafted tokens, its verification, and
+ * the append of what is accepted (paper §4.2.1 stacks draft rows behind the row
+ * being verified; these calls verify such rows against the target itself).
+ *
+ * A tree has T = num_q_tokens rows per request, T <= 64: row 0 is the token being
+ * verified and row t > 0 a drafted token that follows row parent[r][t].
+ *   parent    int32 [R][T]  a value outside [0, t) makes row t a root; NULL: a
+ *                           chain (row t follows row t - 1)
+ *   tree_len  int32 [R]     rows in use, clamped to [0, T]; NULL: T. What belongs
+ *                           to later rows is not read as a key or value, and
+ *                           their outputs are left as they were.
+ *   tree_k, tree_v  bf16 [R][T][Hkv][d]  the rows' own keys and values, which are
+ *                           in no cache yet (ctx_len does not count them)
+ * Pointers to bf16 tensors and workspaces are 16-byte aligned. All pointers are
+ * device pointers, except pages (device memory or pinned host memory).
+ */
+
+/*
+ * Attention of a drafted tree over the paged cache: for every request r, row
+ * t < tree_len[r] and query head qh (KV head h = qh / G), over the attended set
+ * of the first ctx_len[r] cached tokens (logical block b in page
+ * block_table[r][b]; the tokens of a page outside [0, num_pages) are left out)
+ * and the tree's rows on the path from row t to its root, t among them:
+ *   out = softmax(scale * q . K^T) V,  lse = log sum exp(scale * q . K^T).
+ * This is also the dense attention of a request below the sparsification
+ * threshold (§5.2), whose blocks are all in device pages. Arithmetic as
+ * oasis_sparse_decode_attn. A row of the tree that is not on another's path has
+ * no influence on it, whatever it holds. G * T <= 4096. lse is nullable.
+ * workspace: oasis_tree_attn_workspace_bytes (0: may be NULL); calls that run at
+ * the same time need separate workspaces.
+ */
+OASIS_API size_t oasis_tree_attn_workspace_bytes(const oasis_dims* dims, int32_t num_q_tokens);
+OASIS_API oasis_status oasis_tree_attn(const oasis_dims* dims, const uint16_t* q, int32_t num_q_tokens,
+                                       const uint16_t* k_pages, const uint16_t* v_pages, int64_t num_pages,
+                                       const int32_t* block_table, const int32_t* ctx_len, const uint16_t* tree_k,
+                                       const uint16_t* tree_v, const int32_t* parent, const int32_t* tree_len,
+                                       float scale, uint16_t* out, float* lse, void* workspace,
+                                       size_t workspace_bytes, void* stream);
+
+/*
+ * The same over the working set: the attended set is that of
+ * oasis_sparse_decode_attn (the B tokens of every slot s < k_slots with
+ * slot_map[r][h][s] >= 0 and the first local_len_r tokens of slot k_slots) and
+ * the rows on the path from row t to its root.
+ */
+OASIS_API size_t oasis_sparse_tree_attn_workspace_bytes(const oasis_dims* dims, int32_t num_q_tokens,
+                                                        int32_t k_slots);
+OASIS_API oasis_status oasis_sparse_tree_attn(const oasis_dims* dims, const uint16_t* q, int32_t num_q_tokens,
+                                              const uint16_t* pool_k, const uint16_t* pool_v,
+                                              const int32_t* slot_map, int32_t k_slots, const int32_t* ctx_len,
+                                              const uint16_t* tree_k, const uint16_t* tree_v, const int32_t* parent,
+                                              const int32_t* tree_len, float scale, uint16_t* out, float* lse,
+                                              void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Verification of the drafted tokens against the target's probabilities, from
+ * given random numbers (rejection sampling over a tree: the tokens emitted are
+ * distributed as the target's own where the drafted ones were drawn from
+ * draft_probs, or chosen without regard to the random numbers).
+ *
+ *   target_probs  fp32 [R][T] rows of vocab, target_stride elements apart: row t
+ *                 is the target's distribution of the token after row t
+ *   draft_probs   fp32, the same with draft_stride: row t is the distribution that
+ *                 the children of row t were drawn from; NULL: certain drafts
+ *   tokens        int32 [R][T], row t's token (row 0's is not read)
+ *   accept_u      fp32 [R][T] and sample_u fp32 [R], uniform in [0, 1)
+ *
+ * The walk starts at row 0 of a request with tree_len >= 1. At row n, with target
+ * row p, draft row q, C = 0 and Z = 1, the children c of n are taken in ascending
+ * order, x = tokens[r][c]: c is accepted when
+ *   accept_u[r][c] * q(x) * Z < w(x),   w = max(p - C q, 0),
+ * and the walk goes on at c; otherwise C += Z and Z = sum of the new w. With
+ * certain drafts q(x) is 1, w is p without the tokens rejected at n, and a
+ * rejection takes w(x) off Z. Where no child is accepted the walk ends and the
+ * next token is the first v whose sum of w(0..v) exceeds sample_u[r] times the
+ * sum of w (where w has no mass, p stands in for it; where p has none, -1). All of
+ * it in 64-bit floating point. A child whose token is outside [0, vocab) is passed
+ * over; a NaN or negative probability counts as 0.
+ *
+ *   path        int32 [R][T]  the rows walked, row 0 first, -1 padded
+ *   path_len    int32 [R]     how many (0 when tree_len is 0)
+ *   out_tokens  int32 [R][T]  the tokens emitted, path_len of them: those of
+ *                             path[1..], then the next token; -1 padded
+ * T <= 64, num_reqs <= 65535, vocab <= 2^28. Only the rows walked are read whole.
+ * workspace: oasis_verify_workspace_bytes; it needs no clearing, and calls that run
+ * at the same time need separate ones.
+ */
+OASIS_API size_t oasis_verify_workspace_bytes(int32_t num_reqs, int32_t num_q_tokens, int32_t vocab);
+OASIS_API oasis_status oasis_verify_drafts(int32_t num_reqs, int32_t num_q_tokens, int32_t vocab,
+                                           const float* target_probs, int64_t target_stride,
+                                           const float* draft_probs, int64_t draft_stride, const int32_t* tokens,
+                                           const int32_t* parent, const int32_t* tree_len, const float* accept_u,
+                                           const float* sample_u, int32_t* path, int32_t* path_len,
+                                           int32_t* out_tokens, void* workspace, size_t workspace_bytes,
+                                           void* stream);
+
+/*
+ * Append to the paged cache: for every request r and i < path_len[r], the K and V
+ * rows path[r][i] of new_k / new_v (bf16 [R][num_tokens][Hkv][d]) go to token
+ * position ctx_len[r] + i, in page block_table[r][position / B] of the pages
+ * [num_pages][Hkv][B][d]. Positions past max_blocks * B, rows outside
+ * [0, num_tokens) and pages outside [0, num_pages) are not written. path NULL: rows
+ * 0, 1, ... (path_len NULL then: num_tokens of them, a prompt chunk).
+ * new_ctx_len[r] (nullable, device [R], not ctx_len itself) = ctx_len[r] + path_len[r],
+ * at most max_blocks * B. Two requests must not share the pages they append to.
+ * With several tiers the call is made once for each; oasis_update_summaries and the
+ * local-only form of oasis_stage_blocks bring the compressed keys and the working
+ * set's local block up to date. num_tokens * Hkv <= 2^26.
+ */
+OASIS_API oasis_status oasis_append_tokens(const oasis_dims* dims, const uint16_t* new_k, const uint16_t* new_v,
+                                           int32_t num_tokens, const int32_t* path, const int32_t* path_len,
+                                           uint16_t* k_pages, uint16_t* v_pages, int64_t num_pages,
+                                           const int32_t* block_table, const int32_t* ctx_len, int32_t* new_ctx_len,
+                                           void* stream);
 
 /*
  * Native step issuer for the layer-pipelined schedule (paper §4.2.2, the

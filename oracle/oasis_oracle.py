@@ -40,7 +40,8 @@ import numpy as np
 
 __all__ = [
     "bf16_to_f64", "block_counts", "block_summaries", "update_summaries", "copy_blocks", "block_scores",
-    "select_topk", "union_selection", "stage_blocks", "sparse_attend", "dense_attend",
+    "select_topk", "union_selection", "stage_blocks", "sparse_attend", "dense_attend", "tree_paths", "tree_attend",
+    "sparse_tree_attend", "verify_drafts", "append_tokens",
 ]
 
 
@@ -408,3 +409,167 @@ def dense_attend(q, host_k, host_v, block_table, ctx_len, block_size: int, scale
             out[r, :, h * G:(h + 1) * G, :] = o.reshape(T, G, d)
             lse[r, :, h * G:(h + 1) * G] = l.reshape(T, G)
     return out, lse
+
+
+# ---------------------------------------------------------------------------
+# Speculative step: tree attention, verification, append
+# ---------------------------------------------------------------------------
+
+def tree_paths(parent, tree_len, T: int):
+    """For every request and row t < tree_len: the rows from t up to its root, t first.
+
+    A parent outside [0, t) makes row t a root; ``parent`` None is a chain.
+    """
+    out = []
+    for r, n in enumerate(tree_len):
+        rows = []
+        for t in range(max(0, min(int(n), T))):
+            up, path = t, [t]
+            while True:
+                p = up - 1 if parent is None else int(parent[r][up])
+                if not 0 <= p < up:
+                    break
+                path.append(p)
+                up = p
+            rows.append(path)
+        out.append(rows)
+    return out
+
+
+def _tree_attend(q, cache, tree_k, tree_v, parent, tree_len, scale):
+    """``cache(r, h)``: the attended cached keys and values of a (request, KV head), float64 [S][d]. Rows past a
+    tree's end are NaN in the result."""
+    qf, tk, tv = bf16_to_f64(q), bf16_to_f64(tree_k), bf16_to_f64(tree_v)
+    R, T, Hq, d = qf.shape
+    Hkv = tk.shape[2]
+    G = Hq // Hkv
+    scale = 1.0 / math.sqrt(d) if scale is None else scale
+    out, lse = np.full((R, T, Hq, d), np.nan), np.full((R, T, Hq), np.nan)
+    for r, rows in enumerate(tree_paths(parent, tree_len, T)):
+        for h in range(Hkv):
+            ck, cv = cache(r, h)
+            for t, path in enumerate(rows):
+                keys, vals = np.concatenate([ck, tk[r, path, h]]), np.concatenate([cv, tv[r, path, h]])
+                o, l = _softmax_attend(qf[r, t, h * G:(h + 1) * G], keys, vals, scale)
+                out[r, t, h * G:(h + 1) * G], lse[r, t, h * G:(h + 1) * G] = o, l
+    return out, lse
+
+
+def tree_attend(q, k_pages, v_pages, block_table, ctx_len, tree_k, tree_v, parent, tree_len, block_size: int,
+                scale: float | None = None):
+    """Rows of a drafted tree over the paged cache and the rows on their own path.
+
+    Row t's keys are the first ctx_len tokens of the pages (tokens of a page
+    outside the tier are left out) and the tree rows from t to its root.
+    """
+    B = block_size
+    NB = len(block_table[0])
+
+    def cache(r, h):
+        L = max(0, min(int(ctx_len[r]), NB * B))
+        ks, vs = [np.zeros((0, k_pages.shape[3]))], [np.zeros((0, k_pages.shape[3]))]
+        for b in range((L + B - 1) // B):
+            page = int(block_table[r][b])
+            if 0 <= page < len(k_pages):
+                ks.append(bf16_to_f64(k_pages[page, h, :min(B, L - b * B)]))
+                vs.append(bf16_to_f64(v_pages[page, h, :min(B, L - b * B)]))
+        return np.concatenate(ks), np.concatenate(vs)
+
+    return _tree_attend(q, cache, tree_k, tree_v, parent, tree_len, scale)
+
+
+def sparse_tree_attend(q, pool_k, pool_v, slot_map, ctx_len, tree_k, tree_v, parent, tree_len, block_size: int,
+                       scale: float | None = None):
+    """Rows of a drafted tree over the working set (as ``sparse_attend``) and the rows on their own path."""
+    K = pool_k.shape[1] - 1
+
+    def cache(r, h):
+        _, _, local = block_counts(ctx_len[r], block_size)
+        parts = [(s, block_size) for s in range(K) if slot_map[r, h, s] >= 0] + [(K, local)]
+        return tuple(np.concatenate([bf16_to_f64(p[r, s, h, :n]) for s, n in parts]) for p in (pool_k, pool_v))
+
+    return _tree_attend(q, cache, tree_k, tree_v, parent, tree_len, scale)
+
+
+def verify_drafts(target, draft, tokens, parent, tree_len, accept_u, sample_u):
+    """Accepted path, emitted tokens and next token of each request's drafted tree.
+
+    Rejection sampling from given random numbers, in float64. At a node with
+    target distribution p the children are tried in ascending row order against
+    the residual distribution that the rejected ones leave: residual r (p at
+    first, of mass 1), draft distribution q, token x: accepted when
+    u * q(x) < r(x) / mass; otherwise r becomes max(r - mass * q, 0) (both
+    distributions scaled to r's mass) and mass its sum. Without draft
+    probabilities q is the certain distribution at x. Where no child is accepted
+    the next token is drawn from r by its running sum; a residual without mass
+    gives way to p. Returns (path [R][T], path_len [R], out_tokens [R][T]).
+    """
+    R, T, V = target.shape
+    path = np.full((R, T), -1, np.int32)
+    emitted = np.full((R, T), -1, np.int32)
+    count = np.zeros(R, np.int32)
+
+    def clean(row):
+        row = np.asarray(row, dtype=np.float64)
+        return np.where(row > 0, row, 0.0)
+
+    for r in range(R):
+        n = max(0, min(int(tree_len[r]), T))
+        if n == 0:
+            continue
+        rows, toks = [0], []
+        while True:
+            at = rows[-1]
+            p = clean(target[r, at])
+            q = None if draft is None else clean(draft[r, at])
+            res, mass, took = p.copy(), 1.0, None
+            for c in range(at + 1, n):
+                x = int(tokens[r, c])
+                if (c - 1 if parent is None else int(parent[r, c])) != at or not 0 <= x < V:
+                    continue
+                if float(accept_u[r, c]) * (1.0 if q is None else q[x]) * mass < res[x]:
+                    took = c
+                    break
+                if q is None:
+                    mass = max(mass - res[x], 0.0)
+                    res[x] = 0.0
+                else:
+                    res = np.maximum(res - mass * q, 0.0)
+                    mass = math.fsum(res)
+            if took is None:
+                break
+            rows.append(took)
+            toks.append(int(tokens[r, took]))
+        if not res.sum() > 0:
+            res = p
+        cum, nxt = np.cumsum(res), -1
+        if cum[-1] > 0:
+            over = np.nonzero((cum > float(sample_u[r]) * cum[-1]) & (res > 0))[0]
+            nxt = int(over[0]) if len(over) else int(np.nonzero(res > 0)[0][-1])
+        toks.append(nxt)
+        path[r, :len(rows)], emitted[r, :len(toks)], count[r] = rows, toks, len(rows)
+    return path, count, emitted
+
+
+def append_tokens(new_k, new_v, path, path_len, k_pages, v_pages, block_table, ctx_len, block_size: int):
+    """Rows path[r][:path_len[r]] of the new keys and values to token positions ctx_len[r] on; in place.
+
+    Positions past the table, rows outside the new tokens and pages outside the
+    tier are skipped. Returns the new lengths.
+    """
+    R, T = new_k.shape[:2]
+    NB = len(block_table[0])
+    cap = NB * block_size
+    ends = np.zeros(R, np.int32)
+    for r in range(R):
+        ctx = max(0, min(int(ctx_len[r]), cap))
+        n = T if path_len is None else max(0, min(int(path_len[r]), T))
+        n = min(n, cap - ctx)
+        for i in range(n):
+            row = i if path is None else int(path[r, i])
+            page = int(block_table[r][(ctx + i) // block_size])
+            if 0 <= row < T and 0 <= page < len(k_pages):
+                k_pages[page, :, (ctx + i) % block_size] = new_k[r, row]
+                v_pages[page, :, (ctx + i) % block_size] = new_v[r, row]
+        ends[r] = ctx + n
+    return ends

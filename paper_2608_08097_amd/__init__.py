@@ -14,5 +14,6 @@ from ._lib import (  # noqa: F401
     oasis_pipeline_profile_begin, oasis_pipeline_profile_end, oasis_update_summaries, oasis_copy_blocks,
     oasis_union_selection, oasis_pipeline_set_local_source, oasis_pipeline_set_plan_stream, PLAN_ON_TRANSFER,
     PLAN_ON_PREDICTION, oasis_pipeline_set_fused_prediction, FUSED_PREDICTION_AUTO, FUSED_PREDICTION_OFF,
-    FUSED_PREDICTION_ON,
+    FUSED_PREDICTION_ON, oasis_tree_attn, oasis_tree_attn_workspace_bytes, oasis_sparse_tree_attn,
+    oasis_sparse_tree_attn_workspace_bytes, oasis_verify_drafts, oasis_verify_workspace_bytes, oasis_append_tokens,
 )

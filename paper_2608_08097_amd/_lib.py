@@ -33,6 +33,8 @@ EXPORTS = (
     "oasis_select_topk", "oasis_stage_blocks",
     "oasis_attn_workspace_bytes", "oasis_sparse_decode_attn", "oasis_sparse_decode_attn_noalloc",
     "oasis_union_selection",
+    "oasis_tree_attn_workspace_bytes", "oasis_tree_attn", "oasis_sparse_tree_attn_workspace_bytes",
+    "oasis_sparse_tree_attn", "oasis_verify_workspace_bytes", "oasis_verify_drafts", "oasis_append_tokens",
     "oasis_pipeline_create", "oasis_pipeline_set_layer", "oasis_pipeline_set_local_source",
     "oasis_pipeline_set_plan_stream", "oasis_pipeline_set_fused_prediction", "oasis_pipeline_step",
     "oasis_pipeline_join", "oasis_pipeline_check", "oasis_pipeline_set_wait_limit",
@@ -118,6 +120,23 @@ def lib() -> ctypes.CDLL:
         L.oasis_sparse_decode_attn_noalloc.restype = _I32
         L.oasis_sparse_decode_attn_noalloc.argtypes = [_DIMS, _P, _I32, _P, _P, _P, _I32, _P, ctypes.c_float, _P,
                                                        _P, _P]
+        L.oasis_tree_attn_workspace_bytes.restype = _SZ
+        L.oasis_tree_attn_workspace_bytes.argtypes = [_DIMS, _I32]
+        L.oasis_tree_attn.restype = _I32
+        L.oasis_tree_attn.argtypes = [_DIMS, _P, _I32, _P, _P, _I64, _P, _P, _P, _P, _P, _P, ctypes.c_float, _P, _P, _P,
+                                      _SZ, _P]
+        L.oasis_sparse_tree_attn_workspace_bytes.restype = _SZ
+        L.oasis_sparse_tree_attn_workspace_bytes.argtypes = [_DIMS, _I32, _I32]
+        L.oasis_sparse_tree_attn.restype = _I32
+        L.oasis_sparse_tree_attn.argtypes = [_DIMS, _P, _I32, _P, _P, _P, _I32, _P, _P, _P, _P, _P, ctypes.c_float, _P,
+                                             _P, _P, _SZ, _P]
+        L.oasis_verify_workspace_bytes.restype = _SZ
+        L.oasis_verify_workspace_bytes.argtypes = [_I32, _I32, _I32]
+        L.oasis_verify_drafts.restype = _I32
+        L.oasis_verify_drafts.argtypes = [_I32, _I32, _I32, _P, _I64, _P, _I64, _P, _P, _P, _P, _P, _P, _P, _P, _P, _SZ,
+                                          _P]
+        L.oasis_append_tokens.restype = _I32
+        L.oasis_append_tokens.argtypes = [_DIMS, _P, _P, _I32, _P, _P, _P, _P, _I64, _P, _P, _P, _P]
         L.oasis_pipeline_create.restype = _I32
         L.oasis_pipeline_create.argtypes = [_DIMS, _I32, _I32, _I32, _I32, _I32, ctypes.c_float, _P, _P, _I64, _P,
                                             _I32, _P, _P, ctypes.POINTER(_P)]
@@ -440,6 +459,152 @@ def oasis_sparse_decode_attn_noalloc(d: OasisDims, q, num_q_tokens: int, pool_k,
         _dev(pool_v, "pool_v", _BF16), _dev(slot_map, "slot_map", _I32T, nullable=k_slots == 0), int(k_slots),
         _dev(ctx_len, "ctx_len", _I32T), float(scale), _dev(out, "out", _BF16),
         _dev(lse, "lse", _F32, nullable=True), _stream(stream)))
+
+
+# --- speculative step ----------------------------------------------------------
+
+
+def _one_device(**tensors) -> None:
+    """The device tensors of a call are all on the current device, whose stream it takes."""
+    dev = torch.cuda.current_device() if torch.cuda.is_initialized() else None
+    for name, t in tensors.items():
+        if t is not None and t.is_cuda and t.device.index != dev:
+            raise ValueError(f"{name} is on {t.device}, the current device is cuda:{dev}")
+
+
+def _pages(d: OasisDims, t: torch.Tensor, name: str) -> int:
+    """Number of pages [Hkv][B][d] of a tier."""
+    per = d.num_kv_heads * d.block_size * d.head_dim
+    if t.dim() < 1 or per < 1 or t.numel() % per:
+        raise ValueError(f"{name}: not whole pages of [Hkv][B][d]")
+    return t.numel() // per
+
+
+def _bytes(t: torch.Tensor | None) -> int:
+    return 0 if t is None else t.numel() * t.element_size()
+
+
+def oasis_tree_attn_workspace_bytes(d: OasisDims, num_q_tokens: int) -> int:
+    return int(lib().oasis_tree_attn_workspace_bytes(ctypes.byref(d), int(num_q_tokens)))
+
+
+def _tree_needs(d: OasisDims, T: int, q, ctx_len, tree_k, tree_v, parent, tree_len, out, lse) -> None:
+    R, Hq, H, D = d.num_reqs, d.num_q_heads, d.num_kv_heads, d.head_dim
+    for t, n, name in ((q, R * T * Hq * D, "q"), (out, R * T * Hq * D, "out"), (lse, R * T * Hq, "lse"),
+                       (tree_k, R * T * H * D, "tree_k"), (tree_v, R * T * H * D, "tree_v"), (ctx_len, R, "ctx_len"),
+                       (parent, R * T, "parent"), (tree_len, R, "tree_len")):
+        _need(t, n, name)
+
+
+def oasis_tree_attn(d: OasisDims, q, num_q_tokens: int, k_pages, v_pages, block_table, ctx_len, tree_k, tree_v,
+                    parent, tree_len, scale: float | None, out, lse, workspace, stream=None) -> None:
+    """Attention of a drafted token tree over the paged cache (parent None: a chain; tree_len None: every row)."""
+    if scale is None:
+        scale = 1.0 / math.sqrt(d.head_dim)
+    if k_pages.shape != v_pages.shape:
+        raise ValueError("k_pages and v_pages differ in shape")
+    _tree_needs(d, int(num_q_tokens), q, ctx_len, tree_k, tree_v, parent, tree_len, out, lse)
+    _need(block_table, d.num_reqs * d.max_blocks, "block_table")
+    _one_device(q=q, k_pages=k_pages, v_pages=v_pages, block_table=block_table, ctx_len=ctx_len, tree_k=tree_k,
+                tree_v=tree_v, parent=parent, tree_len=tree_len, out=out, lse=lse, workspace=workspace)
+    _check("oasis_tree_attn", lib().oasis_tree_attn(
+        ctypes.byref(d), _dev(q, "q", _BF16), int(num_q_tokens), _host_or_dev(k_pages, "k_pages", _BF16),
+        _host_or_dev(v_pages, "v_pages", _BF16), _pages(d, k_pages, "k_pages"),
+        _dev(block_table, "block_table", _I32T), _dev(ctx_len, "ctx_len", _I32T), _dev(tree_k, "tree_k", _BF16),
+        _dev(tree_v, "tree_v", _BF16), _dev(parent, "parent", _I32T, nullable=True),
+        _dev(tree_len, "tree_len", _I32T, nullable=True), float(scale), _dev(out, "out", _BF16),
+        _dev(lse, "lse", _F32, nullable=True),
+        _dev(workspace, "workspace", (torch.uint8,), nullable=True), _bytes(workspace), _stream(stream)))
+
+
+def oasis_sparse_tree_attn_workspace_bytes(d: OasisDims, num_q_tokens: int, k_slots: int) -> int:
+    return int(lib().oasis_sparse_tree_attn_workspace_bytes(ctypes.byref(d), int(num_q_tokens), int(k_slots)))
+
+
+def oasis_sparse_tree_attn(d: OasisDims, q, num_q_tokens: int, pool_k, pool_v, slot_map, k_slots: int, ctx_len, tree_k,
+                           tree_v, parent, tree_len, scale: float | None, out, lse, workspace, stream=None) -> None:
+    """Attention of a drafted token tree over the working set (parent None: a chain; tree_len None: every row)."""
+    if scale is None:
+        scale = 1.0 / math.sqrt(d.head_dim)
+    R, H, B, D = d.num_reqs, d.num_kv_heads, d.block_size, d.head_dim
+    _tree_needs(d, int(num_q_tokens), q, ctx_len, tree_k, tree_v, parent, tree_len, out, lse)
+    _need(pool_k, R * (k_slots + 1) * H * B * D, "pool_k")
+    _need(pool_v, R * (k_slots + 1) * H * B * D, "pool_v")
+    _need(slot_map, R * H * k_slots, "slot_map")
+    _one_device(q=q, pool_k=pool_k, pool_v=pool_v, slot_map=slot_map, ctx_len=ctx_len, tree_k=tree_k, tree_v=tree_v,
+                parent=parent, tree_len=tree_len, out=out, lse=lse, workspace=workspace)
+    _check("oasis_sparse_tree_attn", lib().oasis_sparse_tree_attn(
+        ctypes.byref(d), _dev(q, "q", _BF16), int(num_q_tokens), _dev(pool_k, "pool_k", _BF16),
+        _dev(pool_v, "pool_v", _BF16), _dev(slot_map, "slot_map", _I32T, nullable=k_slots == 0), int(k_slots),
+        _dev(ctx_len, "ctx_len", _I32T), _dev(tree_k, "tree_k", _BF16), _dev(tree_v, "tree_v", _BF16),
+        _dev(parent, "parent", _I32T, nullable=True), _dev(tree_len, "tree_len", _I32T, nullable=True), float(scale),
+        _dev(out, "out", _BF16), _dev(lse, "lse", _F32, nullable=True),
+        _dev(workspace, "workspace", (torch.uint8,), nullable=True), _bytes(workspace), _stream(stream)))
+
+
+def oasis_verify_workspace_bytes(num_reqs: int, num_q_tokens: int, vocab: int) -> int:
+    return int(lib().oasis_verify_workspace_bytes(int(num_reqs), int(num_q_tokens), int(vocab)))
+
+
+def _prob_rows(t: torch.Tensor, name: str, shape):
+    """Address and row stride of probabilities [R][T][V]: rows dense, evenly spaced (a padded vocabulary may be
+    sliced off)."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if t.dtype is not torch.float32:
+        raise TypeError(f"{name}: dtype {t.dtype}, torch.float32 expected")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, {tuple(shape)} expected")
+    R, T, V = shape
+    row = t.stride(1) if T > 1 else (t.stride(0) if R > 1 else V)
+    if (V > 1 and t.stride(2) != 1) or row < V or (R > 1 and t.stride(0) != T * row):
+        raise ValueError(f"{name}: rows must be contiguous and evenly spaced")
+    return t.data_ptr(), row
+
+
+def oasis_verify_drafts(target_probs, draft_probs, tokens, parent, tree_len, accept_u, sample_u, path, path_len,
+                        out_tokens, workspace, stream=None) -> None:
+    """Accepted path, emitted tokens and next token of each request's drafted tree (target_probs and draft_probs
+    fp32 [R][T][V]; draft_probs None: certain drafts; parent None: a chain; tree_len None: every row)."""
+    if target_probs.dim() != 3:
+        raise ValueError(f"target_probs: {target_probs.dim()} dimensions, [R][T][V] expected")
+    R, T, V = target_probs.shape
+    for t, n, name in ((tokens, R * T, "tokens"), (parent, R * T, "parent"), (tree_len, R, "tree_len"),
+                       (accept_u, R * T, "accept_u"), (sample_u, R, "sample_u"), (path, R * T, "path"),
+                       (path_len, R, "path_len"), (out_tokens, R * T, "out_tokens")):
+        _need(t, n, name)
+    _one_device(target_probs=target_probs, draft_probs=draft_probs, tokens=tokens, parent=parent, tree_len=tree_len,
+                accept_u=accept_u, sample_u=sample_u, path=path, path_len=path_len, out_tokens=out_tokens,
+                workspace=workspace)
+    tp, ts = _prob_rows(target_probs, "target_probs", (R, T, V))
+    dp, ds = (None, 0) if draft_probs is None else _prob_rows(draft_probs, "draft_probs", (R, T, V))
+    _check("oasis_verify_drafts", lib().oasis_verify_drafts(
+        R, T, V, tp, ts, dp, ds, _dev(tokens, "tokens", _I32T), _dev(parent, "parent", _I32T, nullable=True),
+        _dev(tree_len, "tree_len", _I32T, nullable=True), _dev(accept_u, "accept_u", _F32),
+        _dev(sample_u, "sample_u", _F32), _dev(path, "path", _I32T), _dev(path_len, "path_len", _I32T),
+        _dev(out_tokens, "out_tokens", _I32T), _dev(workspace, "workspace", (torch.uint8,), nullable=True),
+        _bytes(workspace), _stream(stream)))
+
+
+def oasis_append_tokens(d: OasisDims, new_k, new_v, num_tokens: int, path, path_len, k_pages, v_pages, block_table,
+                        ctx_len, new_ctx_len, stream=None) -> None:
+    """Rows path[r][:path_len[r]] of new_k / new_v into the paged cache at ctx_len[r] (path None: rows 0, 1, ...;
+    path_len None then: all of them)."""
+    if k_pages.shape != v_pages.shape:
+        raise ValueError("k_pages and v_pages differ in shape")
+    R, H, D, N = d.num_reqs, d.num_kv_heads, d.head_dim, int(num_tokens)
+    for t, n, name in ((new_k, R * N * H * D, "new_k"), (new_v, R * N * H * D, "new_v"), (path, R * N, "path"),
+                       (path_len, R, "path_len"), (block_table, R * d.max_blocks, "block_table"),
+                       (ctx_len, R, "ctx_len"), (new_ctx_len, R, "new_ctx_len")):
+        _need(t, n, name)
+    _one_device(new_k=new_k, new_v=new_v, path=path, path_len=path_len, k_pages=k_pages, v_pages=v_pages,
+                block_table=block_table, ctx_len=ctx_len, new_ctx_len=new_ctx_len)
+    _check("oasis_append_tokens", lib().oasis_append_tokens(
+        ctypes.byref(d), _dev(new_k, "new_k", _BF16), _dev(new_v, "new_v", _BF16), N,
+        _dev(path, "path", _I32T, nullable=True), _dev(path_len, "path_len", _I32T, nullable=True),
+        _host_or_dev(k_pages, "k_pages", _BF16), _host_or_dev(v_pages, "v_pages", _BF16), _pages(d, k_pages, "k_pages"),
+        _dev(block_table, "block_table", _I32T), _dev(ctx_len, "ctx_len", _I32T),
+        _dev(new_ctx_len, "new_ctx_len", _I32T, nullable=True), _stream(stream)))
 
 
 # --- native step issuer --------------------------------------------------------
