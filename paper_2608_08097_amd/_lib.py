@@ -184,6 +184,7 @@ def _bind_fast(L: ctypes.CDLL) -> None:
     try:
         fast = _load_fast()
         built_for = fast.abi_version
+        bind_drafts = fast.bind_drafts if built_for == ABI_VERSION else None
     except (ImportError, AttributeError) as e:
         warnings.warn(f"native marshalling not loaded ({e}): calls go through the slower Python binding. {_BUILD_HINT}",
                       RuntimeWarning, stacklevel=2)
@@ -195,6 +196,8 @@ def _bind_fast(L: ctypes.CDLL) -> None:
     fast.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
         L.oasis_sparse_decode_attn, L.oasis_score_blocks, L.oasis_select_topk, L.oasis_score_select,
         L.oasis_stage_blocks)))
+    bind_drafts(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
+        L.oasis_tree_attn, L.oasis_sparse_tree_attn, L.oasis_verify_drafts, L.oasis_append_tokens)))
     _fast = fast
 
 
@@ -499,6 +502,11 @@ def _tree_needs(d: OasisDims, T: int, q, ctx_len, tree_k, tree_v, parent, tree_l
 def oasis_tree_attn(d: OasisDims, q, num_q_tokens: int, k_pages, v_pages, block_table, ctx_len, tree_k, tree_v,
                     parent, tree_len, scale: float | None, out, lse, workspace, stream=None) -> None:
     """Attention of a drafted token tree over the paged cache (parent None: a chain; tree_len None: every row)."""
+    if _fast is not None and type(d) is OasisDims:
+        st = _fast.tree_attn(ctypes.addressof(d), q, num_q_tokens, k_pages, v_pages, block_table, ctx_len, tree_k, tree_v,
+                             parent, tree_len, scale, out, lse, workspace, _handle(stream))
+        if st is not None:
+            return _check("oasis_tree_attn", st)
     if scale is None:
         scale = 1.0 / math.sqrt(d.head_dim)
     if k_pages.shape != v_pages.shape:
@@ -524,6 +532,11 @@ def oasis_sparse_tree_attn_workspace_bytes(d: OasisDims, num_q_tokens: int, k_sl
 def oasis_sparse_tree_attn(d: OasisDims, q, num_q_tokens: int, pool_k, pool_v, slot_map, k_slots: int, ctx_len, tree_k,
                            tree_v, parent, tree_len, scale: float | None, out, lse, workspace, stream=None) -> None:
     """Attention of a drafted token tree over the working set (parent None: a chain; tree_len None: every row)."""
+    if _fast is not None and type(d) is OasisDims:
+        st = _fast.sparse_tree_attn(ctypes.addressof(d), q, num_q_tokens, pool_k, pool_v, slot_map, k_slots, ctx_len,
+                                    tree_k, tree_v, parent, tree_len, scale, out, lse, workspace, _handle(stream))
+        if st is not None:
+            return _check("oasis_sparse_tree_attn", st)
     if scale is None:
         scale = 1.0 / math.sqrt(d.head_dim)
     R, H, B, D = d.num_reqs, d.num_kv_heads, d.block_size, d.head_dim
@@ -566,6 +579,11 @@ def oasis_verify_drafts(target_probs, draft_probs, tokens, parent, tree_len, acc
                         out_tokens, workspace, stream=None) -> None:
     """Accepted path, emitted tokens and next token of each request's drafted tree (target_probs and draft_probs
     fp32 [R][T][V]; draft_probs None: certain drafts; parent None: a chain; tree_len None: every row)."""
+    if _fast is not None:
+        st = _fast.verify_drafts(target_probs, draft_probs, tokens, parent, tree_len, accept_u, sample_u, path, path_len,
+                                 out_tokens, workspace, _handle(stream))
+        if st is not None:
+            return _check("oasis_verify_drafts", st)
     if target_probs.dim() != 3:
         raise ValueError(f"target_probs: {target_probs.dim()} dimensions, [R][T][V] expected")
     R, T, V = target_probs.shape
@@ -590,6 +608,11 @@ def oasis_append_tokens(d: OasisDims, new_k, new_v, num_tokens: int, path, path_
                         ctx_len, new_ctx_len, stream=None) -> None:
     """Rows path[r][:path_len[r]] of new_k / new_v into the paged cache at ctx_len[r] (path None: rows 0, 1, ...;
     path_len None then: all of them)."""
+    if _fast is not None and type(d) is OasisDims:
+        st = _fast.append_tokens(ctypes.addressof(d), new_k, new_v, num_tokens, path, path_len, k_pages, v_pages,
+                                 block_table, ctx_len, new_ctx_len, _handle(stream))
+        if st is not None:
+            return _check("oasis_append_tokens", st)
     if k_pages.shape != v_pages.shape:
         raise ValueError("k_pages and v_pages differ in shape")
     R, H, D, N = d.num_reqs, d.num_kv_heads, d.head_dim, int(num_tokens)

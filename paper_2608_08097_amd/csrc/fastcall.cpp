@@ -27,6 +27,10 @@ decltype(&oasis_score_blocks) f_score;
 decltype(&oasis_select_topk) f_topk;
 decltype(&oasis_score_select) f_score_select;
 decltype(&oasis_stage_blocks) f_stage;
+decltype(&oasis_tree_attn) f_tree;
+decltype(&oasis_sparse_tree_attn) f_sparse_tree;
+decltype(&oasis_verify_drafts) f_verify;
+decltype(&oasis_append_tokens) f_append;
 
 enum Kind { kBf16, kI32, kF32, kU8 };
 
@@ -236,6 +240,171 @@ PyObject* stage_blocks(PyObject*, Args a, Py_ssize_t n) {
   });
 }
 
+// The calls of the speculative step take tensors of the current device alone.
+bool on_current(Args a, std::initializer_list<int> which) {
+  const auto dev = c10::hip::current_device();
+  for (const int i : which) {
+    if (a[i] == Py_None) continue;
+    const at::Tensor& t = THPVariable_Unpack(a[i]);
+    if (t.is_cuda() && t.device().index() != dev) return false;
+  }
+  return true;
+}
+
+// As tensor(), or None.
+bool optional(PyObject* o, int64_t n, Kind kind, void** p) {
+  *p = nullptr;
+  return o == Py_None || tensor(o, n, kind, p);
+}
+
+// A workspace or None.
+bool workspace_at(PyObject* o, void** p, size_t* bytes) {
+  *p = nullptr;
+  *bytes = 0;
+  if (o == Py_None) return true;
+  if (!any_count(o, kU8, p)) return false;
+  *bytes = (size_t)THPVariable_Unpack(o).numel();
+  return true;
+}
+
+bool scale_at(PyObject* o, int64_t D, float* scale) {
+  if (D <= 0) return false;  // no default scale
+  if (o == Py_None) *scale = (float)(1.0 / std::sqrt((double)D));
+  else if (PyFloat_CheckExact(o)) *scale = (float)PyFloat_AS_DOUBLE(o);
+  else return false;
+  return true;
+}
+
+// Two tiers of the same shape, of whole pages [Hkv][B][d]: their number.
+bool tier_at(PyObject* ko, PyObject* vo, const oasis_dims* d, void** k, void** v, int64_t* pages) {
+  if (!any_count(ko, kBf16, k, true) || !any_count(vo, kBf16, v, true)) return false;
+  const at::Tensor &kt = THPVariable_Unpack(ko), &vt = THPVariable_Unpack(vo);
+  const int64_t per = count({d->num_kv_heads, d->block_size, d->head_dim});
+  if (per < 1 || kt.dim() < 1 || kt.sizes() != vt.sizes() || kt.numel() % per) return false;
+  *pages = kt.numel() / per;
+  return true;
+}
+
+struct Tree {
+  void *ctx, *tk, *tv, *parent, *len, *out, *lse, *ws, *s;
+  size_t bytes;
+  float scale;
+};
+// ctx_len, tree_k, tree_v, parent, tree_len, scale, out, lse, workspace, stream from a[0] on
+bool tree_args(const oasis_dims* d, int32_t T, Args a, Tree* t) {
+  const int64_t R = d->num_reqs, D = d->head_dim, rows = count({R, T, d->num_q_heads}), kv = count({R, T, d->num_kv_heads, D});
+  return tensor(a[0], R, kI32, &t->ctx) && tensor(a[1], kv, kBf16, &t->tk) && tensor(a[2], kv, kBf16, &t->tv) &&
+         optional(a[3], count({R, T}), kI32, &t->parent) && optional(a[4], R, kI32, &t->len) &&
+         scale_at(a[5], D, &t->scale) && tensor(a[6], count({rows, D}), kBf16, &t->out) &&
+         optional(a[7], rows, kF32, &t->lse) && workspace_at(a[8], &t->ws, &t->bytes) && stream_at(a[9], &t->s) &&
+         on_current(a, {0, 1, 2, 3, 4, 6, 7, 8});
+}
+
+// dims, q, num_q_tokens, k_pages, v_pages, block_table, ctx_len, tree_k, tree_v, parent, tree_len, scale, out, lse,
+// workspace, stream
+PyObject* tree_attn(PyObject*, Args a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    if (n != 16) FALLBACK;
+    const oasis_dims* d = dims_at(a[0]);
+    int32_t T;
+    int64_t pages;
+    void *q, *k, *v, *table;
+    Tree t;
+    if (!d || !int32(a[2], &T) || !tensor(a[1], count({d->num_reqs, T, d->num_q_heads, d->head_dim}), kBf16, &q) ||
+        !tier_at(a[3], a[4], d, &k, &v, &pages) || !tensor(a[5], count({d->num_reqs, d->max_blocks}), kI32, &table) ||
+        !tree_args(d, T, a + 6, &t) || !on_current(a, {1, 3, 4, 5}))
+      FALLBACK;
+    return run([&] {
+      return f_tree(d, (const uint16_t*)q, T, (const uint16_t*)k, (const uint16_t*)v, pages, (const int32_t*)table,
+                    (const int32_t*)t.ctx, (const uint16_t*)t.tk, (const uint16_t*)t.tv, (const int32_t*)t.parent,
+                    (const int32_t*)t.len, t.scale, (uint16_t*)t.out, (float*)t.lse, t.ws, t.bytes, t.s);
+    });
+  });
+}
+
+// dims, q, num_q_tokens, pool_k, pool_v, slot_map, k_slots, ctx_len, tree_k, tree_v, parent, tree_len, scale, out, lse,
+// workspace, stream
+PyObject* sparse_tree_attn(PyObject*, Args a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    if (n != 17) FALLBACK;
+    const oasis_dims* d = dims_at(a[0]);
+    int32_t T, ks;
+    void *q, *k, *v, *map;
+    Tree t;
+    if (!d || !int32(a[2], &T) || !int32(a[6], &ks)) FALLBACK;
+    const int64_t R = d->num_reqs, H = d->num_kv_heads;
+    const int64_t pool = count({R, (int64_t)ks + 1, H, d->block_size, d->head_dim});
+    if (!tensor(a[1], count({R, T, d->num_q_heads, d->head_dim}), kBf16, &q) || !tensor(a[3], pool, kBf16, &k) ||
+        !tensor(a[4], pool, kBf16, &v) || !tensor(a[5], count({R, H, ks}), kI32, &map) ||
+        !tree_args(d, T, a + 7, &t) || !on_current(a, {1, 3, 4, 5}))
+      FALLBACK;
+    return run([&] {
+      return f_sparse_tree(d, (const uint16_t*)q, T, (const uint16_t*)k, (const uint16_t*)v, (const int32_t*)map, ks,
+                           (const int32_t*)t.ctx, (const uint16_t*)t.tk, (const uint16_t*)t.tv, (const int32_t*)t.parent,
+                           (const int32_t*)t.len, t.scale, (uint16_t*)t.out, (float*)t.lse, t.ws, t.bytes, t.s);
+    });
+  });
+}
+
+// Probabilities [R][T][V] of dense rows, evenly spaced: their address and row stride.
+bool prob_rows(PyObject* o, int64_t R, int64_t T, int64_t V, void** p, int64_t* row) {
+  if (!THPVariable_CheckExact(o)) return false;
+  const at::Tensor& t = THPVariable_Unpack(o);
+  if (!t.is_cuda() || t.scalar_type() != at::kFloat || t.dim() != 3 || t.size(0) != R || t.size(1) != T || t.size(2) != V)
+    return false;
+  *row = T > 1 ? t.stride(1) : (R > 1 ? t.stride(0) : V);
+  if ((V > 1 && t.stride(2) != 1) || *row < V || (R > 1 && t.stride(0) != T * *row)) return false;
+  *p = t.data_ptr();
+  return true;
+}
+
+// target_probs, draft_probs, tokens, parent, tree_len, accept_u, sample_u, path, path_len, out_tokens, workspace, stream
+PyObject* verify_drafts(PyObject*, Args a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    if (n != 12 || !THPVariable_CheckExact(a[0])) FALLBACK;
+    const at::Tensor& target = THPVariable_Unpack(a[0]);
+    if (target.dim() != 3) FALLBACK;
+    const int64_t R = target.size(0), T = target.size(1), V = target.size(2), RT = count({R, T});
+    if (R > INT32_MAX || T > INT32_MAX || V > INT32_MAX) FALLBACK;
+    void *tp, *dp = nullptr, *tok, *par, *len, *ua, *us, *path, *plen, *out, *ws, *s;
+    int64_t ts, ds = 0;
+    size_t bytes;
+    if (!prob_rows(a[0], R, T, V, &tp, &ts) || (a[1] != Py_None && !prob_rows(a[1], R, T, V, &dp, &ds)) ||
+        !tensor(a[2], RT, kI32, &tok) || !optional(a[3], RT, kI32, &par) || !optional(a[4], R, kI32, &len) ||
+        !tensor(a[5], RT, kF32, &ua) || !tensor(a[6], R, kF32, &us) || !tensor(a[7], RT, kI32, &path) ||
+        !tensor(a[8], R, kI32, &plen) || !tensor(a[9], RT, kI32, &out) || !workspace_at(a[10], &ws, &bytes) ||
+        !stream_at(a[11], &s) || !on_current(a, {0, 1, 2, 3, 4, 5, 6, 7, 8, 9, 10}))
+      FALLBACK;
+    return run([&] {
+      return f_verify((int32_t)R, (int32_t)T, (int32_t)V, (const float*)tp, ts, (const float*)dp, ds, (const int32_t*)tok,
+                      (const int32_t*)par, (const int32_t*)len, (const float*)ua, (const float*)us, (int32_t*)path,
+                      (int32_t*)plen, (int32_t*)out, ws, bytes, s);
+    });
+  });
+}
+
+// dims, new_k, new_v, num_tokens, path, path_len, k_pages, v_pages, block_table, ctx_len, new_ctx_len, stream
+PyObject* append_tokens(PyObject*, Args a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    if (n != 12) FALLBACK;
+    const oasis_dims* d = dims_at(a[0]);
+    int32_t N;
+    int64_t pages;
+    if (!d || !int32(a[3], &N)) FALLBACK;
+    const int64_t R = d->num_reqs, kv = count({R, N, d->num_kv_heads, d->head_dim});
+    void *nk, *nv, *path, *plen, *k, *v, *table, *ctx, *end, *s;
+    if (!tensor(a[1], kv, kBf16, &nk) || !tensor(a[2], kv, kBf16, &nv) || !optional(a[4], count({R, N}), kI32, &path) ||
+        !optional(a[5], R, kI32, &plen) || !tier_at(a[6], a[7], d, &k, &v, &pages) ||
+        !tensor(a[8], count({R, d->max_blocks}), kI32, &table) || !tensor(a[9], R, kI32, &ctx) ||
+        !optional(a[10], R, kI32, &end) || !stream_at(a[11], &s) || !on_current(a, {1, 2, 4, 5, 6, 7, 8, 9, 10}))
+      FALLBACK;
+    return run([&] {
+      return f_append(d, (const uint16_t*)nk, (const uint16_t*)nv, N, (const int32_t*)path, (const int32_t*)plen,
+                      (uint16_t*)k, (uint16_t*)v, pages, (const int32_t*)table, (const int32_t*)ctx, (int32_t*)end, s);
+    });
+  });
+}
+
 // bind(attn, score, topk, score_select, stage): addresses of the library's entry points
 PyObject* bind(PyObject*, Args a, Py_ssize_t n) {
   void* p[5];
@@ -252,9 +421,25 @@ PyObject* bind(PyObject*, Args a, Py_ssize_t n) {
   Py_RETURN_NONE;
 }
 
+// bind_drafts(tree_attn, sparse_tree_attn, verify, append): addresses of the library's entry points
+PyObject* bind_drafts(PyObject*, Args a, Py_ssize_t n) {
+  void* p[4];
+  if (n != 4) return PyErr_Format(PyExc_TypeError, "bind_drafts takes 4 addresses");
+  for (int i = 0; i < 4; ++i) {
+    p[i] = PyLong_AsVoidPtr(a[i]);
+    if (!p[i]) return PyErr_Occurred() ? nullptr : PyErr_Format(PyExc_ValueError, "bind_drafts: null address");
+  }
+  f_tree = reinterpret_cast<decltype(f_tree)>(p[0]);
+  f_sparse_tree = reinterpret_cast<decltype(f_sparse_tree)>(p[1]);
+  f_verify = reinterpret_cast<decltype(f_verify)>(p[2]);
+  f_append = reinterpret_cast<decltype(f_append)>(p[3]);
+  Py_RETURN_NONE;
+}
+
 #define METHOD(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(bind),         METHOD(sparse_decode_attn), METHOD(score_blocks), METHOD(select_topk),
-                         METHOD(score_select), METHOD(stage_blocks),       {nullptr, nullptr, 0, nullptr}};
+                         METHOD(score_select), METHOD(stage_blocks),       METHOD(bind_drafts),  METHOD(tree_attn),
+                         METHOD(sparse_tree_attn), METHOD(verify_drafts),  METHOD(append_tokens), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -561,3 +561,49 @@ def test_binding_checks_on_the_device():
         P.oasis_append_tokens(m.d, s["k"], s["v"], m.T, None, None, m.dk.cpu(), m.dv.cpu(), m.dtable, m.ctx[0], None)
     with pytest.raises(P.OasisError, match="new_ctx_len is ctx_len"):
         P.oasis_append_tokens(m.d, s["k"], s["v"], m.T, None, None, m.dk, m.dv, m.dtable, m.ctx[0], m.ctx[0])
+
+
+def test_native_marshalling_takes_the_plain_calls_alone():
+    """The step's calls go through the native marshalling (status 0), give what the Python binding gives, and hand every
+    other form back to it."""
+    import ctypes
+    L = P._lib
+    ms = [_Loop(), _Loop()]
+    keep = L._fast
+    for m, fast in zip(ms, (keep, None)):
+        L._fast = fast
+        try:
+            for i in range(2):
+                m.step(i, m.dev[i])
+        finally:
+            L._fast = keep
+    torch.cuda.synchronize()
+    for a, b in zip((ms[0].dk, ms[0].dv, ms[0].out, *ms[0].ints), (ms[1].dk, ms[1].dv, ms[1].out, *ms[1].ints)):
+        assert torch.equal(a, b)
+    m, s = ms[0], ms[0].dev[0]
+    d = ctypes.addressof(m.d)
+    smap = torch.full((m.R, m.Hkv, 11), -1, dtype=torch.int32, device="cuda")
+    pv = torch.zeros(m.R, 12, m.Hkv, 128, m.B, dtype=torch.bfloat16, device="cuda")
+    calls = {
+        "tree_attn": [d, s["q"], m.T, m.dk, m.dv, m.dtable, m.ctx[0], s["k"], s["v"], m.dparent, None, None, m.out, None,
+                      m.ws, None],
+        "sparse_tree_attn": [d, s["q"], m.T, m.dk, pv, smap, 11, m.ctx[0], s["k"], s["v"], m.dparent, None, 0.5, m.out,
+                             None, torch.zeros(1 << 20, dtype=torch.uint8, device="cuda"), None],
+        "verify_drafts": [m.probs, None, s["tokens"], None, None, s["ua"], s["us"], *m.ints, m.ws, None],
+        "append_tokens": [d, s["k"], s["v"], m.T, m.ints[0], m.ints[1], m.dk, m.dv, m.dtable, m.ctx[0], m.ctx[1], None],
+    }
+    wrong = {"tree_attn": {1: s["q"].float(), 2: -1, 3: m.dk[:-1], 5: m.dtable[:1], 6: m.ctx[0].long(), 7: s["k"][:1],
+                           9: m.dparent.cpu(), 11: 1, 12: m.out.transpose(0, 1), 14: m.out, 15: "0"},
+             "sparse_tree_attn": {3: m.dk[:-1], 6: 12, 5: None, 8: s["v"][:, :1], 14: m.out},
+             "verify_drafts": {0: m.probs.double(), 1: m.probs[:, :, :-1], 2: None, 5: s["ua"].double(), 6: s["ua"],
+                               7: m.ints[1], 10: m.out},
+             "append_tokens": {1: s["k"].float(), 3: 1 << 40, 4: m.ints[1], 6: m.dk[:-1], 8: None, 10: m.ctx[1].long()}}
+    for name, args in calls.items():
+        note(f"native marshalling of {name}")
+        assert getattr(keep, name)(*args) == 0
+        assert getattr(keep, name)(*args[:-1]) is None
+        for i, x in wrong[name].items():
+            bad = list(args)
+            bad[i] = x
+            assert getattr(keep, name)(*bad) is None, (name, i)
+    torch.cuda.synchronize()
