@@ -42,7 +42,7 @@ def flags() -> list[str]:
 # results in VGPRs; otherwise the compiler parks the attention's accumulators in
 # AGPRs and copies all 64 of them to VGPRs on every unit for the rare rescale
 # path.
-FILE_FLAGS = {"attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+FILE_FLAGS = {f: ["-mllvm", "-amdgpu-mfma-vgpr-form"] for f in ("attn.hip", "tree_attn.hip")}
 
 
 FASTCALL_PATH = os.path.join(PKG_DIR, "_fastcall.so")

@@ -5,25 +5,26 @@
 // on its path to the root, itself among them: out = softmax(scale q K^T) V over
 // the two sets together, one pass with a running maximum and sum.
 //
-// Work decomposition. Cached tokens come in units of 32; a workgroup of four
-// waves takes a run of a (request, KV head) pair's units for up to four 16-row
-// tiles, every wave a strided subset of the units with its own online softmax.
-// The tree's tokens are one or two more units, with a mask per row, that the last
-// split's waves take after their own. The waves merge through LDS, the splits
-// through the workspace and a second kernel.
-//
-// One unit for one 16-row tile is, as in the working set's attention,
+// One 32-token unit of keys and values for one 16-row tile is, as in the working
+// set's attention,
 //   S^T (tokens x rows) = K . Q^T     8 of v_mfma_f32_16x16x32_bf16
 //   O^T (d x rows)     += V^T . P^T   8 of them
 // with the tokens dealt to MFMA rows so that lane (g, n) holds row n's scores of
 // unit tokens 8g .. 8g+7, which makes the probabilities directly the B operand of
 // the second product: no cross-lane movement and no LDS for P. The A operand of
-// that product needs V[8g .. 8g+7][one d] in a lane. The working set keeps V
-// transposed, so it is one load per d-tile (d = 16 dt + i). Pages keep V
-// token-major: there lane (g, i) loads dims 8i .. 8i+7 of each of its 8 tokens (a
-// wave reads whole rows) and transposes the 8 x 8 block in registers, 32 byte
-// permutes a unit; d-tile j is then the dims d = 8i + j, and a lane's outputs of
-// one row are 32 consecutive dims.
+// that product is 8 tokens of one dim in a lane. The working set keeps V
+// transposed, so it is one load; pages keep V token-major.
+//
+// Two forms. Up to two row tiles (G * T <= 32) bandwidth bounds everything and
+// tree_attn_kernel streams K and V from HBM straight into MFMA registers, four
+// waves a workgroup, every wave a strided subset of the units with its own online
+// softmax; token-major V is transposed in registers, 8 x 8 blocks, 32 byte
+// permutes a unit. With more rows tree_attn_rows_kernel brings each unit's K and V
+// into LDS once for eight waves, which hold different row tiles; token-major V is
+// read back with the transposing LDS read.
+//
+// The tree's own tokens are one or two more units, with a mask per row, in the
+// last split of every pair. Splits leave partials that a second kernel merges.
 #include "drafts_internal.h"
 
 namespace oasis {
@@ -68,25 +69,35 @@ __device__ __forceinline__ void clear_tokens(u32x4 (&v)[8], int keep) {
   }
 }
 
-__device__ __forceinline__ bool odd_bf16(uint32_t b) { return (b & 0x7F80u) == 0x7F80u; }  // infinity or NaN
-
-// First dim of the 4 that element quad dt of a lane's accumulators holds, and
-// whether the quad runs over e (dims d0 + e) or over tiles: see store_dims.
-template <bool PAGED>
-__device__ __forceinline__ int acc_dim(int dt, int g, int e) {
-  return PAGED ? 32 * g + 8 * e + dt : 16 * dt + 4 * g + e;
+// The tree's values: a row that attends a token takes up its infinities and NaN,
+// the other rows must not, but 0 times them is NaN in the product. So they are
+// taken out of the product (true: there were some) and added to the rows that
+// attend them when those are written (add_wild).
+__device__ __forceinline__ bool wild_bf16(uint32_t b) { return (b & 0x7F80u) == 0x7F80u; }
+__device__ __forceinline__ bool take_wild(u32x4 (&v)[8]) {
+  uint32_t any = 0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+      // an exponent of ones carries into the sign's place
+      const uint32_t m = ((v[j][p] & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
+      any |= m;
+      v[j][p] &= ~((m >> 15) * 0xFFFFu);
+    }
+  return __builtin_amdgcn_ballot_w64(any != 0) != 0;
 }
 
 // Scores of one unit for one tile: lane (g, n) gets row n against tokens 8g .. 8g+7.
-__device__ __forceinline__ void unit_scores(const TreeUnit& u, const bf16x8 (&qb)[4], float scale_log2, float (&x)[8]) {
+__device__ __forceinline__ void unit_scores(const u32x4 (&k)[2][4], const bf16x8 (&qb)[4], float scale_log2,
+                                            float (&x)[8]) {
   f32x4 sc[2];
+  sc[0] = sc[1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int tau = 0; tau < 2; ++tau) {
-    sc[tau] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int st = 0; st < 4; ++st)
 #pragma unroll
-    for (int st = 0; st < 4; ++st)
-      sc[tau] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(u.k[tau][st]), qb[st], sc[tau], 0, 0, 0);
-  }
+    for (int tau = 0; tau < 2; ++tau)
+      sc[tau] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(k[tau][st]), qb[st], sc[tau], 0, 0, 0);
 #pragma unroll
   for (int e = 0; e < 8; ++e) x[e] = sc[e >> 2][e & 3] * scale_log2;
 }
@@ -120,10 +131,10 @@ __device__ __forceinline__ bf16x8 unit_softmax(const float (&x)[8], float& m_ref
   return pb;
 }
 
-__device__ __forceinline__ void unit_pv(const TreeUnit& u, bf16x8 pb, f32x4 (&acc)[8]) {
+__device__ __forceinline__ void unit_pv(const u32x4 (&v)[8], bf16x8 pb, f32x4 (&acc)[8]) {
 #pragma unroll
   for (int dt = 0; dt < 8; ++dt)
-    acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(u.v[dt]), pb, acc[dt], 0, 0, 0);
+    acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(v[dt]), pb, acc[dt], 0, 0, 0);
 }
 
 // Ancestor masks of a request's tree, lane t: row t's (its own bit among them).
@@ -168,51 +179,162 @@ __device__ __forceinline__ int tree_length(const TreeAttnArgs& a, int r) {
   return n < 0 ? 0 : (n > a.T ? a.T : n);
 }
 
+// What a workgroup works on.
+struct TreeItem {
+  int r, h, rh, split, row0, tlen;
+  long long unit_elems;   // of a page or a slot
+  const uint16_t *kb, *vb;  // this head's part of the pages, or of the request's slots
+  const int32_t* tab;     // the request's block table, or the pair's slot map
+  long long tree_row, tree_base;  // elements between the tree's rows, and to this head's first one
+};
+template <int BS, bool PAGED>
+__device__ __forceinline__ bool tree_setup(const TreeAttnArgs& a, int group_rows, TreeItem& t) {
+  const int item = tree_item(blockIdx.x, a.R * a.Hkv * a.nsplit * a.groups);
+  if (item < 0) return false;
+  const int rs = item / a.groups;
+  t.row0 = (item - rs * a.groups) * group_rows;
+  t.rh = rs / a.nsplit;
+  t.split = rs - t.rh * a.nsplit;
+  t.r = t.rh / a.Hkv;
+  t.h = t.rh - t.r * a.Hkv;
+  t.unit_elems = (long long)a.Hkv * BS * kHeadDim;
+  const long long base = (PAGED ? 0 : (long long)t.r * (a.k_slots + 1) * t.unit_elems) + (long long)t.h * BS * kHeadDim;
+  t.kb = a.k + base;
+  t.vb = a.v + base;
+  t.tab = a.table + (PAGED ? (long long)t.r * a.NBmax : (long long)t.rh * a.k_slots);
+  t.tree_row = (long long)a.Hkv * kHeadDim;
+  t.tree_base = (long long)t.r * a.T * t.tree_row + (long long)t.h * kHeadDim;
+  t.tlen = tree_length(a, t.r);
+  return t.row0 < t.tlen * a.G;  // else no row of this group is in the tree
+}
+
+// The cached tokens of request r and the units [begin, end) of a split of them.
+template <int BS, bool PAGED>
+__device__ __forceinline__ Ctx tree_units(const TreeAttnArgs& a, const TreeItem& t, int& L, int& begin, int& end) {
+  const Ctx c = ctx_blocks(a.ctx_len[t.r], BS, a.NBmax);
+  L = c.nb ? c.n_cand * BS + c.local_len : 0;
+  const int nu = PAGED ? (L + 31) / 32 : (BS == 16 ? (a.k_slots + 2) / 2 : a.k_slots + 1);
+  begin = (int)((long long)nu * t.split / a.nsplit);
+  end = (int)((long long)nu * (t.split + 1) / a.nsplit);
+  return c;
+}
+
+// Table entry of block b: its place (page or slot; a valid one where nothing of it
+// is attended) and its attended tokens.
+template <int BS, bool PAGED>
+__device__ __forceinline__ int block_raw(const TreeAttnArgs& a, const TreeItem& t, const Ctx& c, int b) {
+  if constexpr (PAGED) return b < c.nb ? t.tab[b] : -1;
+  else return b < a.k_slots ? t.tab[b] : (b == a.k_slots ? 0 : -1);
+}
+template <int BS, bool PAGED>
+__device__ __forceinline__ void block_entry(const TreeAttnArgs& a, const Ctx& c, int L, int b, int raw, int& place,
+                                            int& count) {
+  if constexpr (PAGED) {
+    const bool ok = raw >= 0 && raw < a.num_pages;
+    const int n = L - b * BS;
+    place = ok ? raw : 0;
+    count = ok ? (n < BS ? n : BS) : 0;
+  } else {
+    place = b <= a.k_slots ? b : 0;
+    count = raw < 0 ? 0 : (b == a.k_slots ? c.local_len : BS);
+  }
+}
+
+// Q^T operand of the tile whose first row is `first`: lane (g, i) holds row first + i.
+__device__ __forceinline__ void load_q(const TreeAttnArgs& a, const TreeItem& t, int first, int g, int i, bf16x8 (&qb)[4]) {
+  const int row = first + i;
+  const int tq = row < a.rows ? row / a.G : 0;
+  const int qh = t.h * a.G + (row < a.rows ? row - tq * a.G : 0);
+  const uint16_t* qrow = a.q + (((long long)t.r * a.T + tq) * a.Hq + qh) * kHeadDim;
+#pragma unroll
+  for (int st = 0; st < 4; ++st) {
+    const u32x4 x = ldg16(qrow + st * 32 + g * 8);
+    qb[st] = as_bf16x8(row < a.rows ? x : u32x4{0, 0, 0, 0});
+  }
+}
+
+// The infinities and NaN that row `row` attends in the tree, in dims 4 c4 .. +3.
+__device__ __forceinline__ void add_wild(const TreeAttnArgs& a, const TreeItem& t, uint64_t anc, int c4, f32x4& o) {
+  for (; anc; anc &= anc - 1) {
+    const int j = __builtin_ctzll(anc);
+    const uint2 w = *reinterpret_cast<const uint2*>(a.tree_v + t.tree_base + j * t.tree_row + c4 * 4);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t b = (e < 2 ? w.x : w.y) >> (e & 1) * 16 & 0xFFFFu;
+      if (wild_bf16(b)) o[e] += bf16_bits_to_f32(b);
+    }
+  }
+}
+
 template <int NT, int BS, bool PAGED>
 __global__ __launch_bounds__(kTW * 64) void tree_attn_kernel(TreeAttnArgs a) {
+  static_assert(NT <= 2, "three or more row tiles take tree_attn_rows_kernel");
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
   const int g = lane >> 4;
   const int i = lane & 15;
-  const int item = tree_item(blockIdx.x, a.R * a.Hkv * a.nsplit * a.groups);
-  if (item < 0) return;
-  const int rg = item % a.groups;
-  const int rs = item / a.groups;
-  const int split = rs % a.nsplit;
-  const int rh = rs / a.nsplit;
-  const int r = rh / a.Hkv;
-  const int h = rh - r * a.Hkv;
-  const int tlen = tree_length(a, r);
-  const int row0 = rg * NT * 16;
-  if (row0 >= tlen * a.G) return;  // no row of this group is in the tree
+  TreeItem t;
+  if (!tree_setup<BS, PAGED>(a, NT * 16, t)) return;
+  int L, u_begin, u_end;
+  const Ctx c = tree_units<BS, PAGED>(a, t, L, u_begin, u_end);
 
-  const long long unit_elems = (long long)a.Hkv * BS * kHeadDim;  // a page, or a slot
-  const int ks = a.k_slots;
-  const Ctx c = ctx_blocks(a.ctx_len[r], BS, a.NBmax);
-  const int L = c.nb ? c.n_cand * BS + c.local_len : 0;
-  const int nu = PAGED ? (L + 31) / 32 : (BS == 16 ? (ks + 2) / 2 : ks + 1);
-  const int u_begin = (int)((long long)nu * split / a.nsplit);
-  const int u_end = (int)((long long)nu * (split + 1) / a.nsplit);
-  const long long base = (PAGED ? 0 : (long long)r * (ks + 1) * unit_elems) + (long long)h * BS * kHeadDim;
-  const uint16_t* kb = a.k + base;
-  const uint16_t* vb = a.v + base;
-  const int32_t* tab = a.table + (PAGED ? (long long)r * a.NBmax : (long long)rh * ks);
+  // A wave's units are u_begin + wave + n * kTW. For kChunk of them at a time, lane
+  // e holds the place and the attended tokens of one block: block e % 2 of unit
+  // e / 2 at B = 16, of unit e at B = 32. The next chunk's table entries are on
+  // their way while a chunk is attended.
+  constexpr int kPer = 32 / BS;  // blocks per unit
+  constexpr int kChunk = 64 / kPer;
+  const int u_first = u_begin + wave;
+  const int nt = u_first < u_end ? (u_end - u_first + kTW - 1) / kTW : 0;
+  auto entry_block = [&](int n0) { return (u_first + (n0 + lane / kPer) * kTW) * kPer + lane % kPer; };
+  auto entry_load = [&](int n0) -> int {
+    return n0 + lane / kPer < nt ? block_raw<BS, PAGED>(a, t, c, entry_block(n0)) : -1;
+  };
+  int n0 = 0, place, count;  // of this lane's block of the current chunk
+  uint64_t live;             // blocks of the chunk with an attended token, not yet taken
+  int raw = entry_load(0);
+  auto chunk_set = [&]() __attribute__((always_inline)) {
+    block_entry<BS, PAGED>(a, c, L, entry_block(n0), raw, place, count);
+    raw = entry_load(n0 + kChunk);
+    live = __builtin_amdgcn_ballot_w64(count > 0);
+  };
+  struct Next {
+    int p0, p1, n0, n1;
+    bool any;
+  };
+  // The wave's next unit with an attended token.
+  auto next = [&]() __attribute__((always_inline)) {
+    while (!live && n0 + kChunk < nt) {
+      n0 += kChunk;
+      chunk_set();
+    }
+    if (!live) return Next{0, 0, 0, 0, false};
+    const int p = __builtin_ctzll(live) / kPer * kPer;
+    live &= ~(((1ull << kPer) - 1) << p);
+    return Next{__builtin_amdgcn_readlane(place, p), __builtin_amdgcn_readlane(place, p + kPer - 1),
+                __builtin_amdgcn_readlane(count, p), __builtin_amdgcn_readlane(count, p + kPer - 1), true};
+  };
+  const uint32_t tok = 8 * (i >> 2) + (i & 3);  // K: token tile tau -> unit token tok + 4 tau
+  const uint32_t ko = (BS == 16 ? tok & 15 : tok) * kHeadDim + g * 8;
+  const uint32_t vo = PAGED ? (uint32_t)((BS == 16 ? g & 1 : g) * 8 * kHeadDim + i * 8)
+                            : (uint32_t)(i * BS + (BS == 16 ? g & 1 : g) * 8);
+  // Loads are issued for a wave without a next unit too, every lane on the first
+  // bytes of place 0: the same number on every path keeps the compiler's wait
+  // counts exact, so that waiting for one unit never drains the one behind it.
+  auto load = [&](TreeUnit& u, const Next& n) __attribute__((always_inline)) {
+    const uint16_t* ku = t.kb + (long long)(BS == 16 && i >= 8 ? n.p1 : n.p0) * t.unit_elems + (n.any ? ko : 0u);
+    const uint16_t* vu = t.vb + (long long)(BS == 16 && g >= 2 ? n.p1 : n.p0) * t.unit_elems + (n.any ? vo : 0u);
+#pragma unroll
+    for (int tau = 0; tau < 2; ++tau)
+#pragma unroll
+      for (int st = 0; st < 4; ++st) u.k[tau][st] = ldg16(ku + tau * 4 * kHeadDim + st * 32);
+#pragma unroll
+    for (int dt = 0; dt < 8; ++dt) u.v[dt] = ldg16(vu + (PAGED ? dt * kHeadDim : dt * 16 * BS));
+  };
 
   bf16x8 qb[NT][4];
 #pragma unroll
-  for (int v = 0; v < NT; ++v) {
-    const int row = row0 + v * 16 + i;
-    if (row < a.rows) {
-      const int tq = row / a.G;
-      const int qh = h * a.G + (row - tq * a.G);
-      const uint16_t* qrow = a.q + (((long long)r * a.T + tq) * a.Hq + qh) * kHeadDim;
-#pragma unroll
-      for (int st = 0; st < 4; ++st) qb[v][st] = as_bf16x8(ldg16(qrow + st * 32 + g * 8));
-    } else {
-#pragma unroll
-      for (int st = 0; st < 4; ++st) qb[v][st] = as_bf16x8(u32x4{0, 0, 0, 0});
-    }
-  }
+  for (int v = 0; v < NT; ++v) load_q(a, t, t.row0 + v * 16, g, i, qb[v]);
   float m_run[NT], l_run[NT];
   f32x4 acc[NT][8];
 #pragma unroll
@@ -222,166 +344,95 @@ __global__ __launch_bounds__(kTW * 64) void tree_attn_kernel(TreeAttnArgs a) {
 #pragma unroll
     for (int dt = 0; dt < 8; ++dt) acc[v][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-
-  // A wave's units are u_begin + wave + t * kTW. For kChunk of them at a time, lane
-  // e holds the place (page or slot) and the attended tokens of one block: block
-  // e % 2 of unit e / 2 at B = 16, of unit e at B = 32.
-  constexpr int kPer = 32 / BS;  // blocks per unit
-  constexpr int kChunk = 64 / kPer;
-  const int u_first = u_begin + wave;
-  const int nt = u_first < u_end ? (u_end - u_first + kTW - 1) / kTW : 0;
-  auto entry_block = [&](int t0) { return (u_first + (t0 + lane / kPer) * kTW) * kPer + lane % kPer; };
-  auto entry_load = [&](int t0) -> int {
-    const int b = entry_block(t0);
-    if (t0 + lane / kPer >= nt) return -1;
-    if constexpr (PAGED) return b < c.nb ? tab[b] : -1;
-    else return b < ks ? tab[b] : (b == ks ? 0 : -1);
-  };
-  int place = 0, count = 0;  // of this lane's block of the current chunk
-  auto entry_set = [&](int t0, int raw) {
-    const int b = entry_block(t0);
-    if constexpr (PAGED) {
-      const bool ok = raw >= 0 && raw < a.num_pages;
-      place = ok ? raw : 0;
-      const int n = L - b * BS;
-      count = ok ? (n < BS ? n : BS) : 0;
-    } else {
-      place = b <= ks ? b : 0;
-      count = raw < 0 ? 0 : (b == ks ? c.local_len : BS);
-    }
-  };
-  // units with an attended token, bit per block
-  auto next_live = [&](uint64_t live, int p) -> int {  // first unit >= p of the chunk, kChunk: none
-    const uint64_t rest = p < kChunk ? live >> (p * kPer) : 0;
-    return rest ? p + __builtin_ctzll(rest) / kPer : kChunk;
-  };
-  const uint32_t tok = 8 * (i >> 2) + (i & 3);
-  const uint32_t ko = ((BS == 16 ? tok & 15 : tok) * kHeadDim + g * 8);
-  const uint32_t vo = PAGED ? (uint32_t)((BS == 16 ? g & 1 : g) * 8 * kHeadDim + i * 8)
-                            : (uint32_t)(i * BS + (BS == 16 ? g & 1 : g) * 8);
-  auto load = [&](TreeUnit& u, int p0, int p1) __attribute__((always_inline)) {
-    const uint16_t* ku = kb + (long long)(BS == 16 && i >= 8 ? p1 : p0) * unit_elems + ko;
-    const uint16_t* vu = vb + (long long)(BS == 16 && g >= 2 ? p1 : p0) * unit_elems + vo;
-#pragma unroll
-    for (int tau = 0; tau < 2; ++tau)
-#pragma unroll
-      for (int st = 0; st < 4; ++st) u.k[tau][st] = ldg16(ku + tau * 4 * kHeadDim + st * 32);
-#pragma unroll
-    for (int dt = 0; dt < 8; ++dt) u.v[dt] = ldg16(vu + (PAGED ? dt * kHeadDim : dt * 16 * BS));
-  };
-  auto run = [&](TreeUnit& u, int n0, int n1) __attribute__((always_inline)) {
+  auto run = [&](TreeUnit& u, const Next& nx) __attribute__((always_inline)) {
     if constexpr (PAGED) transpose8(u.v);
-    const int n = BS == 16 ? (g < 2 ? n0 : n1) - (g & 1) * 8 : n0 - g * 8;
+    const int n = BS == 16 ? (g < 2 ? nx.n0 : nx.n1) - (g & 1) * 8 : nx.n0 - g * 8;
     const int keep = n < 0 ? 0 : (n > 8 ? 8 : n);
     const bool partial = __builtin_amdgcn_ballot_w64(keep < 8) != 0;
     if (partial) clear_tokens(u.v, keep);  // 0 times what an unused place holds must stay 0
 #pragma unroll
     for (int v = 0; v < NT; ++v) {
       float x[8];
-      unit_scores(u, qb[v], a.scale_log2, x);
+      unit_scores(u.k, qb[v], a.scale_log2, x);
       if (partial) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = e < keep ? x[e] : -INFINITY;
       }
-      unit_pv(u, unit_softmax(x, m_run[v], l_run[v], acc[v]), acc[v]);
+      unit_pv(u.v, unit_softmax(x, m_run[v], l_run[v], acc[v]), acc[v]);
     }
   };
-
-  for (int t0 = 0; t0 < nt; t0 += kChunk) {
-    entry_set(t0, entry_load(t0));
-    const uint64_t live = __builtin_amdgcn_ballot_w64(count > 0);
-    for (int p = next_live(live, 0); p < kChunk; p = next_live(live, p + 1)) {
-      TreeUnit u;
-      const int p0 = __builtin_amdgcn_readlane(place, p * kPer), p1 = __builtin_amdgcn_readlane(place, p * kPer + kPer - 1);
-      const int n0 = __builtin_amdgcn_readlane(count, p * kPer), n1 = __builtin_amdgcn_readlane(count, p * kPer + kPer - 1);
-      load(u, p0, p1);
-      run(u, n0, n1);
-    }
-  }
 
   constexpr int kRows = NT * 16;
   constexpr int kPad = kHeadDim + 4;
   __shared__ float s_m[kTW][kRows], s_l[kTW][kRows], s_ml[2][kRows];
+  __shared__ uint64_t s_anc[kTreeMaxTokens];
+  __shared__ int s_wild[kTW];
   __shared__ __align__(16) float s_o[kTW][kRows][kPad];
 
-  // ---- the tree's own tokens: unit tu of them to wave tu of the last split ----
+  TreeUnit ua, ub;
+  chunk_set();
+  Next na = next();
+  load(ua, na);
+
+  // ---- the tree's own tokens: unit tu of them to wave tu of the last split, while
+  // the first unit of the cache is on its way ----
   const int tu = wave;
-  if (split == a.nsplit - 1 && tu * 32 < tlen) {
-    const uint64_t anc = ancestors(a.parent ? a.parent + (long long)r * a.T : nullptr, a.T, tlen, lane);
-    const long long row_elems = (long long)a.Hkv * kHeadDim;
-    const long long tb = (long long)r * a.T * row_elems + (long long)h * kHeadDim;
-    TreeUnit u;
+  int wild = 0;
+  if (t.split == a.nsplit - 1 && tu * 32 < t.tlen) {
+    const uint64_t anc = ancestors(a.parent ? a.parent + (long long)t.r * a.T : nullptr, a.T, t.tlen, lane);
+    if (wave == 0) s_anc[lane] = anc;
 #pragma unroll
     for (int tau = 0; tau < 2; ++tau) {
-      const int j = min(tu * 32 + (int)tok + 4 * tau, tlen - 1);
+      const int j = min(tu * 32 + (int)tok + 4 * tau, t.tlen - 1);
 #pragma unroll
-      for (int st = 0; st < 4; ++st) u.k[tau][st] = ldg16(a.tree_k + tb + j * row_elems + st * 32 + g * 8);
+      for (int st = 0; st < 4; ++st) ub.k[tau][st] = ldg16(a.tree_k + t.tree_base + j * t.tree_row + st * 32 + g * 8);
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const int j = min(tu * 32 + 8 * g + e, tlen - 1);
-      u.v[e] = ldg16(a.tree_v + tb + j * row_elems + i * 8);
+      const int j = min(tu * 32 + 8 * g + e, t.tlen - 1);
+      ub.v[e] = ldg16(a.tree_v + t.tree_base + j * t.tree_row + i * 8);
     }
-    transpose8(u.v);
-    const int n = tlen - tu * 32 - 8 * g;
-    clear_tokens(u.v, n < 0 ? 0 : (n > 8 ? 8 : n));
-    // A value that is not finite counts for the rows that attend it alone: it is
-    // taken out of the product (where 0 times it would spoil every row) and added to
-    // those rows below.
-    bool odd = false;
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        if (odd_bf16(u.v[j][w])) odd = true, u.v[j][w] &= 0xFFFF0000u;
-        if (odd_bf16(u.v[j][w] >> 16)) odd = true, u.v[j][w] &= 0x0000FFFFu;
-      }
-    const uint64_t any_odd = __builtin_amdgcn_ballot_w64(odd);
+    transpose8(ub.v);
+    const int n = t.tlen - tu * 32 - 8 * g;
+    clear_tokens(ub.v, n < 0 ? 0 : (n > 8 ? 8 : n));
+    wild = take_wild(ub.v);
     if constexpr (!PAGED) {
       // the working set's accumulators hold d-tile dt = dims 16 dt + i: through LDS,
       // [dim][32 tokens], each wave in its own part of the merge area
       u32x4* sv = reinterpret_cast<u32x4*>(&s_o[wave][0][0]);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) sv[(8 * i + j) * 4 + g] = u.v[j];
-      __builtin_amdgcn_wave_barrier();
+      for (int j = 0; j < 8; ++j) sv[(8 * i + j) * 4 + g] = ub.v[j];
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
-      for (int dt = 0; dt < 8; ++dt) u.v[dt] = sv[(16 * dt + i) * 4 + g];
+      for (int dt = 0; dt < 8; ++dt) ub.v[dt] = sv[(16 * dt + i) * 4 + g];
     }
 #pragma unroll
     for (int v = 0; v < NT; ++v) {
-      const int row = row0 + v * 16 + i;
-      const int t = row < a.rows ? row / a.G : 0;
-      const uint64_t mine = (uint64_t)__shfl((uint32_t)(anc >> 32), t) << 32 | (uint32_t)__shfl((uint32_t)anc, t);
-      const uint32_t bits = (uint32_t)(mine >> (tu * 32 + 8 * g)) & 0xFF;
+      const int row = t.row0 + v * 16 + i;
+      const int tq = row < a.rows ? row / a.G : 0;
+      const uint32_t half = __shfl((uint32_t)(anc >> (tu * 32)), tq);
+      const uint32_t bits = half >> (8 * g) & 0xFF;
       float x[8];
-      unit_scores(u, qb[v], a.scale_log2, x);
+      unit_scores(ub.k, qb[v], a.scale_log2, x);
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[e] = bits >> e & 1 ? x[e] : -INFINITY;
-      const bf16x8 pb = unit_softmax(x, m_run[v], l_run[v], acc[v]);
-      unit_pv(u, pb, acc[v]);
-      if (any_odd) {
-        const float m_use = m_run[v] == -INFINITY ? 0.f : m_run[v];
-        for (int e = 0; e < 8; ++e)
-          for (int gg = 0; gg < 4; ++gg) {
-            const int j = tu * 32 + 8 * gg + e;
-            if (j >= tlen) break;
-            float xe = x[0];
-#pragma unroll
-            for (int f = 1; f < 8; ++f) xe = e == f ? x[f] : xe;
-            const float p = __shfl(fast_exp2(xe - m_use), gg * 16 + i);
-            if (!(mine >> j & 1)) continue;
-            const uint16_t* vr = a.tree_v + tb + j * row_elems;
-#pragma unroll
-            for (int dt = 0; dt < 8; ++dt)
-#pragma unroll
-              for (int f = 0; f < 4; ++f) {
-                const uint32_t b = vr[acc_dim<PAGED>(dt, g, f)];
-                if (odd_bf16(b)) acc[v][dt][f] += p * bf16_bits_to_f32(b);
-              }
-          }
-      }
+      unit_pv(ub.v, unit_softmax(x, m_run[v], l_run[v], acc[v]), acc[v]);
     }
+  }
+  if (lane == 0) s_wild[wave] = wild;
+
+  // A unit's loads go out before the one ahead of it is computed.
+  Next nb = next();
+  load(ub, nb);
+  if (na.any) for (;;) {
+    run(ua, na);
+    if (!nb.any) break;
+    na = next();
+    load(ua, na);
+    run(ub, nb);
+    nb = next();
+    load(ub, nb);
+    if (!na.any) break;
   }
 #pragma unroll
   for (int v = 0; v < NT; ++v) {
@@ -415,22 +466,22 @@ __global__ __launch_bounds__(kTW * 64) void tree_attn_kernel(TreeAttnArgs a) {
       s_ml[0][row] = M;
       s_ml[1][row] = S;
     }
-    if constexpr (PAGED) {
+    if constexpr (PAGED) {  // dims 32 g + 8 e + dt
 #pragma unroll
       for (int e = 0; e < 4; ++e)
 #pragma unroll
         for (int q = 0; q < 2; ++q)
           *reinterpret_cast<f32x4*>(&s_o[wave][row][32 * g + 8 * e + 4 * q]) =
               f32x4{acc[v][4 * q][e], acc[v][4 * q + 1][e], acc[v][4 * q + 2][e], acc[v][4 * q + 3][e]};
-    } else {
+    } else {  // dims 16 dt + 4 g + e
 #pragma unroll
       for (int dt = 0; dt < 8; ++dt) *reinterpret_cast<f32x4*>(&s_o[wave][row][16 * dt + 4 * g]) = acc[v][dt];
     }
   }
   __syncthreads();
 
-  const long long pbase = ((long long)rh * a.nsplit + split) * a.rows;
-  const int last = min(tlen * a.G, a.rows) - row0;  // rows of this group in the tree
+  const long long pbase = ((long long)t.rh * a.nsplit + t.split) * a.rows + t.row0;
+  const int last = min(t.tlen * a.G, a.rows) - t.row0;  // rows of this group in the tree
   for (int pos = threadIdx.x; pos < kRows * (kHeadDim / 4); pos += kTW * 64) {
     const int row = pos >> 5;
     const int c4 = pos & 31;
@@ -438,13 +489,302 @@ __global__ __launch_bounds__(kTW * 64) void tree_attn_kernel(TreeAttnArgs a) {
     f32x4 o = *reinterpret_cast<const f32x4*>(&s_o[0][row][c4 * 4]);
 #pragma unroll
     for (int w = 1; w < kTW; ++w) o += *reinterpret_cast<const f32x4*>(&s_o[w][row][c4 * 4]);
+    if (s_wild[0] | s_wild[1]) add_wild(a, t, s_anc[(t.row0 + row) / a.G], c4, o);
     if (a.nsplit == 1) {
-      write_row(a, r, h, row0 + row, c4, o, s_ml[0][row], s_ml[1][row]);
+      write_row(a, t.r, t.h, t.row0 + row, c4, o, s_ml[0][row], s_ml[1][row]);
     } else {
-      *reinterpret_cast<f32x4*>(a.part_o + (pbase + row0 + row) * kHeadDim + c4 * 4) = o;
-      if (c4 == 0)
-        *reinterpret_cast<float2*>(a.part_ml + (pbase + row0 + row) * 2) = make_float2(s_ml[0][row], s_ml[1][row]);
+      *reinterpret_cast<f32x4*>(a.part_o + (pbase + row) * kHeadDim + c4 * 4) = o;
+      if (c4 == 0) *reinterpret_cast<float2*>(a.part_ml + (pbase + row) * 2) = make_float2(s_ml[0][row], s_ml[1][row]);
     }
+  }
+}
+
+// 16 bytes a lane from global memory straight into LDS: lane L's bytes land at
+// lds_row + 16 L, lds_row being the same in every lane. In assembly for the reason
+// given at the working set's attention (lds_dma16): the compiler would drain every
+// earlier load before each one; the waits are the kernel's own counts instead.
+__device__ __forceinline__ void tree_dma16(const void* src, void* lds_row) {
+  const uint32_t lds =
+      __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)lds_row);
+  uint32_t saved;
+  asm volatile(
+      "s_mov_b32 %0, m0\n\t"
+      "s_mov_b32 m0, %2\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dwordx4 %1, off\n\t"
+      "s_mov_b32 m0, %0"
+      : "=&s"(saved)
+      : "v"(src), "s"(lds)
+      : "memory");
+}
+template <int N>
+__device__ __forceinline__ void tree_wait() {  // s_waitcnt vmcnt(N) alone
+  static_assert(N >= 0 && N < 64, "vmcnt range");
+  __builtin_amdgcn_s_waitcnt((N & 0xF) | ((N >> 4) << 14) | (0x7 << 4) | (0xF << 8));
+}
+
+// More than two row tiles. Eight waves: RT places for row tiles, NT tiles in each,
+// and TM teams of them (RT * TM = 8). A step is two units; with two teams each
+// takes one of them, with one both. A ring of kRingSteps steps in LDS is filled by
+// loads that go straight there, four a wave and step; one barrier a step
+// publishes it and frees the one before.
+//
+// The units of a split are listed first, the ones without an attended token left
+// out, up to kListUnits at a time. K is put into LDS in MFMA operand layout, and so
+// is the working set's V. Token-major V lies there row by row, 16-byte piece c of
+// row p at c ^ swizzle(p), and the transposing read takes 4 tokens x 16 dims a group
+// of 16 lanes: lane (g, i) names dims 4 (i % 4) .. +3 of token i / 4 and receives
+// dim i of the 4 tokens. The swizzle spreads the tokens that one read names over
+// different banks.
+constexpr int kRingSteps = 4;
+constexpr int kListUnits = 1024;
+constexpr int kListPad = 2 + 2 * kRingSteps;  // the tree's units, and none behind them
+constexpr int kRowsThreads = 512;
+
+__device__ __forceinline__ int v_swizzle(int token) { return ((token & 3) | (token >> 1 & 4)) << 1; }
+
+template <int RT, int TM, int NT, int BS, bool PAGED>
+__global__ __launch_bounds__(kRowsThreads) void tree_attn_rows_kernel(TreeAttnArgs a) {
+  static_assert(RT * TM == 8 && (TM == 1 || TM == 2), "eight waves");
+  constexpr int kLook = kRingSteps - 1;
+  __shared__ __align__(16) u32x4 s_ring[kRingSteps][2][16][64];
+  __shared__ __align__(16) int4 s_list[kListUnits + kListPad];  // places, attended tokens of a unit's blocks (see below)
+  __shared__ uint64_t s_anc[kTreeMaxTokens];
+  __shared__ int s_wave[8], s_wild;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63;
+  const int g = lane >> 4;
+  const int i = lane & 15;
+  const int team = TM == 1 ? 0 : wave / RT;
+  const int rt = TM == 1 ? wave : wave % RT;
+  TreeItem t;
+  if (!tree_setup<BS, PAGED>(a, a.tiles * 16, t)) return;
+  int L, u_begin, u_end;
+  const Ctx c = tree_units<BS, PAGED>(a, t, L, u_begin, u_end);
+  const bool last_split = t.split == a.nsplit - 1;
+
+  // tile v of this wave is rt + v * RT of the group
+  const int nv = rt >= a.tiles ? 0 : (a.tiles - rt + RT - 1) / RT;
+  bf16x8 qb[NT][4];
+#pragma unroll
+  for (int v = 0; v < NT; ++v) load_q(a, t, t.row0 + (rt + v * RT) * 16, g, i, qb[v]);
+  if (wave == 0) {
+    if (last_split) s_anc[lane] = ancestors(a.parent ? a.parent + (long long)t.r * a.T : nullptr, a.T, t.tlen, lane);
+    if (lane == 0) s_wild = 0;
+  }
+  float m_run[NT], l_run[NT];
+  f32x4 acc[NT][8];
+#pragma unroll
+  for (int v = 0; v < NT; ++v) {
+    m_run[v] = -INFINITY;
+    l_run[v] = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < 8; ++dt) acc[v][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  // What this wave loads: of unit `half` of a step, four pieces of K (token tile
+  // j0 / 4, its four k-steps) or of V. A lane's element offset within the unit's block
+  // lo or hi, piece jj being jj * step further, xor-ed from the third on.
+  const int half = wave >> 2;
+  const bool load_v = wave & 2;
+  const int j0 = (wave & 1) * 4;
+  const int k_row = 8 * (i >> 2) + (i & 3) + j0;  // K: this lane's token of the unit
+  const int v_row = 4 * j0 + g;                   // token-major V: of the first piece
+  int off;
+  bool hi;
+  if (!load_v) {
+    off = (BS == 16 ? k_row & 15 : k_row) * kHeadDim + g * 8;
+    hi = BS == 16 && k_row >= 16;
+  } else if (PAGED) {
+    off = (BS == 16 ? v_row & 15 : v_row) * kHeadDim + (i ^ v_swizzle(v_row)) * 8;
+    hi = BS == 16 && v_row >= 16;
+  } else {
+    off = (j0 * 16 + i) * BS + (BS == 16 ? g & 1 : g) * 8;
+    hi = BS == 16 && g >= 2;
+  }
+  const int step = !load_v ? 32 : (PAGED ? 4 * kHeadDim : 16 * BS);
+  const int flip = load_v && PAGED ? 64 : 0;  // rows 8 apart: the swizzle's highest bit
+  const uint16_t* src0 = load_v ? t.vb : t.kb;
+  const int tree_units_n = last_split ? (t.tlen + 31) / 32 : 0;
+
+  for (int seg = u_begin; seg == u_begin || seg < u_end; seg += kListUnits) {
+    // ---- list this segment's units ----
+    const int n_seg = min(kListUnits, u_end - seg);
+    const bool final_seg = seg + kListUnits >= u_end;
+    int total = 0;
+    for (int b0 = 0; b0 < n_seg; b0 += kRowsThreads) {
+      const int n = b0 + (int)threadIdx.x;
+      int4 e = make_int4(0, 0, 0, 0);
+      if (n < n_seg) {
+        const int b = (seg + n) * (32 / BS);
+        block_entry<BS, PAGED>(a, c, L, b, block_raw<BS, PAGED>(a, t, c, b), e.x, e.z);
+        if (BS == 16) block_entry<BS, PAGED>(a, c, L, b + 1, block_raw<BS, PAGED>(a, t, c, b + 1), e.y, e.w);
+        if (e.w < 0) e.w = 0;  // a block past the context
+      }
+      const bool live = e.z > 0 || e.w > 0;
+      const uint64_t bal = __builtin_amdgcn_ballot_w64(live);
+      if (lane == 0) s_wave[wave] = __popcll(bal);
+      __syncthreads();
+      int at = total, all = 0;
+      for (int w = 0; w < 8; ++w) {
+        const int k = s_wave[w];
+        at += w < wave ? k : 0;
+        all += k;
+      }
+      if (live) s_list[at + __popcll(bal & ((1ull << lane) - 1))] = e;
+      total += all;
+      __syncthreads();
+    }
+    // behind them the tree's units (x: which, z: -1) and the places of none (z: -2)
+    const int units = total + (final_seg ? tree_units_n : 0);
+    const int steps = (units + 1) / 2;
+    if (threadIdx.x < kListPad) {
+      const int n = total + (int)threadIdx.x;
+      s_list[n] = n < units ? make_int4((int)threadIdx.x, 0, -1, 0) : make_int4(0, 0, -2, 0);
+    }
+    __syncthreads();
+    auto entry = [&](int n) __attribute__((always_inline)) {
+      const int4 e = s_list[n];
+      return make_int4(__builtin_amdgcn_readfirstlane(e.x), __builtin_amdgcn_readfirstlane(e.y),
+                       __builtin_amdgcn_readfirstlane(e.z), __builtin_amdgcn_readfirstlane(e.w));
+    };
+    auto issue = [&](int s) __attribute__((always_inline)) {
+      const int4 e = entry(s * 2 + half);
+      u32x4* dst = &s_ring[s % kRingSteps][half][(load_v ? 8 : 0) + j0][0];
+      int o = off;
+      asm volatile("" : "+v"(o));  // the sums below are not worth a register each from step to step
+      if (e.z != -1) {
+        const uint16_t* src = src0 + (long long)(hi ? e.y : e.x) * t.unit_elems;
+#pragma unroll
+        for (int jj = 0; jj < 4; ++jj) tree_dma16(src + ((o + jj * step) ^ (jj >= 2 ? flip : 0)), dst + jj * 64);
+      } else {  // the tree's rows
+        const uint16_t* src = (load_v ? a.tree_v : a.tree_k) + t.tree_base;
+#pragma unroll
+        for (int jj = 0; jj < 4; ++jj) {
+          const int row = load_v ? 4 * (j0 + jj) + g : k_row;
+          const int col = load_v ? (i ^ v_swizzle(row)) * 8 : jj * 32 + g * 8;
+          tree_dma16(src + min(e.x * 32 + row, t.tlen - 1) * t.tree_row + col, dst + jj * 64);
+        }
+      }
+    };
+    for (int s = 0; s < kLook; ++s) issue(s);
+
+    for (int s = 0; s < steps; ++s) {
+      // this wave's loads of step s are in; the barrier publishes every wave's and
+      // tells that the step before is no longer read, whose place takes step s + kLook
+      tree_wait<4 * (kLook - 1)>();
+      __syncthreads();
+      issue(s + kLook);
+#pragma unroll 1
+      for (int half_u = TM == 1 ? 0 : team; half_u < (TM == 1 ? 2 : team + 1); ++half_u) {
+        const int4 e = entry(s * 2 + half_u);
+        if (e.z == -2 || nv == 0) continue;
+        const u32x4(&buf)[16][64] = s_ring[s % kRingSteps][half_u];
+        const bool tree = e.z == -1;
+        TreeUnit u;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) u.k[j >> 2][j & 3] = buf[j][lane];
+        if (PAGED || tree) {
+          char* rows = reinterpret_cast<char*>(&s_ring[s % kRingSteps][half_u][8][0]);
+          typedef short s16x4 __attribute__((ext_vector_type(4)));
+          typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+          const int token = 8 * g + (i >> 2);  // and 4 further, with the same swizzle
+#pragma unroll
+          for (int dt = 0; dt < 8; ++dt) {
+            char* at = rows + token * 256 + ((2 * dt + (i >> 1 & 1)) ^ v_swizzle(token)) * 16 + (i & 1) * 8;
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+              const u32x2 w = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                                            (__attribute__((address_space(3))) s16x4*)(at + q * 1024)));
+              u.v[dt][2 * q] = w[0];
+              u.v[dt][2 * q + 1] = w[1];
+            }
+          }
+        } else {
+#pragma unroll
+          for (int dt = 0; dt < 8; ++dt) u.v[dt] = buf[8 + dt][lane];
+        }
+        const int n = tree ? t.tlen - e.x * 32 - 8 * g
+                           : (BS == 16 ? (g < 2 ? e.z : e.w) - (g & 1) * 8 : e.z - g * 8);
+        const int keep = n < 0 ? 0 : (n > 8 ? 8 : n);
+        const bool partial = __builtin_amdgcn_ballot_w64(keep < 8) != 0;
+        if (partial) clear_tokens(u.v, keep);  // 0 times what an unused place holds must stay 0
+        if (tree && take_wild(u.v)) s_wild = 1;
+#pragma unroll
+        for (int v = 0; v < NT; ++v) {
+          if (v > 0 && v >= nv) break;
+          float x[8];
+          unit_scores(u.k, qb[v], a.scale_log2, x);
+          if (tree || partial) {
+            uint32_t bits = (1u << keep) - 1;
+            if (tree) {
+              const int row = t.row0 + (rt + v * RT) * 16 + i;
+              bits = (uint32_t)(s_anc[row < a.rows ? row / a.G : 0] >> (e.x * 32 + 8 * g));
+            }
+#pragma unroll
+            for (int f = 0; f < 8; ++f) x[f] = bits >> f & 1 ? x[f] : -INFINITY;
+          }
+          unit_pv(u.v, unit_softmax(x, m_run[v], l_run[v], acc[v]), acc[v]);
+        }
+      }
+    }
+    tree_wait<0>();   // the loads past the last step land before the ring and the list are reused
+    __syncthreads();
+  }
+
+#pragma unroll
+  for (int v = 0; v < NT; ++v) {
+    l_run[v] += __shfl_xor(l_run[v], 16);
+    l_run[v] += __shfl_xor(l_run[v], 32);
+    if (l_run[v] != l_run[v] && m_run[v] == -INFINITY) m_run[v] = 0.f;  // a NaN sum is not an empty one
+  }
+  const int end = min(t.tlen * a.G, a.rows);  // rows in the tree
+  const long long pbase = ((long long)t.rh * a.nsplit + t.split) * a.rows;
+  // d-tiles d0 .. d0 + 4 * n of a row: its output, or its partial
+  auto put = [&](int row, const f32x4* o, int d0, int n, float M, float S) __attribute__((always_inline)) {
+    if (row >= end) return;
+#pragma unroll
+    for (int dt = 0; dt < n; ++dt) {
+      const int c4 = (d0 + dt) * 4 + g;
+      f32x4 x = o[dt];
+      if (s_wild) add_wild(a, t, s_anc[row / a.G], c4, x);
+      if (a.nsplit == 1) write_row(a, t.r, t.h, row, c4, x, M, S);
+      else *reinterpret_cast<f32x4*>(a.part_o + (pbase + row) * kHeadDim + c4 * 4) = x;
+    }
+    if (a.nsplit > 1 && g == 0 && d0 == 0)
+      *reinterpret_cast<float2*>(a.part_ml + (pbase + row) * 2) = make_float2(M, S);
+  };
+  if constexpr (TM == 1) {
+#pragma unroll
+    for (int v = 0; v < NT; ++v)
+      if (v < nv) put(t.row0 + (rt + v * RT) * 16 + i, acc[v], 0, 8, m_run[v], l_run[v]);
+  } else {
+    // the teams exchange halves of the dims through LDS: team 0 finishes d-tiles 0-3, team 1 4-7
+    static_assert(NT == 1, "one tile a wave with two teams");
+    constexpr int kHalf = kHeadDim / 2 + 4;
+    float(*s_o)[16][kHalf] = reinterpret_cast<float(*)[16][kHalf]>(&s_ring[0][0][0][0]);  // [wave]
+    float(*s_ml)[2][16] = reinterpret_cast<float(*)[2][16]>(&s_list[0]);                 // [wave]
+    f32x4 mine[4];
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt) {
+      mine[dt] = team == 0 ? acc[0][dt] : acc[0][dt + 4];
+      *reinterpret_cast<f32x4*>(&s_o[wave][i][dt * 16 + 4 * g]) = team == 0 ? acc[0][dt + 4] : acc[0][dt];
+    }
+    if (g == 0) {
+      s_ml[wave][0][i] = m_run[0];
+      s_ml[wave][1][i] = l_run[0];
+    }
+    __syncthreads();
+    const int other = wave < RT ? wave + RT : wave - RT;
+    const float mo = s_ml[other][0][i], lo = s_ml[other][1][i];
+    const float M = fmaxf(m_run[0], mo);
+    const float f = m_run[0] == -INFINITY ? 0.f : fast_exp2(m_run[0] - M);
+    const float fo = mo == -INFINITY ? 0.f : fast_exp2(mo - M);
+    const float S = l_run[0] * f + lo * fo;
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+      mine[dt] = mine[dt] * f + *reinterpret_cast<const f32x4*>(&s_o[other][i][dt * 16 + 4 * g]) * fo;
+    if (nv) put(t.row0 + rt * 16 + i, mine, team * 4, 4, M, S);
   }
 }
 
@@ -494,20 +834,20 @@ __global__ __launch_bounds__(kTreeMergeRows * 32) void tree_merge_kernel(TreeAtt
   write_row(a, r, rh - r * a.Hkv, row, c4, o, M, S);
 }
 
-template <int NT, int BS, bool PAGED>
-void launch_nt(const TreeAttnArgs& a, hipStream_t s) {
-  const long long items = (long long)a.R * a.Hkv * a.nsplit * a.groups;
-  hipLaunchKernelGGL((tree_attn_kernel<NT, BS, PAGED>), dim3((unsigned)((items + 7) / 8 * 8)), dim3(kTW * 64), 0, s, a);
-}
-
 template <int BS, bool PAGED>
 void launch_bs(const TreeAttnArgs& a, hipStream_t s) {
-  switch (a.tiles) {
-    case 1: return launch_nt<1, BS, PAGED>(a, s);
-    case 2: return launch_nt<2, BS, PAGED>(a, s);
-    case 3: return launch_nt<3, BS, PAGED>(a, s);
-    default: return launch_nt<4, BS, PAGED>(a, s);
-  }
+  const long long items = (long long)a.R * a.Hkv * a.nsplit * a.groups;
+  const dim3 grid((unsigned)((items + 7) / 8 * 8));
+  if (a.tiles == 1)
+    hipLaunchKernelGGL((tree_attn_kernel<1, BS, PAGED>), grid, dim3(kTW * 64), 0, s, a);
+  else if (a.tiles == 2)
+    hipLaunchKernelGGL((tree_attn_kernel<2, BS, PAGED>), grid, dim3(kTW * 64), 0, s, a);
+  else if (a.tiles <= 4)
+    hipLaunchKernelGGL((tree_attn_rows_kernel<4, 2, 1, BS, PAGED>), grid, dim3(kRowsThreads), 0, s, a);
+  else if (a.tiles <= 8)
+    hipLaunchKernelGGL((tree_attn_rows_kernel<8, 1, 1, BS, PAGED>), grid, dim3(kRowsThreads), 0, s, a);
+  else
+    hipLaunchKernelGGL((tree_attn_rows_kernel<8, 1, 2, BS, PAGED>), grid, dim3(kRowsThreads), 0, s, a);
 }
 
 }  // namespace

@@ -11,8 +11,8 @@
 
 namespace oasis {
 
-constexpr int kTreeWaves = 4;     // waves per workgroup
-constexpr int kTreeTiles = 4;     // 16-row tiles per workgroup at most
+constexpr int kTreeWaves = 4;     // waves per workgroup of the form for up to two row tiles
+constexpr int kTreeTiles = 16;    // 16-row tiles per workgroup at most
 constexpr int kTreeMaxTokens = 64;  // a row's ancestors are one 64-bit mask
 constexpr int kTreeMaxRows = 4096;  // G * T
 constexpr int kTreeMaxSplits = 256;
@@ -33,7 +33,12 @@ inline TreePlan tree_plan(long long pairs, int G, int T, int units) {
   p.tiles = (tiles + p.groups - 1) / p.groups;
   p.units = units;
   const long long items = pairs * p.groups;
-  long long want = items > 0 ? (512 + items - 1) / items : 1;
+  // one workgroup per CU, and up to four where each still has 64 units
+  long long want = items > 0 ? 256 / items : 1;
+  if (want < 1) want = 1;
+  long long more = items > 0 ? 1024 / items : 1;
+  if (more > units / 64) more = units / 64;
+  if (want < more) want = more;
   const long long most = (units + 2 * kTreeWaves - 1) / (2 * kTreeWaves);  // two units a wave at least
   if (want > most) want = most;
   if (want > kTreeMaxSplits) want = kTreeMaxSplits;
