@@ -185,7 +185,7 @@ oasis_status oasis_sparse_tree_attn(const oasis_dims* dims, const uint16_t* q, i
 
 size_t oasis_verify_workspace_bytes(int32_t num_reqs, int32_t num_q_tokens, int32_t vocab) {
   if (num_reqs < 1 || num_q_tokens < 1 || vocab < 1) return 0;
-  return oasis::verify_ws_bytes(num_reqs, vocab);
+  return oasis::verify_ws_bytes(num_reqs);
 }
 
 oasis_status oasis_verify_drafts(int32_t num_reqs, int32_t num_q_tokens, int32_t vocab, const float* target_probs,
@@ -211,13 +211,29 @@ oasis_status oasis_verify_drafts(int32_t num_reqs, int32_t num_q_tokens, int32_t
   REQUIRE_PTR(path, fn);
   REQUIRE_PTR(path_len, fn);
   REQUIRE_PTR(out_tokens, fn);
-  const size_t bytes = oasis::verify_ws_bytes(num_reqs, vocab);
+  const size_t bytes = oasis::verify_ws_bytes(num_reqs);
   if (!workspace || workspace_bytes < bytes)
     return fail(OASIS_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", fn, workspace_bytes, bytes);
   if ((uintptr_t)workspace & 15) return fail(OASIS_ERR_INVALID_ARG, "%s: workspace is not 16-byte aligned", fn);
-  const oasis::VerifyArgs a{target_probs, draft_probs, target_stride, draft_stride, tokens, parent, tree_len, accept_u,
-                            sample_u, path, path_len, out_tokens, static_cast<double*>(workspace), num_reqs,
-                            num_q_tokens, vocab, oasis::verify_chunks(vocab)};
+  oasis::VerifyArgs a{};
+  a.target = target_probs;
+  a.draft = draft_probs;
+  a.target_stride = target_stride;
+  a.draft_stride = draft_stride;
+  a.tokens = tokens;
+  a.parent = parent;
+  a.tree_len = tree_len;
+  a.accept_u = accept_u;
+  a.sample_u = sample_u;
+  a.path = path;
+  a.path_len = path_len;
+  a.out_tokens = out_tokens;
+  a.R = num_reqs;
+  a.T = num_q_tokens;
+  a.V = vocab;
+  a.groups = oasis::verify_groups(num_reqs, vocab, draft_probs != nullptr);
+  a.part = static_cast<double*>(workspace);
+  a.state = reinterpret_cast<oasis::VerifyState*>(a.part + (size_t)num_reqs * oasis::kVerifyBlocks);
   return hip_status(oasis::launch_verify(a, static_cast<hipStream_t>(stream)), fn);
 }
 

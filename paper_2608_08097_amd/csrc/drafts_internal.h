@@ -40,20 +40,31 @@ struct VerifyArgs {
   int32_t* path;             // [R][T]
   int32_t* path_len;         // [R]
   int32_t* out_tokens;       // [R][T]
-  double* part;              // [R][chunks] masses, then the walks' states
-  int R, T, V, chunks;
+  double* part;              // [R][kVerifyBlocks] masses
+  struct VerifyState* state; // [R]
+  int R, T, V, groups;       // workgroups per request
 };
-constexpr int kVerifyChunk = 4096;  // vocabulary entries per workgroup
-// where a request's walk ended: node, rows on the path, rejected siblings, coefficient
+// Where a request's walk ended: coefficient, rejected siblings, node, rows on the path.
 struct VerifyState {
   double coef;
   unsigned long long rejected;
   int node, len;
 };
-inline int verify_chunks(int V) { return (V + kVerifyChunk - 1) / kVerifyChunk; }
-inline size_t verify_ws_bytes(long long R, int V) {
-  return (size_t)R * (verify_chunks(V) * sizeof(double) + sizeof(VerifyState));
+constexpr int kVerifyBlocks = 256;  // blocks of a row at most
+constexpr int kVerifyGroups = 16;   // workgroups per request at most
+// Workgroups per request: one (a single launch), or as many as the CUs allow with
+// 32 KB of the last row, or rows, for each, where that is 128 KB and more. Measured
+// at 64 requests: 64 KB a request 8.0 us with one and 8.3 with two, 256 KB 11.3 and
+// with four 10.8, 1 MB 24.5 and 17.9.
+inline int verify_groups(long long R, long long V, bool draft) {
+  const long long bytes = V * (draft ? 8 : 4);
+  int g = 1;
+  if (bytes >= 128 << 10)
+    while (2 * g <= kVerifyGroups && R * 2 * g <= 256 && bytes / (2 * g) >= 32 << 10) g *= 2;
+  return g;
 }
+// (the same at every size: a caller may use one workspace for calls with and without draft probabilities)
+inline size_t verify_ws_bytes(long long R) { return (size_t)R * (kVerifyBlocks * sizeof(double) + sizeof(VerifyState)); }
 hipError_t launch_verify(const VerifyArgs& a, hipStream_t s);
 
 struct AppendArgs {
