@@ -48,11 +48,11 @@ oasis_status check_slots(const oasis_dims* d, int32_t k_slots, const char* fn) {
 
 TreePlan paged_plan(const oasis_dims* d, int32_t T) {
   return tree_plan((long long)d->num_reqs * d->num_kv_heads, d->num_q_heads / d->num_kv_heads, T,
-                   (int)(((long long)d->max_blocks * d->block_size + 31) / 32));
+                   (int)(((long long)d->max_blocks * d->block_size + 31) / 32), true);
 }
 TreePlan sparse_plan(const oasis_dims* d, int32_t T, int32_t k_slots) {
   return tree_plan((long long)d->num_reqs * d->num_kv_heads, d->num_q_heads / d->num_kv_heads, T,
-                   (int)((((long long)k_slots + 1) * d->block_size + 31) / 32));
+                   (int)((((long long)k_slots + 1) * d->block_size + 31) / 32), false);
 }
 
 struct TreeCall {
@@ -97,7 +97,9 @@ oasis_status make_tree_args(const TreeCall& c, const TreePlan& p, TreeAttnArgs* 
   t.T = c.T;
   t.B = c.dims->block_size;
   t.NBmax = c.dims->max_blocks;
-  t.scale_log2 = c.scale * 1.4426950408889634f;
+  t.scale_log2 = c.scale == 0.f ? 1.f : std::fabs(c.scale) * 1.4426950408889634f;
+  t.q_and = c.scale == 0.f ? 0u : ~0u;
+  t.q_xor = c.scale < 0.f ? 0x80008000u : 0u;
   t.rows = p.rows;
   t.tiles = p.tiles;
   t.groups = p.groups;

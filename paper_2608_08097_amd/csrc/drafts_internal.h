@@ -23,7 +23,8 @@ struct TreeAttnArgs {
   float* part_ml;            // [R*Hkv][nsplit][rows][2]
   long long num_pages;
   int R, Hq, Hkv, G, T, B, NBmax, k_slots;
-  float scale_log2;
+  float scale_log2;          // |scale| * log2(e), 1 for a scale of 0
+  uint32_t q_and, q_xor;     // what makes up for that in the queries' bits
   int rows, tiles, groups, nsplit;
 };
 hipError_t launch_tree_attn(const TreeAttnArgs& a, bool paged, hipStream_t s);

@@ -31,7 +31,6 @@ namespace oasis {
 namespace {
 
 constexpr int kTW = kTreeWaves;
-constexpr float kTreeLazy = 8.f;  // as kLazyTh of the working set's attention: exponents stay below 2^8
 
 // Contiguous runs of the items on each XCD (workgroup ids go round the 8 XCDs): a
 // pair's splits and row groups share one L2.
@@ -75,58 +74,78 @@ __device__ __forceinline__ void clear_tokens(u32x4 (&v)[8], int keep) {
 // attend them when those are written (add_wild).
 __device__ __forceinline__ bool wild_bf16(uint32_t b) { return (b & 0x7F80u) == 0x7F80u; }
 __device__ __forceinline__ bool take_wild(u32x4 (&v)[8]) {
-  uint32_t any = 0;
+  uint32_t any = 0;  // an exponent of ones carries into the sign's place
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+#pragma unroll
+    for (int p = 0; p < 4; ++p) any |= (v[j][p] & 0x7F807F80u) + 0x00800080u;
+  if (!__builtin_amdgcn_ballot_w64((any & 0x80008000u) != 0)) return false;
 #pragma unroll
   for (int j = 0; j < 8; ++j)
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
-      // an exponent of ones carries into the sign's place
-      const uint32_t m = ((v[j][p] & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
-      any |= m;
-      v[j][p] &= ~((m >> 15) * 0xFFFFu);
+      uint32_t x = v[j][p];
+      asm volatile("" : "+v"(x));  // one at a time: the test's terms are not kept for this
+      v[j][p] = x & ~(((((x & 0x7F807F80u) + 0x00800080u) & 0x80008000u) >> 15) * 0xFFFFu);
     }
-  return __builtin_amdgcn_ballot_w64(any != 0) != 0;
+  return true;
 }
 
-// Scores of one unit for one tile: lane (g, n) gets row n against tokens 8g .. 8g+7.
-__device__ __forceinline__ void unit_scores(const u32x4 (&k)[2][4], const bf16x8 (&qb)[4], float scale_log2,
-                                            float (&x)[8]) {
-  f32x4 sc[2];
+// Scores of one unit for one tile, before the scale: lane (g, n) gets row n against
+// tokens 8g .. 8g+7.
+__device__ __forceinline__ void unit_scores(const u32x4 (&k)[2][4], const bf16x8 (&qb)[4], f32x4 (&sc)[2]) {
   sc[0] = sc[1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int st = 0; st < 4; ++st)
 #pragma unroll
     for (int tau = 0; tau < 2; ++tau)
       sc[tau] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(k[tau][st]), qb[st], sc[tau], 0, 0, 0);
+}
+__device__ __forceinline__ void mask_scores(f32x4 (&sc)[2], uint32_t bits) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) x[e] = sc[e >> 2][e & 3] * scale_log2;
+  for (int e = 0; e < 8; ++e) sc[e >> 2][e & 3] = bits >> e & 1 ? sc[e >> 2][e & 3] : -INFINITY;
 }
 
-// Online softmax of one tile's scores: probabilities in bf16 (the second
-// product's operand; 2^-8 of each at most, unbiased, and the sum takes them
-// unrounded), the row reference and the lane's partial sum updated. The
-// accumulators are rescaled only when a score passes its row's reference by 2^8.
-__device__ __forceinline__ bf16x8 unit_softmax(const float (&x)[8], float& m_ref, float& l_part, f32x4 (&acc)[8]) {
-  const float lmax = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-  if (__builtin_amdgcn_ballot_w64(lmax > m_ref + kTreeLazy)) {
-    float rmax = fmaxf(lmax, __shfl_xor(lmax, 16));
-    rmax = fmaxf(rmax, __shfl_xor(rmax, 32));
-    const float m_new = fmaxf(m_ref, rmax);
-    const float alpha = m_new == -INFINITY ? 1.f : fast_exp2(m_ref - m_new);
+// Online softmax of one tile's scores (scale > 0: load_q): probabilities in bf16
+// (the second product's operand; 2^-8 of each at most, unbiased, and the sum takes
+// them unrounded), the row's reference (negated: +inf before its first token) and
+// the lane's partial sum updated. A probability is 2^(score - reference), and the
+// reference follows the row's maximum only when a lane's eight probabilities pass
+// kTreeTop together: that needs no maximum of every unit's scores, and values far
+// above the reference show as large, infinite or NaN sums. The accumulators are
+// rescaled then, in a branch that is rare after a wave's first unit.
+constexpr float kTreeTop = 256.f;
+
+__device__ __forceinline__ float unit_exp(const f32x4 (&s)[2], float scale, float m_neg, float (&p)[8]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) p[e] = fast_exp2(__builtin_fmaf(s[e >> 2][e & 3], scale, m_neg));
+  return ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+}
+
+__device__ __forceinline__ bf16x8 unit_softmax(const f32x4 (&s)[2], float scale, float& m_neg, float& l_part,
+                                               f32x4 (&acc)[8]) {
+  float p[8];
+  float psum = unit_exp(s, scale, m_neg, p);
+  const uint64_t past = __builtin_amdgcn_ballot_w64(!(psum <= kTreeTop));
+  if (__builtin_expect(past != 0, 0)) {
+    // the rows that passed it in one of their four lanes; the others stay as they are
+    const uint64_t rows = past | past >> 16 | past >> 32 | past >> 48;
+    const bool mine = rows >> (threadIdx.x & 15) & 1;
+    const float lmax = scale * fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
+                                     fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
+    float m = fmaxf(lmax, __shfl_xor(lmax, 16));
+    m = fmaxf(fmaxf(m, __shfl_xor(m, 32)), -m_neg);
+    m = mine ? m : -m_neg;
+    const float alpha = m == -INFINITY ? 1.f : fast_exp2(-m_neg - m);
     l_part *= alpha;
 #pragma unroll
     for (int dt = 0; dt < 8; ++dt) acc[dt] *= alpha;
-    m_ref = m_new;
+    m_neg = -m;
+    psum = unit_exp(s, scale, m == -INFINITY ? 0.f : m_neg, p);
   }
-  const float m_use = m_ref == -INFINITY ? 0.f : m_ref;
   bf16x8 pb;
-  float psum = 0.f;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const float pe = fast_exp2(x[e] - m_use);
-    psum += pe;
-    pb[e] = (__bf16)pe;
-  }
+  for (int e = 0; e < 8; ++e) pb[e] = (__bf16)p[e];
   l_part += psum;
   return pb;
 }
@@ -137,16 +156,25 @@ __device__ __forceinline__ void unit_pv(const u32x4 (&v)[8], bf16x8 pb, f32x4 (&
     acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(v[dt]), pb, acc[dt], 0, 0, 0);
 }
 
-// Ancestor masks of a request's tree, lane t: row t's (its own bit among them).
-// Pointer doubling: after n rounds a mask holds 2^n rows of the path. A parent
-// outside [0, t) makes the row a root; lanes past the tree hold 0.
-__device__ __forceinline__ uint64_t ancestors(const int32_t* parent, int T, int len, int lane) {
-  int up = -1;
-  if (lane < len && lane > 0) up = parent ? parent[lane] : lane - 1;
-  if (up >= lane || up < 0) up = -1;
+// A row's maximum and, in l, its sum, from its four lanes' parts.
+__device__ __forceinline__ float finish_row(float m_neg, float& l) {
+  l += __shfl_xor(l, 16);
+  l += __shfl_xor(l, 32);
+  return l != l && m_neg == INFINITY ? 0.f : -m_neg;  // a NaN sum is not an empty one
+}
+
+// A lane's parent in a request's tree, -1 for a root: row t's in lane t.
+__device__ __forceinline__ int tree_parent(const TreeAttnArgs& a, int r, int len, int lane) {
+  if (lane < 1 || lane >= len) return -1;
+  const int up = a.parent ? a.parent[(long long)r * a.T + lane] : lane - 1;
+  return up >= 0 && up < lane ? up : -1;
+}
+// Ancestor masks, lane t: row t's (its own bit among them); lanes past the tree hold
+// 0. Pointer doubling: after n rounds a mask holds 2^n rows of the path, so it ends
+// by the sixth.
+__device__ __forceinline__ uint64_t ancestors(int up, int len, int lane) {
   uint64_t m = lane < len ? 1ull << lane : 0;
-#pragma unroll
-  for (int n = 0; n < 6; ++n) {
+  while (__builtin_amdgcn_ballot_w64(up >= 0)) {
     const int src = up < 0 ? lane : up;
     const uint32_t lo = __shfl((uint32_t)m, src), hi = __shfl((uint32_t)(m >> 32), src);
     const int next = __shfl(up, src);
@@ -181,7 +209,7 @@ __device__ __forceinline__ int tree_length(const TreeAttnArgs& a, int r) {
 
 // What a workgroup works on.
 struct TreeItem {
-  int r, h, rh, split, row0, tlen;
+  int r, h, rh, split, row0, tlen, ctx;
   long long unit_elems;   // of a page or a slot
   const uint16_t *kb, *vb;  // this head's part of the pages, or of the request's slots
   const int32_t* tab;     // the request's block table, or the pair's slot map
@@ -204,6 +232,7 @@ __device__ __forceinline__ bool tree_setup(const TreeAttnArgs& a, int group_rows
   t.tab = a.table + (PAGED ? (long long)t.r * a.NBmax : (long long)t.rh * a.k_slots);
   t.tree_row = (long long)a.Hkv * kHeadDim;
   t.tree_base = (long long)t.r * a.T * t.tree_row + (long long)t.h * kHeadDim;
+  t.ctx = a.ctx_len[t.r];  // read beside the tree's length
   t.tlen = tree_length(a, t.r);
   return t.row0 < t.tlen * a.G;  // else no row of this group is in the tree
 }
@@ -211,7 +240,7 @@ __device__ __forceinline__ bool tree_setup(const TreeAttnArgs& a, int group_rows
 // The cached tokens of request r and the units [begin, end) of a split of them.
 template <int BS, bool PAGED>
 __device__ __forceinline__ Ctx tree_units(const TreeAttnArgs& a, const TreeItem& t, int& L, int& begin, int& end) {
-  const Ctx c = ctx_blocks(a.ctx_len[t.r], BS, a.NBmax);
+  const Ctx c = ctx_blocks(t.ctx, BS, a.NBmax);
   L = c.nb ? c.n_cand * BS + c.local_len : 0;
   const int nu = PAGED ? (L + 31) / 32 : (BS == 16 ? (a.k_slots + 2) / 2 : a.k_slots + 1);
   begin = (int)((long long)nu * t.split / a.nsplit);
@@ -241,6 +270,8 @@ __device__ __forceinline__ void block_entry(const TreeAttnArgs& a, const Ctx& c,
 }
 
 // Q^T operand of the tile whose first row is `first`: lane (g, i) holds row first + i.
+// A negative scale's sign is taken into the queries, and so is a scale of 0 (q_and,
+// q_xor), so that the scale that the scores meet is positive.
 __device__ __forceinline__ void load_q(const TreeAttnArgs& a, const TreeItem& t, int first, int g, int i, bf16x8 (&qb)[4]) {
   const int row = first + i;
   const int tq = row < a.rows ? row / a.G : 0;
@@ -249,7 +280,10 @@ __device__ __forceinline__ void load_q(const TreeAttnArgs& a, const TreeItem& t,
 #pragma unroll
   for (int st = 0; st < 4; ++st) {
     const u32x4 x = ldg16(qrow + st * 32 + g * 8);
-    qb[st] = as_bf16x8(row < a.rows ? x : u32x4{0, 0, 0, 0});
+    u32x4 y;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) y[w] = row < a.rows ? (x[w] & a.q_and) ^ a.q_xor : 0u;
+    qb[st] = as_bf16x8(y);
   }
 }
 
@@ -266,7 +300,7 @@ __device__ __forceinline__ void add_wild(const TreeAttnArgs& a, const TreeItem& 
   }
 }
 
-template <int NT, int BS, bool PAGED>
+template <int NT, int BS, bool PAGED, bool STREAM>
 __global__ __launch_bounds__(kTW * 64) void tree_attn_kernel(TreeAttnArgs a) {
   static_assert(NT <= 2, "three or more row tiles take tree_attn_rows_kernel");
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -320,48 +354,33 @@ __global__ __launch_bounds__(kTW * 64) void tree_attn_kernel(TreeAttnArgs a) {
                             : (uint32_t)(i * BS + (BS == 16 ? g & 1 : g) * 8);
   // Loads are issued for a wave without a next unit too, every lane on the first
   // bytes of place 0: the same number on every path keeps the compiler's wait
-  // counts exact, so that waiting for one unit never drains the one behind it.
-  auto load = [&](TreeUnit& u, const Next& n) __attribute__((always_inline)) {
+  // counts exact, so that waiting for one half of a unit never drains what is behind it.
+  TreeUnit u;
+  auto load_k = [&](const Next& n) __attribute__((always_inline)) {
     const uint16_t* ku = t.kb + (long long)(BS == 16 && i >= 8 ? n.p1 : n.p0) * t.unit_elems + (n.any ? ko : 0u);
-    const uint16_t* vu = t.vb + (long long)(BS == 16 && g >= 2 ? n.p1 : n.p0) * t.unit_elems + (n.any ? vo : 0u);
 #pragma unroll
     for (int tau = 0; tau < 2; ++tau)
 #pragma unroll
       for (int st = 0; st < 4; ++st) u.k[tau][st] = ldg16(ku + tau * 4 * kHeadDim + st * 32);
+  };
+  auto load_v = [&](const Next& n) __attribute__((always_inline)) {
+    const uint16_t* vu = t.vb + (long long)(BS == 16 && g >= 2 ? n.p1 : n.p0) * t.unit_elems + (n.any ? vo : 0u);
 #pragma unroll
-    for (int dt = 0; dt < 8; ++dt) u.v[dt] = ldg16(vu + (PAGED ? dt * kHeadDim : dt * 16 * BS));
+    for (int dt = 0; dt < 8; ++dt) u.v[dt] = ldg16_once<STREAM>(vu + (PAGED ? dt * kHeadDim : dt * 16 * BS));
   };
 
   bf16x8 qb[NT][4];
 #pragma unroll
   for (int v = 0; v < NT; ++v) load_q(a, t, t.row0 + v * 16, g, i, qb[v]);
-  float m_run[NT], l_run[NT];
+  float m_neg[NT], l_run[NT];
   f32x4 acc[NT][8];
 #pragma unroll
   for (int v = 0; v < NT; ++v) {
-    m_run[v] = -INFINITY;
+    m_neg[v] = INFINITY;
     l_run[v] = 0.f;
 #pragma unroll
     for (int dt = 0; dt < 8; ++dt) acc[v][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  auto run = [&](TreeUnit& u, const Next& nx) __attribute__((always_inline)) {
-    if constexpr (PAGED) transpose8(u.v);
-    const int n = BS == 16 ? (g < 2 ? nx.n0 : nx.n1) - (g & 1) * 8 : nx.n0 - g * 8;
-    const int keep = n < 0 ? 0 : (n > 8 ? 8 : n);
-    const bool partial = __builtin_amdgcn_ballot_w64(keep < 8) != 0;
-    if (partial) clear_tokens(u.v, keep);  // 0 times what an unused place holds must stay 0
-#pragma unroll
-    for (int v = 0; v < NT; ++v) {
-      float x[8];
-      unit_scores(u.k, qb[v], a.scale_log2, x);
-      if (partial) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = e < keep ? x[e] : -INFINITY;
-      }
-      unit_pv(u.v, unit_softmax(x, m_run[v], l_run[v], acc[v]), acc[v]);
-    }
-  };
-
   constexpr int kRows = NT * 16;
   constexpr int kPad = kHeadDim + 4;
   __shared__ float s_m[kTW][kRows], s_l[kTW][kRows], s_ml[2][kRows];
@@ -369,77 +388,83 @@ __global__ __launch_bounds__(kTW * 64) void tree_attn_kernel(TreeAttnArgs a) {
   __shared__ int s_wild[kTW];
   __shared__ __align__(16) float s_o[kTW][kRows][kPad];
 
-  TreeUnit ua, ub;
-  chunk_set();
-  Next na = next();
-  load(ua, na);
-
-  // ---- the tree's own tokens: unit tu of them to wave tu of the last split, while
-  // the first unit of the cache is on its way ----
+  // ---- the tree's own tokens: unit tu of them to wave tu of the last split ----
   const int tu = wave;
+  const bool tree = t.split == a.nsplit - 1 && tu * 32 < t.tlen;
   int wild = 0;
-  if (t.split == a.nsplit - 1 && tu * 32 < t.tlen) {
-    const uint64_t anc = ancestors(a.parent ? a.parent + (long long)t.r * a.T : nullptr, a.T, t.tlen, lane);
-    if (wave == 0) s_anc[lane] = anc;
+  if (tree) {
 #pragma unroll
     for (int tau = 0; tau < 2; ++tau) {
       const int j = min(tu * 32 + (int)tok + 4 * tau, t.tlen - 1);
 #pragma unroll
-      for (int st = 0; st < 4; ++st) ub.k[tau][st] = ldg16(a.tree_k + t.tree_base + j * t.tree_row + st * 32 + g * 8);
+      for (int st = 0; st < 4; ++st) u.k[tau][st] = ldg16(a.tree_k + t.tree_base + j * t.tree_row + st * 32 + g * 8);
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const int j = min(tu * 32 + 8 * g + e, t.tlen - 1);
-      ub.v[e] = ldg16(a.tree_v + t.tree_base + j * t.tree_row + i * 8);
+      u.v[e] = ldg16(a.tree_v + t.tree_base + j * t.tree_row + i * 8);
     }
-    transpose8(ub.v);
+    const uint64_t anc = ancestors(tree_parent(a, t.r, t.tlen, lane), t.tlen, lane);
+    if (wave == 0) s_anc[lane] = anc;
+    transpose8(u.v);
     const int n = t.tlen - tu * 32 - 8 * g;
-    clear_tokens(ub.v, n < 0 ? 0 : (n > 8 ? 8 : n));
-    wild = take_wild(ub.v);
+    clear_tokens(u.v, n < 0 ? 0 : (n > 8 ? 8 : n));
+    wild = take_wild(u.v);
     if constexpr (!PAGED) {
       // the working set's accumulators hold d-tile dt = dims 16 dt + i: through LDS,
       // [dim][32 tokens], each wave in its own part of the merge area
       u32x4* sv = reinterpret_cast<u32x4*>(&s_o[wave][0][0]);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) sv[(8 * i + j) * 4 + g] = ub.v[j];
+      for (int j = 0; j < 8; ++j) sv[(8 * i + j) * 4 + g] = u.v[j];
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
-      for (int dt = 0; dt < 8; ++dt) ub.v[dt] = sv[(16 * dt + i) * 4 + g];
+      for (int dt = 0; dt < 8; ++dt) u.v[dt] = sv[(16 * dt + i) * 4 + g];
     }
 #pragma unroll
     for (int v = 0; v < NT; ++v) {
       const int row = t.row0 + v * 16 + i;
       const int tq = row < a.rows ? row / a.G : 0;
       const uint32_t half = __shfl((uint32_t)(anc >> (tu * 32)), tq);
-      const uint32_t bits = half >> (8 * g) & 0xFF;
-      float x[8];
-      unit_scores(ub.k, qb[v], a.scale_log2, x);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = bits >> e & 1 ? x[e] : -INFINITY;
-      unit_pv(ub.v, unit_softmax(x, m_run[v], l_run[v], acc[v]), acc[v]);
+      f32x4 sc[2];
+      unit_scores(u.k, qb[v], sc);
+      mask_scores(sc, half >> (8 * g) & 0xFF);
+      unit_pv(u.v, unit_softmax(sc, a.scale_log2, m_neg[v], l_run[v], acc[v]), acc[v]);
     }
   }
   if (lane == 0) s_wild[wave] = wild;
 
-  // A unit's loads go out before the one ahead of it is computed.
-  Next nb = next();
-  load(ub, nb);
-  if (na.any) for (;;) {
-    run(ua, na);
-    if (!nb.any) break;
-    na = next();
-    load(ua, na);
-    run(ub, nb);
-    nb = next();
-    load(ub, nb);
-    if (!na.any) break;
-  }
+  // ---- the cache: the next unit's K is loaded once this one's scores are known, its V
+  // once this one's is used, into the same registers. Two workgroups of a CU hide what
+  // that leaves of the latency.
+  chunk_set();
+  Next cur = next();
+  load_k(cur);
+  load_v(cur);
+  while (cur.any) {
+    const Next nxt = next();
+    f32x4 sc[NT][2];
 #pragma unroll
-  for (int v = 0; v < NT; ++v) {
-    l_run[v] += __shfl_xor(l_run[v], 16);
-    l_run[v] += __shfl_xor(l_run[v], 32);
-    if (l_run[v] != l_run[v] && m_run[v] == -INFINITY) m_run[v] = 0.f;  // a NaN sum is not an empty one
+    for (int v = 0; v < NT; ++v) unit_scores(u.k, qb[v], sc[v]);
+    __builtin_amdgcn_sched_barrier(0);
+    load_k(nxt);
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (PAGED) transpose8(u.v);
+    if (cur.n0 < BS || (BS == 16 && cur.n1 < BS)) {
+      const int n = BS == 16 ? (g < 2 ? cur.n0 : cur.n1) - (g & 1) * 8 : cur.n0 - g * 8;
+      const int keep = n < 0 ? 0 : (n > 8 ? 8 : n);
+      clear_tokens(u.v, keep);  // 0 times what an unused place holds must stay 0
+#pragma unroll
+      for (int v = 0; v < NT; ++v) mask_scores(sc[v], (1u << keep) - 1);
+    }
+#pragma unroll
+    for (int v = 0; v < NT; ++v) unit_pv(u.v, unit_softmax(sc[v], a.scale_log2, m_neg[v], l_run[v], acc[v]), acc[v]);
+    __builtin_amdgcn_sched_barrier(0);
+    load_v(nxt);
+    cur = nxt;
   }
+  float m_run[NT];
+#pragma unroll
+  for (int v = 0; v < NT; ++v) m_run[v] = finish_row(m_neg[v], l_run[v]);
 
   // ---- merge the waves through LDS ----
   if (g == 0) {
@@ -500,12 +525,10 @@ __global__ __launch_bounds__(kTW * 64) void tree_attn_kernel(TreeAttnArgs a) {
 }
 
 // 16 bytes a lane from global memory straight into LDS: lane L's bytes land at
-// lds_row + 16 L, lds_row being the same in every lane. In assembly for the reason
+// offset lds + 16 L, lds being the same in every lane. In assembly for the reason
 // given at the working set's attention (lds_dma16): the compiler would drain every
 // earlier load before each one; the waits are the kernel's own counts instead.
-__device__ __forceinline__ void tree_dma16(const void* src, void* lds_row) {
-  const uint32_t lds =
-      __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)lds_row);
+__device__ __forceinline__ void tree_dma16(const void* src, uint32_t lds) {
   uint32_t saved;
   asm volatile(
       "s_mov_b32 %0, m0\n\t"
@@ -517,66 +540,74 @@ __device__ __forceinline__ void tree_dma16(const void* src, void* lds_row) {
       : "v"(src), "s"(lds)
       : "memory");
 }
+__device__ __forceinline__ uint32_t lds_offset(const void* p) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
+}
 template <int N>
 __device__ __forceinline__ void tree_wait() {  // s_waitcnt vmcnt(N) alone
   static_assert(N >= 0 && N < 64, "vmcnt range");
   __builtin_amdgcn_s_waitcnt((N & 0xF) | ((N >> 4) << 14) | (0x7 << 4) | (0xF << 8));
 }
 
-// More than two row tiles. Eight waves: RT places for row tiles, NT tiles in each,
-// and TM teams of them (RT * TM = 8). A step is two units; with two teams each
-// takes one of them, with one both. A ring of kRingSteps steps in LDS is filled by
-// loads that go straight there, four a wave and step; one barrier a step
-// publishes it and frees the one before.
+// More than two row tiles. Eight waves in two teams: a wave holds one or two of a
+// team's (up to) eight row tiles, and a team takes every other unit. A step is two
+// units, one for each team; a ring of kRingSteps steps in LDS is filled by loads that
+// go straight there, four a wave and step; one barrier a step publishes it and frees
+// the one before. Two tiles a wave: each unit is read from LDS by four waves, 64 KB,
+// which takes as long as their products do.
 //
-// The units of a split are listed first, the ones without an attended token left
-// out, up to kListUnits at a time. K is put into LDS in MFMA operand layout, and so
-// is the working set's V. Token-major V lies there row by row, 16-byte piece c of
-// row p at c ^ swizzle(p), and the transposing read takes 4 tokens x 16 dims a group
-// of 16 lanes: lane (g, i) names dims 4 (i % 4) .. +3 of token i / 4 and receives
-// dim i of the 4 tokens. The swizzle spreads the tokens that one read names over
-// different banks.
+// The units of a split are listed first, up to kListUnits at a time, the ones without
+// an attended token left out: whole ones ahead, which a loop without masks takes, then
+// the others, then the tree's. K is put into LDS in MFMA operand layout, and so is
+// the working set's V. Of token-major V every load takes four tokens, their 32-byte
+// pieces in turn (token p's piece dt at 128 dt + 32 p), and the transposing read takes
+// 4 tokens x 16 dims a group of 16 lanes, 128 bytes in a row: lane (g, i) names dims
+// 4 (i % 4) .. +3 of token i / 4 and receives dim i of the four.
+//
+// A unit's order is: V is read, scores; the next unit's K is read; softmax, second
+// product. So LDS reads run beside the products, in the registers that these leave.
 constexpr int kRingSteps = 4;
 constexpr int kListUnits = 1024;
-constexpr int kListPad = 2 + 2 * kRingSteps;  // the tree's units, and none behind them
+constexpr int kListPad = 4 + 2 * kRingSteps;  // the tree's units, and none behind them
 constexpr int kRowsThreads = 512;
+constexpr int kRowPlaces = 4;  // waves of a team
+// A unit in LDS: 8 KB of K, 8 KB of V, and 128 bytes between the loads of token-major
+// V that lanes 16 g .. +15 read, so that two of these groups meet no bank twice.
+constexpr int kUnitBytes = 16 * 1024 + 512;
 
-__device__ __forceinline__ int v_swizzle(int token) { return ((token & 3) | (token >> 1 & 4)) << 1; }
-
-template <int RT, int TM, int NT, int BS, bool PAGED>
+template <int NT, int BS, bool PAGED>
 __global__ __launch_bounds__(kRowsThreads) void tree_attn_rows_kernel(TreeAttnArgs a) {
-  static_assert(RT * TM == 8 && (TM == 1 || TM == 2), "eight waves");
-  constexpr int kLook = kRingSteps - 1;
-  __shared__ __align__(16) u32x4 s_ring[kRingSteps][2][16][64];
-  __shared__ __align__(16) int4 s_list[kListUnits + kListPad];  // places, attended tokens of a unit's blocks (see below)
+  constexpr int kRows = NT * kRowPlaces * 16;
+  constexpr int kPad = kHeadDim + 4;
+  __shared__ __align__(16) char s_ring[kRingSteps * 2 * kUnitBytes];
+  // places and attended tokens of a unit's blocks; x: which, z = -1: a unit of the tree; z = -2: none
+  __shared__ __align__(16) int4 s_list[kListUnits + kListPad];
   __shared__ uint64_t s_anc[kTreeMaxTokens];
-  __shared__ int s_wave[8], s_wild;
+  __shared__ float s_ml[2][kRows];
+  __shared__ int s_wave[8][2], s_wild;
+  static_assert(sizeof(float) * kRows * kPad <= sizeof(s_ring), "a team's rows fit the ring");
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
   const int g = lane >> 4;
   const int i = lane & 15;
-  const int team = TM == 1 ? 0 : wave / RT;
-  const int rt = TM == 1 ? wave : wave % RT;
+  const int team = wave / kRowPlaces;
+  const int rt = wave % kRowPlaces;  // this wave's tiles: rt and rt + 4 of the group's
   TreeItem t;
   if (!tree_setup<BS, PAGED>(a, a.tiles * 16, t)) return;
   int L, u_begin, u_end;
   const Ctx c = tree_units<BS, PAGED>(a, t, L, u_begin, u_end);
   const bool last_split = t.split == a.nsplit - 1;
 
-  // tile v of this wave is rt + v * RT of the group
-  const int nv = rt >= a.tiles ? 0 : (a.tiles - rt + RT - 1) / RT;
   bf16x8 qb[NT][4];
 #pragma unroll
-  for (int v = 0; v < NT; ++v) load_q(a, t, t.row0 + (rt + v * RT) * 16, g, i, qb[v]);
-  if (wave == 0) {
-    if (last_split) s_anc[lane] = ancestors(a.parent ? a.parent + (long long)t.r * a.T : nullptr, a.T, t.tlen, lane);
-    if (lane == 0) s_wild = 0;
-  }
-  float m_run[NT], l_run[NT];
+  for (int v = 0; v < NT; ++v) load_q(a, t, t.row0 + (rt + v * kRowPlaces) * 16, g, i, qb[v]);
+  const int parent = last_split && wave == 0 ? tree_parent(a, t.r, t.tlen, lane) : -1;
+  if (threadIdx.x == 0) s_wild = 0;
+  float m_neg[NT], l_run[NT];
   f32x4 acc[NT][8];
 #pragma unroll
   for (int v = 0; v < NT; ++v) {
-    m_run[v] = -INFINITY;
+    m_neg[v] = INFINITY;
     l_run[v] = 0.f;
 #pragma unroll
     for (int dt = 0; dt < 8; ++dt) acc[v][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -584,34 +615,35 @@ __global__ __launch_bounds__(kRowsThreads) void tree_attn_rows_kernel(TreeAttnAr
 
   // What this wave loads: of unit `half` of a step, four pieces of K (token tile
   // j0 / 4, its four k-steps) or of V. A lane's element offset within the unit's block
-  // lo or hi, piece jj being jj * step further, xor-ed from the third on.
+  // lo or hi, piece jj being jj * step further.
   const int half = wave >> 2;
   const bool load_v = wave & 2;
   const int j0 = (wave & 1) * 4;
   const int k_row = 8 * (i >> 2) + (i & 3) + j0;  // K: this lane's token of the unit
-  const int v_row = 4 * j0 + g;                   // token-major V: of the first piece
+  const int v_row = 4 * j0 + (lane >> 1 & 3);     // token-major V: of the first piece
+  const int v_col = (lane >> 3) * 16 + (lane & 1) * 8;
   int off;
   bool hi;
   if (!load_v) {
     off = (BS == 16 ? k_row & 15 : k_row) * kHeadDim + g * 8;
     hi = BS == 16 && k_row >= 16;
   } else if (PAGED) {
-    off = (BS == 16 ? v_row & 15 : v_row) * kHeadDim + (i ^ v_swizzle(v_row)) * 8;
+    off = (BS == 16 ? v_row & 15 : v_row) * kHeadDim + v_col;
     hi = BS == 16 && v_row >= 16;
   } else {
     off = (j0 * 16 + i) * BS + (BS == 16 ? g & 1 : g) * 8;
     hi = BS == 16 && g >= 2;
   }
   const int step = !load_v ? 32 : (PAGED ? 4 * kHeadDim : 16 * BS);
-  const int flip = load_v && PAGED ? 64 : 0;  // rows 8 apart: the swizzle's highest bit
   const uint16_t* src0 = load_v ? t.vb : t.kb;
+  const uint32_t ring = lds_offset(s_ring);
   const int tree_units_n = last_split ? (t.tlen + 31) / 32 : 0;
 
   for (int seg = u_begin; seg == u_begin || seg < u_end; seg += kListUnits) {
-    // ---- list this segment's units ----
+    // ---- list this segment's units: whole ones from the front, others from the back ----
     const int n_seg = min(kListUnits, u_end - seg);
     const bool final_seg = seg + kListUnits >= u_end;
-    int total = 0;
+    int n_full = 0, n_part = 0;
     for (int b0 = 0; b0 < n_seg; b0 += kRowsThreads) {
       const int n = b0 + (int)threadIdx.x;
       int4 e = make_int4(0, 0, 0, 0);
@@ -619,172 +651,217 @@ __global__ __launch_bounds__(kRowsThreads) void tree_attn_rows_kernel(TreeAttnAr
         const int b = (seg + n) * (32 / BS);
         block_entry<BS, PAGED>(a, c, L, b, block_raw<BS, PAGED>(a, t, c, b), e.x, e.z);
         if (BS == 16) block_entry<BS, PAGED>(a, c, L, b + 1, block_raw<BS, PAGED>(a, t, c, b + 1), e.y, e.w);
-        if (e.w < 0) e.w = 0;  // a block past the context
+        e.w = max(e.w, 0);  // a block past the context
       }
-      const bool live = e.z > 0 || e.w > 0;
-      const uint64_t bal = __builtin_amdgcn_ballot_w64(live);
-      if (lane == 0) s_wave[wave] = __popcll(bal);
+      const bool full = e.z == BS && (BS == 32 || e.w == BS);
+      const bool part = !full && (e.z > 0 || e.w > 0);
+      const uint64_t fulls = __builtin_amdgcn_ballot_w64(full), parts = __builtin_amdgcn_ballot_w64(part);
+      if (lane == 0) {
+        s_wave[wave][0] = __popcll(fulls);
+        s_wave[wave][1] = __popcll(parts);
+      }
       __syncthreads();
-      int at = total, all = 0;
+      const uint64_t below = (1ull << lane) - 1;
+      int at_f = n_full + __popcll(fulls & below), at_p = n_part + __popcll(parts & below);
       for (int w = 0; w < 8; ++w) {
-        const int k = s_wave[w];
-        at += w < wave ? k : 0;
-        all += k;
+        const int kf = s_wave[w][0], kp = s_wave[w][1];
+        at_f += w < wave ? kf : 0;
+        at_p += w < wave ? kp : 0;
+        n_full += kf;
+        n_part += kp;
       }
-      if (live) s_list[at + __popcll(bal & ((1ull << lane) - 1))] = e;
-      total += all;
+      if (full) s_list[at_f] = e;
+      if (part) s_list[kListUnits - 1 - at_p] = e;
       __syncthreads();
     }
-    // behind them the tree's units (x: which, z: -1) and the places of none (z: -2)
+    n_full = __builtin_amdgcn_readfirstlane(n_full);
+    n_part = __builtin_amdgcn_readfirstlane(n_part);
+    const int total = n_full + n_part;
     const int units = total + (final_seg ? tree_units_n : 0);
     const int steps = (units + 1) / 2;
-    if (threadIdx.x < kListPad) {
-      const int n = total + (int)threadIdx.x;
-      s_list[n] = n < units ? make_int4((int)threadIdx.x, 0, -1, 0) : make_int4(0, 0, -2, 0);
-    }
+    if (threadIdx.x < kListPad)
+      s_list[kListUnits + threadIdx.x] =
+          total + (int)threadIdx.x < units ? make_int4((int)threadIdx.x, 0, -1, 0) : make_int4(0, 0, -2, 0);
     __syncthreads();
-    auto entry = [&](int n) __attribute__((always_inline)) {
-      const int4 e = s_list[n];
+    auto entry_read = [&](int n) __attribute__((always_inline)) {
+      return s_list[n < n_full ? n : (n < total ? kListUnits - 1 - (n - n_full) : kListUnits + (n - total))];
+    };
+    auto uniform = [&](int4 e) __attribute__((always_inline)) {
       return make_int4(__builtin_amdgcn_readfirstlane(e.x), __builtin_amdgcn_readfirstlane(e.y),
                        __builtin_amdgcn_readfirstlane(e.z), __builtin_amdgcn_readfirstlane(e.w));
     };
-    auto issue = [&](int s) __attribute__((always_inline)) {
-      const int4 e = entry(s * 2 + half);
-      u32x4* dst = &s_ring[s % kRingSteps][half][(load_v ? 8 : 0) + j0][0];
-      int o = off;
-      asm volatile("" : "+v"(o));  // the sums below are not worth a register each from step to step
+    // This wave's loads of step s, whose list entry is `raw`.
+    auto issue = [&](int s, int4 raw) __attribute__((always_inline)) {
+      const int4 e = uniform(raw);
+      const uint32_t dst = ring + (uint32_t)((s % kRingSteps * 2 + half) * kUnitBytes + ((load_v ? 8 : 0) + j0) * 1024);
+      const uint32_t skew = load_v && (PAGED || e.z == -1) ? 128u : 0u;  // per two loads
       if (e.z != -1) {
-        const uint16_t* src = src0 + (long long)(hi ? e.y : e.x) * t.unit_elems;
+        const uint16_t* src = src0 + (long long)(hi ? e.y : e.x) * t.unit_elems + off;
 #pragma unroll
-        for (int jj = 0; jj < 4; ++jj) tree_dma16(src + ((o + jj * step) ^ (jj >= 2 ? flip : 0)), dst + jj * 64);
+        for (int jj = 0; jj < 4; ++jj) tree_dma16(src + jj * step, dst + jj * 1024 + (j0 + jj) / 2 * skew);
       } else {  // the tree's rows
+        int ll = lane;
+        asm volatile("" : "+v"(ll));  // its terms are not worth registers through the loop
         const uint16_t* src = (load_v ? a.tree_v : a.tree_k) + t.tree_base;
 #pragma unroll
         for (int jj = 0; jj < 4; ++jj) {
-          const int row = load_v ? 4 * (j0 + jj) + g : k_row;
-          const int col = load_v ? (i ^ v_swizzle(row)) * 8 : jj * 32 + g * 8;
-          tree_dma16(src + min(e.x * 32 + row, t.tlen - 1) * t.tree_row + col, dst + jj * 64);
+          const int row = load_v ? 4 * (j0 + jj) + (ll >> 1 & 3) : 8 * (ll >> 2 & 3) + (ll & 3) + j0;
+          const int col = load_v ? (ll >> 3) * 16 + (ll & 1) * 8 : jj * 32 + (ll >> 4) * 8;
+          tree_dma16(src + min(e.x * 32 + row, t.tlen - 1) * t.tree_row + col, dst + jj * 1024 + (j0 + jj) / 2 * skew);
         }
       }
     };
-    for (int s = 0; s < kLook; ++s) issue(s);
-
-    for (int s = 0; s < steps; ++s) {
-      // this wave's loads of step s are in; the barrier publishes every wave's and
-      // tells that the step before is no longer read, whose place takes step s + kLook
-      tree_wait<4 * (kLook - 1)>();
-      __syncthreads();
-      issue(s + kLook);
-#pragma unroll 1
-      for (int half_u = TM == 1 ? 0 : team; half_u < (TM == 1 ? 2 : team + 1); ++half_u) {
-        const int4 e = entry(s * 2 + half_u);
-        if (e.z == -2 || nv == 0) continue;
-        const u32x4(&buf)[16][64] = s_ring[s % kRingSteps][half_u];
-        const bool tree = e.z == -1;
-        TreeUnit u;
+    TreeUnit u;
+    auto unit_at = [&](int s) __attribute__((always_inline)) { return s_ring + (s % kRingSteps * 2 + team) * kUnitBytes; };
+    auto read_k = [&](int s) __attribute__((always_inline)) {
+      const u32x4* at = reinterpret_cast<const u32x4*>(unit_at(s)) + lane;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) u.k[j >> 2][j & 3] = buf[j][lane];
-        if (PAGED || tree) {
-          char* rows = reinterpret_cast<char*>(&s_ring[s % kRingSteps][half_u][8][0]);
-          typedef short s16x4 __attribute__((ext_vector_type(4)));
-          typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-          const int token = 8 * g + (i >> 2);  // and 4 further, with the same swizzle
+      for (int j = 0; j < 8; ++j) u.k[j >> 2][j & 3] = at[j * 64];
+    };
+    auto read_v = [&](int s, bool by_row) __attribute__((always_inline)) {
+      if (by_row) {
+        typedef short s16x4 __attribute__((ext_vector_type(4)));
+        typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+        // tokens 8 g + 4 q .. +3 at load 2 g + q
+        char* at = unit_at(s) + 8192 + g * (2048 + 128) + (i >> 2) * 32 + (i & 3) * 8;
 #pragma unroll
-          for (int dt = 0; dt < 8; ++dt) {
-            char* at = rows + token * 256 + ((2 * dt + (i >> 1 & 1)) ^ v_swizzle(token)) * 16 + (i & 1) * 8;
+        for (int dt = 0; dt < 8; ++dt)
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {
-              const u32x2 w = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                                                            (__attribute__((address_space(3))) s16x4*)(at + q * 1024)));
-              u.v[dt][2 * q] = w[0];
-              u.v[dt][2 * q + 1] = w[1];
-            }
+          for (int q = 0; q < 2; ++q) {
+            const u32x2 w = __builtin_bit_cast(
+                u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                           (__attribute__((address_space(3))) s16x4*)(at + q * 1024 + dt * 128)));
+            u.v[dt][2 * q] = w[0];
+            u.v[dt][2 * q + 1] = w[1];
           }
-        } else {
+      } else {
+        const u32x4* at = reinterpret_cast<const u32x4*>(unit_at(s)) + 512 + lane;
 #pragma unroll
-          for (int dt = 0; dt < 8; ++dt) u.v[dt] = buf[8 + dt][lane];
-        }
-        const int n = tree ? t.tlen - e.x * 32 - 8 * g
-                           : (BS == 16 ? (g < 2 ? e.z : e.w) - (g & 1) * 8 : e.z - g * 8);
+        for (int dt = 0; dt < 8; ++dt) u.v[dt] = at[dt * 64];
+      }
+    };
+    // Between the barriers of steps s - 1 and s the units of steps s and s + 1 are in
+    // LDS, and the loads of step s + 3 go out, into the place of step s - 1. Behind
+    // barrier s step s + 2 is there too: this wave's loads of it are in by then, and
+    // the barrier publishes every wave's and tells that step s is no longer read.
+    auto leave = [&]() __attribute__((always_inline)) {
+      tree_wait<4>();
+      __syncthreads();
+    };
+#pragma unroll 1
+    for (int s = 0; s < 3; ++s) issue(s, entry_read(s * 2 + half));
+    if (last_split && wave == 0 && seg == u_begin) s_anc[lane] = ancestors(parent, t.tlen, lane);
+    leave();
+    read_k(0);
+    f32x4 sc[NT][2];
+    auto attend = [&]() __attribute__((always_inline)) {
+#pragma unroll
+      for (int v = 0; v < NT; ++v) unit_pv(u.v, unit_softmax(sc[v], a.scale_log2, m_neg[v], l_run[v], acc[v]), acc[v]);
+      __builtin_amdgcn_sched_barrier(0);  // no reads ahead of it, into registers that are then spilled
+    };
+    // The two waves of a SIMD are of different teams, and do a step's parts in
+    // different order, so that one's products run beside the other's softmax: team 0
+    // leaves a unit's softmax and second product to the next step.
+    const int whole = n_full / 2;  // steps of two whole units
+#pragma unroll 1
+    for (int s = 0; s < steps; ++s) {
+      // (32 loads at once, behind the barrier, would hold every wave up for some 500
+      // cycles: each team's go out at another time, the list entry read ahead)
+      const int4 ahead = entry_read((s + 3) * 2 + half);
+      if (team == 0) {
+        if (s > 0) attend();
+        issue(s + 3, ahead);
+      }
+      read_v(s, PAGED);
+#pragma unroll
+      for (int v = 0; v < NT; ++v) unit_scores(u.k, qb[v], sc[v]);
+      __builtin_amdgcn_sched_barrier(0);
+      read_k(s + 1);
+      if constexpr (PAGED) {  // the halves of the reads above are one operand from here on, in every branch
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) asm volatile("" : "+v"(u.v[dt]));
+      }
+      if (s >= whole) {  // masks
+        const int4 e = uniform(entry_read(s * 2 + team));
+        const bool tree = e.z == -1;
+        if (tree && !PAGED) read_v(s, true);
+        const int n = tree ? t.tlen - e.x * 32 - 8 * g : (BS == 16 ? (g < 2 ? e.z : e.w) - (g & 1) * 8 : e.z - g * 8);
         const int keep = n < 0 ? 0 : (n > 8 ? 8 : n);
-        const bool partial = __builtin_amdgcn_ballot_w64(keep < 8) != 0;
-        if (partial) clear_tokens(u.v, keep);  // 0 times what an unused place holds must stay 0
-        if (tree && take_wild(u.v)) s_wild = 1;
+        clear_tokens(u.v, keep);  // 0 times what an unused place holds must stay 0
+        if (tree) {
+          if (take_wild(u.v)) s_wild = 1;
+        }
 #pragma unroll
         for (int v = 0; v < NT; ++v) {
-          if (v > 0 && v >= nv) break;
-          float x[8];
-          unit_scores(u.k, qb[v], a.scale_log2, x);
-          if (tree || partial) {
-            uint32_t bits = (1u << keep) - 1;
-            if (tree) {
-              const int row = t.row0 + (rt + v * RT) * 16 + i;
-              bits = (uint32_t)(s_anc[row < a.rows ? row / a.G : 0] >> (e.x * 32 + 8 * g));
-            }
-#pragma unroll
-            for (int f = 0; f < 8; ++f) x[f] = bits >> f & 1 ? x[f] : -INFINITY;
+          uint32_t bits = (1u << keep) - 1;
+          if (tree) {
+            const int row = t.row0 + (rt + v * kRowPlaces) * 16 + i;
+            bits = (uint32_t)(s_anc[row < a.rows ? row / a.G : 0] >> (e.x * 32 + 8 * g));
           }
-          unit_pv(u.v, unit_softmax(x, m_run[v], l_run[v], acc[v]), acc[v]);
+          mask_scores(sc[v], bits);
         }
       }
+      if (team == 1) {
+        attend();
+        issue(s + 3, ahead);
+      }
+      leave();
     }
+    if (team == 0 && steps > 0) attend();
     tree_wait<0>();   // the loads past the last step land before the ring and the list are reused
     __syncthreads();
   }
 
+  // ---- merge the teams: the second one's rows through LDS, the sums back there ----
+  float(*s_o)[kPad] = reinterpret_cast<float(*)[kPad]>(s_ring);  // [row of the group]
 #pragma unroll
-  for (int v = 0; v < NT; ++v) {
-    l_run[v] += __shfl_xor(l_run[v], 16);
-    l_run[v] += __shfl_xor(l_run[v], 32);
-    if (l_run[v] != l_run[v] && m_run[v] == -INFINITY) m_run[v] = 0.f;  // a NaN sum is not an empty one
+  for (int v = 0; v < NT; ++v) m_neg[v] = -finish_row(m_neg[v], l_run[v]);
+  if (team == 1) {
+#pragma unroll
+    for (int v = 0; v < NT; ++v) {
+      const int row = (rt + v * kRowPlaces) * 16 + i;
+#pragma unroll
+      for (int dt = 0; dt < 8; ++dt) *reinterpret_cast<f32x4*>(&s_o[row][16 * dt + 4 * g]) = acc[v][dt];
+      if (g == 0) {
+        s_ml[0][row] = -m_neg[v];
+        s_ml[1][row] = l_run[v];
+      }
+    }
   }
-  const int end = min(t.tlen * a.G, a.rows);  // rows in the tree
-  const long long pbase = ((long long)t.rh * a.nsplit + t.split) * a.rows;
-  // d-tiles d0 .. d0 + 4 * n of a row: its output, or its partial
-  auto put = [&](int row, const f32x4* o, int d0, int n, float M, float S) __attribute__((always_inline)) {
-    if (row >= end) return;
+  __syncthreads();
+  if (team == 0) {
 #pragma unroll
-    for (int dt = 0; dt < n; ++dt) {
-      const int c4 = (d0 + dt) * 4 + g;
-      f32x4 x = o[dt];
-      if (s_wild) add_wild(a, t, s_anc[row / a.G], c4, x);
-      if (a.nsplit == 1) write_row(a, t.r, t.h, row, c4, x, M, S);
-      else *reinterpret_cast<f32x4*>(a.part_o + (pbase + row) * kHeadDim + c4 * 4) = x;
+    for (int v = 0; v < NT; ++v) {
+      const int row = (rt + v * kRowPlaces) * 16 + i;
+      const float m0 = -m_neg[v], m1 = s_ml[0][row], M = fmaxf(m0, m1);
+      const float f0 = m0 == -INFINITY ? 0.f : fast_exp2(m0 - M), f1 = m1 == -INFINITY ? 0.f : fast_exp2(m1 - M);
+      const float S = l_run[v] * f0 + s_ml[1][row] * f1;
+#pragma unroll
+      for (int dt = 0; dt < 8; ++dt) {
+        f32x4& o = *reinterpret_cast<f32x4*>(&s_o[row][16 * dt + 4 * g]);
+        o = acc[v][dt] * f0 + o * f1;
+      }
+      if (g == 0) {  // the row's other lanes have read them
+        s_ml[0][row] = M;
+        s_ml[1][row] = S;
+      }
     }
-    if (a.nsplit > 1 && g == 0 && d0 == 0)
-      *reinterpret_cast<float2*>(a.part_ml + (pbase + row) * 2) = make_float2(M, S);
-  };
-  if constexpr (TM == 1) {
-#pragma unroll
-    for (int v = 0; v < NT; ++v)
-      if (v < nv) put(t.row0 + (rt + v * RT) * 16 + i, acc[v], 0, 8, m_run[v], l_run[v]);
-  } else {
-    // the teams exchange halves of the dims through LDS: team 0 finishes d-tiles 0-3, team 1 4-7
-    static_assert(NT == 1, "one tile a wave with two teams");
-    constexpr int kHalf = kHeadDim / 2 + 4;
-    float(*s_o)[16][kHalf] = reinterpret_cast<float(*)[16][kHalf]>(&s_ring[0][0][0][0]);  // [wave]
-    float(*s_ml)[2][16] = reinterpret_cast<float(*)[2][16]>(&s_list[0]);                 // [wave]
-    f32x4 mine[4];
-#pragma unroll
-    for (int dt = 0; dt < 4; ++dt) {
-      mine[dt] = team == 0 ? acc[0][dt] : acc[0][dt + 4];
-      *reinterpret_cast<f32x4*>(&s_o[wave][i][dt * 16 + 4 * g]) = team == 0 ? acc[0][dt + 4] : acc[0][dt];
+  }
+  __syncthreads();
+  const long long pbase = ((long long)t.rh * a.nsplit + t.split) * a.rows + t.row0;
+  const int last = min(min(t.tlen * a.G, a.rows) - t.row0, a.tiles * 16);  // rows of this group in the tree
+  for (int pos = threadIdx.x; pos < kRows * (kHeadDim / 4); pos += kRowsThreads) {
+    const int row = pos >> 5;
+    const int c4 = pos & 31;
+    if (row >= last) break;
+    f32x4 o = *reinterpret_cast<const f32x4*>(&s_o[row][c4 * 4]);
+    if (s_wild) add_wild(a, t, s_anc[(t.row0 + row) / a.G], c4, o);
+    if (a.nsplit == 1) {
+      write_row(a, t.r, t.h, t.row0 + row, c4, o, s_ml[0][row], s_ml[1][row]);
+    } else {
+      *reinterpret_cast<f32x4*>(a.part_o + (pbase + row) * kHeadDim + c4 * 4) = o;
+      if (c4 == 0) *reinterpret_cast<float2*>(a.part_ml + (pbase + row) * 2) = make_float2(s_ml[0][row], s_ml[1][row]);
     }
-    if (g == 0) {
-      s_ml[wave][0][i] = m_run[0];
-      s_ml[wave][1][i] = l_run[0];
-    }
-    __syncthreads();
-    const int other = wave < RT ? wave + RT : wave - RT;
-    const float mo = s_ml[other][0][i], lo = s_ml[other][1][i];
-    const float M = fmaxf(m_run[0], mo);
-    const float f = m_run[0] == -INFINITY ? 0.f : fast_exp2(m_run[0] - M);
-    const float fo = mo == -INFINITY ? 0.f : fast_exp2(mo - M);
-    const float S = l_run[0] * f + lo * fo;
-#pragma unroll
-    for (int dt = 0; dt < 4; ++dt)
-      mine[dt] = mine[dt] * f + *reinterpret_cast<const f32x4*>(&s_o[other][i][dt * 16 + 4 * g]) * fo;
-    if (nv) put(t.row0 + rt * 16 + i, mine, team * 4, 4, M, S);
   }
 }
 
@@ -838,16 +915,22 @@ template <int BS, bool PAGED>
 void launch_bs(const TreeAttnArgs& a, hipStream_t s) {
   const long long items = (long long)a.R * a.Hkv * a.nsplit * a.groups;
   const dim3 grid((unsigned)((items + 7) / 8 * 8));
+  // What the tables and pools hold at most: past kStreamBytes V, whose loads take whole
+  // lines, is read past the caches (8 x 131,072 tokens, 4.3 GB, 711 and 640 us; 64 x
+  // 2,064, 541 MB, half of it attended, 80.8 and 76.5; 68 MB, in the Infinity Cache, 21.2
+  // and 21.3; K as well 639, 80.1).
+  const long long blocks = PAGED ? a.NBmax : (a.k_slots + 1ll < a.NBmax ? a.k_slots + 1ll : a.NBmax);
+  const bool stream = (long long)a.R * a.Hkv * blocks * BS * (2 * kHeadDim * 2) >= kStreamBytes;
   if (a.tiles == 1)
-    hipLaunchKernelGGL((tree_attn_kernel<1, BS, PAGED>), grid, dim3(kTW * 64), 0, s, a);
+    hipLaunchKernelGGL((stream ? tree_attn_kernel<1, BS, PAGED, true> : tree_attn_kernel<1, BS, PAGED, false>), grid,
+                       dim3(kTW * 64), 0, s, a);
   else if (a.tiles == 2)
-    hipLaunchKernelGGL((tree_attn_kernel<2, BS, PAGED>), grid, dim3(kTW * 64), 0, s, a);
-  else if (a.tiles <= 4)
-    hipLaunchKernelGGL((tree_attn_rows_kernel<4, 2, 1, BS, PAGED>), grid, dim3(kRowsThreads), 0, s, a);
-  else if (a.tiles <= 8)
-    hipLaunchKernelGGL((tree_attn_rows_kernel<8, 1, 1, BS, PAGED>), grid, dim3(kRowsThreads), 0, s, a);
+    hipLaunchKernelGGL((stream ? tree_attn_kernel<2, BS, PAGED, true> : tree_attn_kernel<2, BS, PAGED, false>), grid,
+                       dim3(kTW * 64), 0, s, a);
+  else if (a.tiles <= kRowPlaces)
+    hipLaunchKernelGGL((tree_attn_rows_kernel<1, BS, PAGED>), grid, dim3(kRowsThreads), 0, s, a);
   else
-    hipLaunchKernelGGL((tree_attn_rows_kernel<8, 1, 2, BS, PAGED>), grid, dim3(kRowsThreads), 0, s, a);
+    hipLaunchKernelGGL((tree_attn_rows_kernel<2, BS, PAGED>), grid, dim3(kRowsThreads), 0, s, a);
 }
 
 }  // namespace

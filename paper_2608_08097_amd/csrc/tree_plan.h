@@ -12,7 +12,8 @@
 namespace oasis {
 
 constexpr int kTreeWaves = 4;     // waves per workgroup of the form for up to two row tiles
-constexpr int kTreeTiles = 16;    // 16-row tiles per workgroup at most
+constexpr int kTreeRegisterTiles = 2;  // 16-row tiles up to which K and V go straight into registers
+constexpr int kTreeTiles = 8;     // 16-row tiles per workgroup at most
 constexpr int kTreeMaxTokens = 64;  // a row's ancestors are one 64-bit mask
 constexpr int kTreeMaxRows = 4096;  // G * T
 constexpr int kTreeMaxSplits = 256;
@@ -24,8 +25,20 @@ struct TreePlan {
   std::size_t part_o_floats, bytes;
 };
 
-// `units`: 32-token units of the longest context the caller's tables hold.
-inline TreePlan tree_plan(long long pairs, int G, int T, int units) {
+// `units`: 32-token units of the longest context the caller's tables hold; `ragged`:
+// the contexts may be shorter than that.
+//
+// The split count is the one with the least estimated time, in tenths of a
+// microsecond: rounds of workgroups over the CUs, times what one of them takes, and
+// the merge of their partials. A workgroup takes its start and end and its units, at
+// the latency of its waves' loads or of their products, or at its share of the
+// bandwidth (16 KB a unit and KV head) where that is slower. Where contexts are ragged
+// the longest workgroup ends the call, so the most splits within 3 % of the least are
+// taken. Measured against neighbouring counts (pairs, rows, units: count and us): 64, 20,
+// 4,096: 2 840, 3 708, 4 712, 5 864, 8 722; 64, 20, 65: 1 27.3, 2 22.3, 3 20.7, 4 21.2,
+// 5 25.0; 16, 512, 2,048: 3 337, 4 296, 6 404; 192, 64, up to 1,024: 1 360, 2 257, 3 267,
+// 4 234, 8 269; 128, 256, 129: 1 98, 2 116; 512, 28, 65: 1 81, 2 92.
+inline TreePlan tree_plan(long long pairs, int G, int T, int units, bool ragged) {
   TreePlan p{};
   p.rows = G * T;
   const int tiles = (p.rows + 15) / 16;
@@ -33,16 +46,33 @@ inline TreePlan tree_plan(long long pairs, int G, int T, int units) {
   p.tiles = (tiles + p.groups - 1) / p.groups;
   p.units = units;
   const long long items = pairs * p.groups;
-  // one workgroup per CU, and up to four where each still has 64 units
-  long long want = items > 0 ? 256 / items : 1;
-  if (want < 1) want = 1;
-  long long more = items > 0 ? 1024 / items : 1;
-  if (more > units / 64) more = units / 64;
-  if (want < more) want = more;
-  const long long most = (units + 2 * kTreeWaves - 1) / (2 * kTreeWaves);  // two units a wave at least
-  if (want > most) want = most;
-  if (want > kTreeMaxSplits) want = kTreeMaxSplits;
-  p.nsplit = (int)(want < 1 ? 1 : want);
+  const bool rows_form = p.tiles > kTreeRegisterTiles;
+  const long long slots = rows_form ? 256 : 512;  // workgroups that the CUs hold at once
+  long long most = (units + kTreeWaves - 1) / kTreeWaves;  // a unit a wave
+  if (most > kTreeMaxSplits) most = kTreeMaxSplits;
+  if (items > 0 && most > 4 * slots / items) most = 4 * slots / items;
+  auto estimate = [&](long long n) {
+    const long long u = (units + n - 1) / n;
+    const long long rounds = (items * n + slots - 1) / slots;
+    const long long at_once = items * n < slots ? items * n : slots;
+    const long long share = u * 63 * at_once / (2560 * p.groups);  // 6.7 TB/s over 256 CUs
+    long long body = rows_form ? u * 6 : (u + kTreeWaves - 1) / kTreeWaves * 16;
+    if (body < share) body = share;
+    const long long merge = n > 1 ? 30 + pairs * n * p.rows * 1040 / 300000 : 0;  // both ways at 3 TB/s
+    return rounds * (body + (rows_form ? 110 : 70)) + merge;
+  };
+  long long best = estimate(1);
+  p.nsplit = 1;
+  for (long long n = 2; n <= most; ++n) {
+    const long long t = estimate(n);
+    if (t < best) {
+      best = t;
+      p.nsplit = (int)n;
+    }
+  }
+  if (ragged)
+    for (long long n = most; n > p.nsplit; --n)
+      if (estimate(n) * 100 <= best * 103) p.nsplit = (int)n;
   if (p.nsplit > 1) {
     p.part_o_floats = (std::size_t)pairs * p.nsplit * p.rows * 128;
     p.bytes = (std::size_t)pairs * p.nsplit * p.rows * 130 * sizeof(float);

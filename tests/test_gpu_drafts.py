@@ -138,6 +138,9 @@ def test_paged_many_pairs():
 def test_paged_scale_and_no_lse():
     _paged(406, 2, 8, 2, 4, 16, [300, 20], lse=False, scale=0.05)
     _paged(407, 1, 8, 2, 4, 16, [300], scale=0.0)
+    _paged(409, 1, 8, 2, 4, 16, [300], scale=-0.07)
+    _paged(410, 1, 16, 2, 20, 32, [300], scale=-0.07)
+    _paged(411, 1, 16, 2, 20, 32, [45], scale=0.0)
 
 
 def test_paged_pinned_tier():
