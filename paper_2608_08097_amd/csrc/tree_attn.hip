@@ -558,11 +558,12 @@ __device__ __forceinline__ void tree_wait() {  // s_waitcnt vmcnt(N) alone
 //
 // The units of a split are listed first, up to kListUnits at a time, the ones without
 // an attended token left out: whole ones ahead, which a loop without masks takes, then
-// the others, then the tree's. K is put into LDS in MFMA operand layout, and so is
-// the working set's V. Of token-major V every load takes four tokens, their 32-byte
-// pieces in turn (token p's piece dt at 128 dt + 32 p), and the transposing read takes
-// 4 tokens x 16 dims a group of 16 lanes, 128 bytes in a row: lane (g, i) names dims
-// 4 (i % 4) .. +3 of token i / 4 and receives dim i of the four.
+// the others, then the tree's. A load takes four tokens of K or of token-major V, whole
+// rows of them, and leaves their 32-byte pieces in turn (token p's piece c at 128 c +
+// 32 p): an MFMA operand of K is a 16-byte read a lane, one of V the transposing read of
+// 4 tokens x 16 dims a group of 16 lanes, 128 bytes in a row, where lane (g, i) names
+// dims 4 (i % 4) .. +3 of token i / 4 and receives dim i of the four. The working set's
+// transposed V is put there in operand layout.
 //
 // A unit's order is: V is read, scores; the next unit's K is read; softmax, second
 // product. So LDS reads run beside the products, in the registers that these leave.
@@ -571,9 +572,11 @@ constexpr int kListUnits = 1024;
 constexpr int kListPad = 4 + 2 * kRingSteps;  // the tree's units, and none behind them
 constexpr int kRowsThreads = 512;
 constexpr int kRowPlaces = 4;  // waves of a team
-// A unit in LDS: 8 KB of K, 8 KB of V, and 128 bytes between the loads of token-major
-// V that lanes 16 g .. +15 read, so that two of these groups meet no bank twice.
-constexpr int kUnitBytes = 16 * 1024 + 512;
+// A unit in LDS: K, then V, 8 KB each and a skew after every two pieces, so that the
+// lanes of one read meet no bank twice.
+constexpr int kSkewK = 16, kSkewV = 128;
+constexpr int kUnitV = 8 * 1024 + 64;
+constexpr int kUnitBytes = kUnitV + 8 * 1024 + 4 * kSkewV;
 
 template <int NT, int BS, bool PAGED>
 __global__ __launch_bounds__(kRowsThreads) void tree_attn_rows_kernel(TreeAttnArgs a) {
@@ -613,28 +616,24 @@ __global__ __launch_bounds__(kRowsThreads) void tree_attn_rows_kernel(TreeAttnAr
     for (int dt = 0; dt < 8; ++dt) acc[v][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  // What this wave loads: of unit `half` of a step, four pieces of K (token tile
-  // j0 / 4, its four k-steps) or of V. A lane's element offset within the unit's block
-  // lo or hi, piece jj being jj * step further.
+  // What this wave loads: of unit `half` of a step, pieces j0 .. j0 + 3 of K or of V,
+  // tokens 4 j .. 4 j + 3 in piece j (of transposed V d-tile j). A lane's element
+  // offset within the unit's block lo or hi, piece jj being jj * step further.
   const int half = wave >> 2;
   const bool load_v = wave & 2;
   const int j0 = (wave & 1) * 4;
-  const int k_row = 8 * (i >> 2) + (i & 3) + j0;  // K: this lane's token of the unit
-  const int v_row = 4 * j0 + (lane >> 1 & 3);     // token-major V: of the first piece
-  const int v_col = (lane >> 3) * 16 + (lane & 1) * 8;
+  const bool by_row = PAGED || !load_v;  // token-major
   int off;
   bool hi;
-  if (!load_v) {
-    off = (BS == 16 ? k_row & 15 : k_row) * kHeadDim + g * 8;
-    hi = BS == 16 && k_row >= 16;
-  } else if (PAGED) {
-    off = (BS == 16 ? v_row & 15 : v_row) * kHeadDim + v_col;
-    hi = BS == 16 && v_row >= 16;
+  if (by_row) {
+    const int row = 4 * j0 + (lane >> 1 & 3);
+    off = (BS == 16 ? row & 15 : row) * kHeadDim + (lane >> 3) * 16 + (lane & 1) * 8;
+    hi = BS == 16 && j0 >= 4;
   } else {
     off = (j0 * 16 + i) * BS + (BS == 16 ? g & 1 : g) * 8;
     hi = BS == 16 && g >= 2;
   }
-  const int step = !load_v ? 32 : (PAGED ? 4 * kHeadDim : 16 * BS);
+  const int step = by_row ? 4 * kHeadDim : 16 * BS;
   const uint16_t* src0 = load_v ? t.vb : t.kb;
   const uint32_t ring = lds_offset(s_ring);
   const int tree_units_n = last_split ? (t.tlen + 31) / 32 : 0;
@@ -693,8 +692,8 @@ __global__ __launch_bounds__(kRowsThreads) void tree_attn_rows_kernel(TreeAttnAr
     // This wave's loads of step s, whose list entry is `raw`.
     auto issue = [&](int s, int4 raw) __attribute__((always_inline)) {
       const int4 e = uniform(raw);
-      const uint32_t dst = ring + (uint32_t)((s % kRingSteps * 2 + half) * kUnitBytes + ((load_v ? 8 : 0) + j0) * 1024);
-      const uint32_t skew = load_v && (PAGED || e.z == -1) ? 128u : 0u;  // per two loads
+      const uint32_t dst = ring + (uint32_t)((s % kRingSteps * 2 + half) * kUnitBytes + (load_v ? kUnitV : 0) + j0 * 1024);
+      const uint32_t skew = load_v ? (PAGED || e.z == -1 ? kSkewV : 0) : kSkewK;  // per two pieces
       if (e.z != -1) {
         const uint16_t* src = src0 + (long long)(hi ? e.y : e.x) * t.unit_elems + off;
 #pragma unroll
@@ -702,28 +701,31 @@ __global__ __launch_bounds__(kRowsThreads) void tree_attn_rows_kernel(TreeAttnAr
       } else {  // the tree's rows
         int ll = lane;
         asm volatile("" : "+v"(ll));  // its terms are not worth registers through the loop
-        const uint16_t* src = (load_v ? a.tree_v : a.tree_k) + t.tree_base;
+        const uint16_t* src = (load_v ? a.tree_v : a.tree_k) + t.tree_base + (ll >> 3) * 16 + (ll & 1) * 8;
 #pragma unroll
         for (int jj = 0; jj < 4; ++jj) {
-          const int row = load_v ? 4 * (j0 + jj) + (ll >> 1 & 3) : 8 * (ll >> 2 & 3) + (ll & 3) + j0;
-          const int col = load_v ? (ll >> 3) * 16 + (ll & 1) * 8 : jj * 32 + (ll >> 4) * 8;
-          tree_dma16(src + min(e.x * 32 + row, t.tlen - 1) * t.tree_row + col, dst + jj * 1024 + (j0 + jj) / 2 * skew);
+          const int row = e.x * 32 + 4 * (j0 + jj) + (ll >> 1 & 3);
+          tree_dma16(src + min(row, t.tlen - 1) * t.tree_row, dst + jj * 1024 + (j0 + jj) / 2 * skew);
         }
       }
     };
     TreeUnit u;
     auto unit_at = [&](int s) __attribute__((always_inline)) { return s_ring + (s % kRingSteps * 2 + team) * kUnitBytes; };
     auto read_k = [&](int s) __attribute__((always_inline)) {
-      const u32x4* at = reinterpret_cast<const u32x4*>(unit_at(s)) + lane;
+      // token tile tau, k-step st: token 4 (2 (i / 4) + tau) + i % 4, dims 32 st + 8 g .. +7
+      const char* at = unit_at(s) + (i >> 2) * (2048 + kSkewK) + (g >> 1) * 128 + (i & 3) * 32 + (g & 1) * 16;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) u.k[j >> 2][j & 3] = at[j * 64];
+      for (int tau = 0; tau < 2; ++tau)
+#pragma unroll
+        for (int st = 0; st < 4; ++st)
+          u.k[tau][st] = *reinterpret_cast<const u32x4*>(at + tau * 1024 + st * 256);
     };
     auto read_v = [&](int s, bool by_row) __attribute__((always_inline)) {
       if (by_row) {
         typedef short s16x4 __attribute__((ext_vector_type(4)));
         typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
         // tokens 8 g + 4 q .. +3 at load 2 g + q
-        char* at = unit_at(s) + 8192 + g * (2048 + 128) + (i >> 2) * 32 + (i & 3) * 8;
+        char* at = unit_at(s) + kUnitV + g * (2048 + kSkewV) + (i >> 2) * 32 + (i & 3) * 8;
 #pragma unroll
         for (int dt = 0; dt < 8; ++dt)
 #pragma unroll
@@ -735,7 +737,7 @@ __global__ __launch_bounds__(kRowsThreads) void tree_attn_rows_kernel(TreeAttnAr
             u.v[dt][2 * q + 1] = w[1];
           }
       } else {
-        const u32x4* at = reinterpret_cast<const u32x4*>(unit_at(s)) + 512 + lane;
+        const u32x4* at = reinterpret_cast<const u32x4*>(unit_at(s) + kUnitV) + lane;
 #pragma unroll
         for (int dt = 0; dt < 8; ++dt) u.v[dt] = at[dt * 64];
       }
