@@ -265,6 +265,60 @@ def test_offsets_past_32_bits():
     assert np.array_equal(host_bits(kp[-3:]), hk) and np.array_equal(host_bits(vp[-3:]), hv)
 
 
+@pytest.mark.parametrize("G,T", [(4, 3), (20, 2)])
+def test_paged_long_contexts_in_one_split(G, T):
+    """So many pairs that they are hardly split, or not at all, two of them with thousands of units: lists of units in
+    several pieces."""
+    R, B, NB = 1024, 32, 2205
+    ctx = np.zeros(R, np.int32)
+    ctx[[3, 700]] = 1029 * 32 + 5, NB * B - 40
+    rng, q, tk, tv, parent, n = _inputs(1100 + G, R, G, 1, T, "random", None)
+    NP = 2300
+    kp, vp = random_bf16(1101, (NP, 1, B, 128)), random_bf16(1102, (NP, 1, B, 128))
+    table = np.broadcast_to(rng.permutation(NP)[:NB], (R, NB)).astype(np.int32)
+    table[:, 1025:1031] = -1  # a hole around the end of a piece
+    d = P.dims(R, G, 1, 128, B, NB)
+    ws = torch.zeros(P.oasis_tree_attn_workspace_bytes(d, T), dtype=torch.uint8, device="cuda")
+    assert ws.numel() == 0 or G * T <= 32
+    note(f"long contexts in one split G={G} T={T}")
+    out = torch.zeros((R, T, G, 128), dtype=torch.bfloat16, device="cuda")
+    lse = torch.zeros((R, T, G), device="cuda")
+    P.oasis_tree_attn(d, dev_bf16(q), T, dev_bf16(kp), dev_bf16(vp), dev_i32(table), dev_i32(ctx), dev_bf16(tk),
+                      dev_bf16(tv), dev_i32(parent), None, None, out, lse, ws)
+    some = [0, 3, 512, 700, 1023]
+    ref, ref_lse = O.tree_attend(q[some], kp, vp, table[some], ctx[some], tk[some], tv[some], parent[some], [T] * 5, B)
+    ref_abs, _ = O.tree_attend(q[some], kp, _magnitude(vp), table[some], ctx[some], tk[some], _magnitude(tv[some]),
+                               parent[some], [T] * 5, B)
+    _check(out[some], lse[some], ref, ref_abs, ref_lse, out[some])
+
+
+def test_sparse_working_set_of_many_slots_in_one_split():
+    """As above over the working set, in blocks of 16: two slots a unit, many of them free."""
+    R, G, T, B, ks = 1024, 20, 2, 16, 2301
+    rng, q, tk, tv, parent, n = _inputs(1110, R, G, 1, T, "random", None)
+    ctx = np.zeros(R, np.int32)
+    ctx[700] = 5000 * B + 3
+    pk, pv = (random_bf16(s, (1, ks + 1, 1, B, 128)) for s in (1111, 1112))
+    smap = np.full((R, 1, ks), -1, np.int32)
+    smap[700, 0] = np.where(rng.random(ks) < 0.05, -1, 1)
+    d = P.dims(R, G, 1, 128, B, 5001)
+    assert P.oasis_sparse_tree_attn_workspace_bytes(d, T, ks) == 0
+    dk = torch.empty((R, ks + 1, 1, B, 128), dtype=torch.bfloat16, device="cuda")
+    dv = torch.empty((R, ks + 1, 1, 128, B), dtype=torch.bfloat16, device="cuda")
+    dk[700], dv[700] = dev_bf16(pk)[0], dev_bf16(pool_v_from_htd(pv))[0]
+    note("a working set of many slots in one split")
+    out = torch.zeros((R, T, G, 128), dtype=torch.bfloat16, device="cuda")
+    lse = torch.zeros((R, T, G), device="cuda")
+    P.oasis_sparse_tree_attn(d, dev_bf16(q), T, dk, dv, dev_i32(smap), ks, dev_i32(ctx), dev_bf16(tk), dev_bf16(tv),
+                             dev_i32(parent), None, None, out, lse, None)
+    for one in ([700], [5]):  # the other one: nothing cached
+        at = (smap[one], ctx[one])
+        rows = (parent[one], [T], B)
+        ref, ref_lse = O.sparse_tree_attend(q[one], pk, pv, *at, tk[one], tv[one], *rows)
+        ref_abs, _ = O.sparse_tree_attend(q[one], pk, _magnitude(pv), *at, tk[one], _magnitude(tv[one]), *rows)
+        _check(out[one], lse[one], ref, ref_abs, ref_lse, out[one])
+
+
 # -- verification --------------------------------------------------------------------
 
 
