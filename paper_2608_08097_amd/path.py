@@ -168,6 +168,7 @@ class DecodePath:
         # pages a growing step refreshes the local block from (None: the host tier)
         self.local_source = None
         self._ws_attn = None  # the attention workspace of every layer (new_layer)
+        self._spec = None     # workspace and outputs of the speculative step (_speculative)
 
     def new_layer(self) -> LayerState:
         # One attention workspace for all layers of the path: it is scratch of a
@@ -285,6 +286,64 @@ class DecodePath:
     def attend(self, st: LayerState, q: torch.Tensor, ctx_len: torch.Tensor, stream=None):
         L.oasis_sparse_decode_attn(self.dims, q, self.T, st.pool_k, st.pool_v, st.slot_map, self.k, ctx_len,
                                    self.scale, st.out, st.lse, st.ws_attn, stream)
+
+    # -- speculative step (the T rows of q are a drafted tree) ---------------------
+    def _speculative(self):
+        """Workspace, path, path_len and out_tokens, shared by the layers: their calls run in order."""
+        if self._spec is None:
+            if torch.cuda.is_current_stream_capturing():
+                raise RuntimeError("the speculative step's buffers are allocated by its first call, which must not be "
+                                   "captured")
+            d, dev = self.dims, self.block_table.device
+            need = max(L.oasis_tree_attn_workspace_bytes(d, self.T),
+                       L.oasis_sparse_tree_attn_workspace_bytes(d, self.T, self.k),
+                       L.oasis_verify_workspace_bytes(d.num_reqs, self.T, 1))  # alike for every vocabulary
+            ints = [torch.empty(s, dtype=torch.int32, device=dev)
+                    for s in ((d.num_reqs, self.T), (d.num_reqs,), (d.num_reqs, self.T))]
+            self._spec = (torch.empty(need, dtype=torch.uint8, device=dev), *ints)
+        return self._spec
+
+    def attend_tree(self, st: LayerState, q: torch.Tensor, ctx_len: torch.Tensor, tree_k: torch.Tensor,
+                    tree_v: torch.Tensor, parent: torch.Tensor | None = None, tree_len: torch.Tensor | None = None,
+                    stream=None):
+        """Attention of a drafted tree over the layer's working set, into ``st.out`` and ``st.lse``: ``attend`` with the
+        rows' own keys and values (bf16 [R][T][Hkv][d], in no cache yet) added to each row that descends from them."""
+        L.oasis_sparse_tree_attn(self.dims, q, self.T, st.pool_k, st.pool_v, st.slot_map, self.k, ctx_len, tree_k,
+                                 tree_v, parent, tree_len, self.scale, st.out, st.lse, self._speculative()[0], stream)
+
+    def attend_tree_dense(self, st: LayerState, q: torch.Tensor, ctx_len: torch.Tensor, tree_k: torch.Tensor,
+                          tree_v: torch.Tensor, parent: torch.Tensor | None = None,
+                          tree_len: torch.Tensor | None = None, pages: tuple | None = None, stream=None):
+        """The same over every cached token, for requests below the sparsification threshold (§5.2): ``pages`` are
+        (k_pages, v_pages, block_table) that hold all of them, the host tier by default."""
+        kp, vp, bt = pages if pages is not None else (self.host_k, self.host_v, self.block_table)
+        L.oasis_tree_attn(self.dims, q, self.T, kp, vp, bt, ctx_len, tree_k, tree_v, parent, tree_len, self.scale,
+                          st.out, st.lse, self._speculative()[0], stream)
+
+    def verify(self, target_probs: torch.Tensor, draft_probs: torch.Tensor | None, tokens: torch.Tensor,
+               accept_u: torch.Tensor, sample_u: torch.Tensor, parent: torch.Tensor | None = None,
+               tree_len: torch.Tensor | None = None, stream=None):
+        """(path, path_len, out_tokens) of the drafted tree, in buffers that the next call writes again."""
+        ws, path, path_len, out_tokens = self._speculative()
+        L.oasis_verify_drafts(target_probs, draft_probs, tokens, parent, tree_len, accept_u, sample_u, path, path_len,
+                              out_tokens, ws, stream)
+        return path, path_len, out_tokens
+
+    def commit(self, st: LayerState, tree_k: torch.Tensor, tree_v: torch.Tensor, path: torch.Tensor,
+               path_len: torch.Tensor, ctx_len: torch.Tensor, new_ctx_len: torch.Tensor, stream=None):
+        """Append the accepted rows' keys and values at ``ctx_len`` to the host tier (and to the local-block source),
+        write the lengths that follow, and bring the layer's compressed keys and local block up to them. Before it, no
+        step of the layer may be under way on the background streams (``join``)."""
+        L.oasis_append_tokens(self.dims, tree_k, tree_v, self.T, path, path_len, self.host_k, self.host_v,
+                              self.block_table, ctx_len, new_ctx_len, stream)
+        kp, bt = self.host_k, self.block_table
+        if self.local_source is not None:
+            kp, vp, bt = self.local_source
+            L.oasis_append_tokens(self.dims, tree_k, tree_v, self.T, path, path_len, kp, vp, bt, ctx_len, None,
+                                  stream)
+        L.oasis_update_summaries(self.dims, kp, bt, ctx_len, new_ctx_len, -(-self.T // self.dims.block_size), st.kmax,
+                                 st.kmin, stream)
+        self.refresh_local(st, new_ctx_len, stream)
 
     # -- schedules --------------------------------------------------------------
     def step_serial(self, st: LayerState, q: torch.Tensor, ctx_len: torch.Tensor, step: int):
