@@ -37,7 +37,8 @@ struct TreePlan {
 // taken. Measured against neighbouring counts (pairs, rows, units: count and us): 64, 20,
 // 4,096: 2 840, 3 708, 4 712, 5 864, 8 722; 64, 20, 65: 1 27.3, 2 22.3, 3 20.7, 4 21.2,
 // 5 25.0; 16, 512, 2,048: 3 337, 4 296, 6 404; 192, 64, up to 1,024: 1 360, 2 257, 3 267,
-// 4 234, 8 269; 128, 256, 129: 1 98, 2 116; 512, 28, 65: 1 81, 2 92.
+// 4 234, 8 269; 128, 256, 129: 1 98, 2 116; 512, 28, 65: 1 81, 2 92; 8, 8, 129: 4 17.9,
+// 8 12.7, 16 11.6, 24 12.0, 33 14.8; 1, 8, 1,001: 16 28.6, 32 21.1, 64 20.5, 128 27.6.
 inline TreePlan tree_plan(long long pairs, int G, int T, int units, bool ragged) {
   TreePlan p{};
   p.rows = G * T;
@@ -58,8 +59,10 @@ inline TreePlan tree_plan(long long pairs, int G, int T, int units, bool ragged)
     const long long share = u * 63 * at_once / (2560 * p.groups);  // 6.7 TB/s over 256 CUs
     long long body = rows_form ? u * 6 : (u + kTreeWaves - 1) / kTreeWaves * 16;
     if (body < share) body = share;
-    const long long merge = n > 1 ? 30 + pairs * n * p.rows * 1040 / 300000 : 0;  // both ways at 3 TB/s
-    return rounds * (body + (rows_form ? 110 : 70)) + merge;
+    // its launch, a wait for every few splits, the partials both ways at 3 TB/s
+    const long long merge = n > 1 ? 30 + n * 6 / 5 + pairs * n * p.rows * 1040 / 300000 : 0;
+    const long long shared = !rows_form && items * n > 256 ? 25 : 0;  // two workgroups on a CU
+    return rounds * (body + (rows_form ? 110 : 70)) + shared + merge;
   };
   long long best = estimate(1);
   p.nsplit = 1;
