@@ -5,6 +5,9 @@
 #include "drafts_internal.h"
 
 namespace oasis {
+
+constexpr float kLog2e = 1.4426950408889634f;
+
 namespace {
 
 oasis_status need(const void* p, const char* name, const char* fn) {
@@ -34,7 +37,7 @@ oasis_status check_tree(const oasis_dims* d, int32_t T, const char* fn) {
   if (rows > kTreeMaxRows)
     return fail(OASIS_ERR_UNSUPPORTED, "%s: G * num_q_tokens = %lld rows per KV head (at most %d)", fn, rows,
                 kTreeMaxRows);
-  if ((long long)d->max_blocks * d->block_size > INT32_MAX)
+  if ((long long)d->max_blocks * d->block_size > INT32_MAX - 32)  // positions are rounded up to units of 32
     return fail(OASIS_ERR_UNSUPPORTED, "%s: max_blocks * block_size past 31 bits", fn);
   return OASIS_OK;
 }
@@ -97,7 +100,7 @@ oasis_status make_tree_args(const TreeCall& c, const TreePlan& p, TreeAttnArgs* 
   t.T = c.T;
   t.B = c.dims->block_size;
   t.NBmax = c.dims->max_blocks;
-  t.scale_log2 = c.scale == 0.f ? 1.f : std::fabs(c.scale) * 1.4426950408889634f;
+  t.scale_log2 = c.scale == 0.f ? 1.f : std::fabs(c.scale) * kLog2e;
   t.q_and = c.scale == 0.f ? 0u : ~0u;
   t.q_xor = c.scale < 0.f ? 0x80008000u : 0u;
   t.rows = p.rows;
@@ -113,6 +116,7 @@ oasis_status make_tree_args(const TreeCall& c, const TreePlan& p, TreeAttnArgs* 
 
 using oasis::fail;
 using oasis::hip_status;
+using oasis::kLog2e;
 using oasis::ok;
 
 extern "C" {
@@ -131,7 +135,7 @@ oasis_status oasis_tree_attn(const oasis_dims* dims, const uint16_t* q, int32_t 
   oasis_status st = oasis::check_tree(dims, num_q_tokens, fn);
   if (st != OASIS_OK) return st;
   if (num_pages < 1 || num_pages > INT32_MAX) return fail(OASIS_ERR_INVALID_ARG, "%s: num_pages out of range", fn);
-  if (!std::isfinite(scale)) return fail(OASIS_ERR_INVALID_ARG, "%s: scale is not finite", fn);
+  if (!std::isfinite(scale * kLog2e)) return fail(OASIS_ERR_INVALID_ARG, "%s: scale is not finite", fn);
   if (dims->num_reqs == 0) return ok();
   REQUIRE_ALIGNED(k_pages, fn);
   REQUIRE_ALIGNED(v_pages, fn);
@@ -168,7 +172,7 @@ oasis_status oasis_sparse_tree_attn(const oasis_dims* dims, const uint16_t* q, i
   oasis_status st = oasis::check_tree(dims, num_q_tokens, fn);
   if (st != OASIS_OK) return st;
   if ((st = oasis::check_slots(dims, k_slots, fn)) != OASIS_OK) return st;
-  if (!std::isfinite(scale)) return fail(OASIS_ERR_INVALID_ARG, "%s: scale is not finite", fn);
+  if (!std::isfinite(scale * kLog2e)) return fail(OASIS_ERR_INVALID_ARG, "%s: scale is not finite", fn);
   if (dims->num_reqs == 0) return ok();
   REQUIRE_ALIGNED(pool_k, fn);
   REQUIRE_ALIGNED(pool_v, fn);

@@ -140,6 +140,13 @@ def test_tree_attention_refusals():
     _refused(paged(table=None), 1, "block_table is NULL")
     _refused(sparse(ks=-1), 1, "k_slots < 0")
     _refused(sparse(map=None), 1, "slot_map is NULL")
+    # positions are rounded up to whole units, and the scale multiplied by log2(e), before they are used
+    longest = P.dims(1, 32, 8, 128, 16, (1 << 27) - 1)
+    _refused(paged(dims=longest), 2, "31 bits")
+    _refused(sparse(dims=longest), 2, "31 bits")
+    for f in (paged, sparse):
+        _refused(f(scale=3e38), 1, "scale")
+    assert P.oasis_tree_attn_workspace_bytes(P.dims(1, 32, 8, 128, 16, (1 << 27) - 3), 5) > 0
     assert P.oasis_tree_attn_workspace_bytes(d, 65) == 0 == P.oasis_sparse_tree_attn_workspace_bytes(d, 5, -1)
 
 
