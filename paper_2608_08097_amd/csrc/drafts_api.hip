@@ -152,6 +152,7 @@ oasis_status oasis_tree_attn(const oasis_dims* dims, const uint16_t* q, int32_t 
   a.v = static_cast<const uint16_t*>(vp);
   a.table = block_table;
   a.num_pages = num_pages;
+  a.by_length = oasis::tree_by_length(oasis::paged_plan(dims, num_q_tokens), dims->num_reqs, dims->num_kv_heads);
   return hip_status(oasis::launch_tree_attn(a, true, static_cast<hipStream_t>(stream)), fn);
 }
 

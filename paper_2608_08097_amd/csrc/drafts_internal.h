@@ -26,6 +26,7 @@ struct TreeAttnArgs {
   float scale_log2;          // |scale| * log2(e), 1 for a scale of 0
   uint32_t q_and, q_xor;     // what makes up for that in the queries' bits
   int rows, tiles, groups, nsplit;
+  int by_length;             // pages: the requests by length (tree_by_length)
 };
 hipError_t launch_tree_attn(const TreeAttnArgs& a, bool paged, hipStream_t s);
 

@@ -39,6 +39,29 @@ __device__ __forceinline__ int tree_item(int wg, int items) {
   return (wg >> 3) < ((items + 7) >> 3) && item < items ? item : -1;
 }
 
+// The same where the requests are taken by length (tree_by_length): the n-th of `count`
+// runs of keys and values goes to XCD n % 8, its row groups one after the other there.
+__device__ __forceinline__ int tree_item_spread(int wg, int groups, int count, int& group) {
+  const int n = wg >> 3;
+  const int item = n / groups * 8 + (wg & 7);
+  group = n - n / groups * groups;
+  return item < count ? item : -1;
+}
+// The request of rank k by length, and in `len` its length: the longest first, equal ones
+// in order. At most 64 of them, one a lane.
+__device__ __forceinline__ int request_of_rank(const int32_t* ctx_len, int R, int k, int& len) {
+  const int lane = threadIdx.x & 63;
+  const int mine = lane < R ? ctx_len[lane] : INT32_MIN;
+  int rank = lane < R ? 0 : R;
+  for (int r = 0; r < R; ++r) {
+    const int other = __builtin_amdgcn_readlane(mine, r);
+    rank += other > mine || (other == mine && r < lane);
+  }
+  const int at = __builtin_ctzll(__builtin_amdgcn_ballot_w64(rank == k));
+  len = __builtin_amdgcn_readlane(mine, at);
+  return at;
+}
+
 struct TreeUnit {
   u32x4 k[2][4];
   u32x4 v[8];
@@ -217,14 +240,27 @@ struct TreeItem {
 };
 template <int BS, bool PAGED>
 __device__ __forceinline__ bool tree_setup(const TreeAttnArgs& a, int group_rows, TreeItem& t) {
-  const int item = tree_item(blockIdx.x, a.R * a.Hkv * a.nsplit * a.groups);
-  if (item < 0) return false;
-  const int rs = item / a.groups;
-  t.row0 = (item - rs * a.groups) * group_rows;
+  int group, rs;
+  if (PAGED && a.by_length) {
+    rs = tree_item_spread(blockIdx.x, a.groups, a.R * a.Hkv * a.nsplit, group);
+    if (rs < 0) return false;
+  } else {
+    const int item = tree_item(blockIdx.x, a.R * a.Hkv * a.nsplit * a.groups);
+    if (item < 0) return false;
+    rs = item / a.groups;
+    group = item - rs * a.groups;
+  }
+  t.row0 = group * group_rows;
   t.rh = rs / a.nsplit;
   t.split = rs - t.rh * a.nsplit;
   t.r = t.rh / a.Hkv;
   t.h = t.rh - t.r * a.Hkv;
+  if (PAGED && a.by_length) {
+    t.r = request_of_rank(a.ctx_len, a.R, t.r, t.ctx);
+    t.rh = t.r * a.Hkv + t.h;
+  } else {
+    t.ctx = a.ctx_len[t.r];  // read beside the tree's length
+  }
   t.unit_elems = (long long)a.Hkv * BS * kHeadDim;
   const long long base = (PAGED ? 0 : (long long)t.r * (a.k_slots + 1) * t.unit_elems) + (long long)t.h * BS * kHeadDim;
   t.kb = a.k + base;
@@ -232,7 +268,6 @@ __device__ __forceinline__ bool tree_setup(const TreeAttnArgs& a, int group_rows
   t.tab = a.table + (PAGED ? (long long)t.r * a.NBmax : (long long)t.rh * a.k_slots);
   t.tree_row = (long long)a.Hkv * kHeadDim;
   t.tree_base = (long long)t.r * a.T * t.tree_row + (long long)t.h * kHeadDim;
-  t.ctx = a.ctx_len[t.r];  // read beside the tree's length
   t.tlen = tree_length(a, t.r);
   return t.row0 < t.tlen * a.G;  // else no row of this group is in the tree
 }
@@ -528,17 +563,29 @@ __global__ __launch_bounds__(kTW * 64) void tree_attn_kernel(TreeAttnArgs a) {
 // offset lds + 16 L, lds being the same in every lane. In assembly for the reason
 // given at the working set's attention (lds_dma16): the compiler would drain every
 // earlier load before each one; the waits are the kernel's own counts instead.
+template <bool STREAM>
 __device__ __forceinline__ void tree_dma16(const void* src, uint32_t lds) {
   uint32_t saved;
-  asm volatile(
-      "s_mov_b32 %0, m0\n\t"
-      "s_mov_b32 m0, %2\n\t"
-      "s_nop 0\n\t"
-      "global_load_lds_dwordx4 %1, off\n\t"
-      "s_mov_b32 m0, %0"
-      : "=&s"(saved)
-      : "v"(src), "s"(lds)
-      : "memory");
+  if constexpr (STREAM)
+    asm volatile(
+        "s_mov_b32 %0, m0\n\t"
+        "s_mov_b32 m0, %2\n\t"
+        "s_nop 0\n\t"
+        "global_load_lds_dwordx4 %1, off nt\n\t"
+        "s_mov_b32 m0, %0"
+        : "=&s"(saved)
+        : "v"(src), "s"(lds)
+        : "memory");
+  else
+    asm volatile(
+        "s_mov_b32 %0, m0\n\t"
+        "s_mov_b32 m0, %2\n\t"
+        "s_nop 0\n\t"
+        "global_load_lds_dwordx4 %1, off\n\t"
+        "s_mov_b32 m0, %0"
+        : "=&s"(saved)
+        : "v"(src), "s"(lds)
+        : "memory");
 }
 __device__ __forceinline__ uint32_t lds_offset(const void* p) {
   return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
@@ -578,7 +625,7 @@ constexpr int kSkewK = 16, kSkewV = 128;
 constexpr int kUnitV = 8 * 1024 + 64;
 constexpr int kUnitBytes = kUnitV + 8 * 1024 + 4 * kSkewV;
 
-template <int NT, int BS, bool PAGED>
+template <int NT, int BS, bool PAGED, bool STREAM>
 __global__ __launch_bounds__(kRowsThreads) void tree_attn_rows_kernel(TreeAttnArgs a) {
   constexpr int kRows = NT * kRowPlaces * 16;
   constexpr int kPad = kHeadDim + 4;
@@ -697,7 +744,7 @@ __global__ __launch_bounds__(kRowsThreads) void tree_attn_rows_kernel(TreeAttnAr
       if (e.z != -1) {
         const uint16_t* src = src0 + (long long)(hi ? e.y : e.x) * t.unit_elems + off;
 #pragma unroll
-        for (int jj = 0; jj < 4; ++jj) tree_dma16(src + jj * step, dst + jj * 1024 + (j0 + jj) / 2 * skew);
+        for (int jj = 0; jj < 4; ++jj) tree_dma16<STREAM>(src + jj * step, dst + jj * 1024 + (j0 + jj) / 2 * skew);
       } else {  // the tree's rows
         int ll = lane;
         asm volatile("" : "+v"(ll));  // its terms are not worth registers through the loop
@@ -705,7 +752,7 @@ __global__ __launch_bounds__(kRowsThreads) void tree_attn_rows_kernel(TreeAttnAr
 #pragma unroll
         for (int jj = 0; jj < 4; ++jj) {
           const int row = e.x * 32 + 4 * (j0 + jj) + (ll >> 1 & 3);
-          tree_dma16(src + min(row, t.tlen - 1) * t.tree_row, dst + jj * 1024 + (j0 + jj) / 2 * skew);
+          tree_dma16<false>(src + min(row, t.tlen - 1) * t.tree_row, dst + jj * 1024 + (j0 + jj) / 2 * skew);
         }
       }
     };
@@ -915,8 +962,8 @@ __global__ __launch_bounds__(kTreeMergeRows * 32) void tree_merge_kernel(TreeAtt
 
 template <int BS, bool PAGED>
 void launch_bs(const TreeAttnArgs& a, hipStream_t s) {
-  const long long items = (long long)a.R * a.Hkv * a.nsplit * a.groups;
-  const dim3 grid((unsigned)((items + 7) / 8 * 8));
+  const long long runs = (long long)a.R * a.Hkv * a.nsplit;  // of keys and values
+  const dim3 grid((unsigned)(a.by_length ? (runs + 7) / 8 * 8 * a.groups : (runs * a.groups + 7) / 8 * 8));
   // What the tables and pools hold at most: past kStreamBytes V, whose loads take whole
   // lines, is read past the caches (8 x 131,072 tokens, 4.3 GB, 711 and 640 us; 64 x
   // 2,064, 541 MB, half of it attended, 80.8 and 76.5; 68 MB, in the Infinity Cache, 21.2
@@ -930,9 +977,10 @@ void launch_bs(const TreeAttnArgs& a, hipStream_t s) {
     hipLaunchKernelGGL((stream ? tree_attn_kernel<2, BS, PAGED, true> : tree_attn_kernel<2, BS, PAGED, false>), grid,
                        dim3(kTW * 64), 0, s, a);
   else if (a.tiles <= kRowPlaces)
-    hipLaunchKernelGGL((tree_attn_rows_kernel<1, BS, PAGED>), grid, dim3(kRowsThreads), 0, s, a);
+    hipLaunchKernelGGL((stream ? tree_attn_rows_kernel<1, BS, PAGED, true> : tree_attn_rows_kernel<1, BS, PAGED, false>),
+                       grid, dim3(kRowsThreads), 0, s, a);
   else
-    hipLaunchKernelGGL((tree_attn_rows_kernel<2, BS, PAGED>), grid, dim3(kRowsThreads), 0, s, a);
+    hipLaunchKernelGGL((tree_attn_rows_kernel<2, BS, PAGED, false>), grid, dim3(kRowsThreads), 0, s, a);
 }
 
 }  // namespace

@@ -25,6 +25,10 @@ struct TreePlan {
   std::size_t part_o_floats, bytes;
 };
 
+inline long long tree_slots(const TreePlan& p) {  // workgroups that the CUs hold at once
+  return p.tiles > kTreeRegisterTiles ? 256 : 512;
+}
+
 // `units`: 32-token units of the longest context the caller's tables hold; `ragged`:
 // the contexts may be shorter than that.
 //
@@ -36,8 +40,8 @@ struct TreePlan {
 // the longest workgroup ends the call, so the most splits within 3 % of the least are
 // taken. Measured against neighbouring counts (pairs, rows, units: count and us): 64, 20,
 // 4,096: 2 840, 3 708, 4 712, 5 864, 8 722; 64, 20, 65: 1 27.3, 2 22.3, 3 20.7, 4 21.2,
-// 5 25.0; 16, 512, 2,048: 3 337, 4 296, 6 404; 192, 64, up to 1,024: 1 360, 2 257, 3 267,
-// 4 234, 8 269; 128, 256, 129: 1 98, 2 116; 512, 28, 65: 1 81, 2 92; 8, 8, 129: 4 17.9,
+// 5 25.0; 16, 512, 2,048: 3 337, 4 296, 6 404; 192, 64, up to 1,024: 1 372, 2 276, 3 276,
+// 4 269, 6 290; 128, 256, 129: 1 98, 2 116; 512, 28, 65: 1 81, 2 92; 8, 8, 129: 4 17.9,
 // 8 12.7, 16 11.6, 24 12.0, 33 14.8; 1, 8, 1,001: 16 28.6, 32 21.1, 64 20.5, 128 27.6.
 inline TreePlan tree_plan(long long pairs, int G, int T, int units, bool ragged) {
   TreePlan p{};
@@ -48,7 +52,7 @@ inline TreePlan tree_plan(long long pairs, int G, int T, int units, bool ragged)
   p.units = units;
   const long long items = pairs * p.groups;
   const bool rows_form = p.tiles > kTreeRegisterTiles;
-  const long long slots = rows_form ? 256 : 512;  // workgroups that the CUs hold at once
+  const long long slots = tree_slots(p);
   long long most = (units + kTreeWaves - 1) / kTreeWaves;  // a unit a wave
   if (most > kTreeMaxSplits) most = kTreeMaxSplits;
   if (items > 0 && most > 4 * slots / items) most = 4 * slots / items;
@@ -81,6 +85,14 @@ inline TreePlan tree_plan(long long pairs, int G, int T, int units, bool ragged)
     p.bytes = (std::size_t)pairs * p.nsplit * p.rows * 130 * sizeof(float);
   }
   return p;
+}
+
+// Whether a paged call takes its requests by length, the longest first: a call of more
+// workgroups than the CUs hold at once ends with the last ones it starts, so these had
+// better be short. Up to 64 requests, one a lane. Measured, 64 rows, 24 requests of 1 to
+// 32,768 tokens each, six draws: 311 us in order, 278 by length.
+inline bool tree_by_length(const TreePlan& p, long long R, long long Hkv) {
+  return R > 1 && R <= 64 && R * Hkv * p.nsplit * p.groups > tree_slots(p);
 }
 
 }  // namespace oasis
