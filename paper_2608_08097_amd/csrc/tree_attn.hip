@@ -19,9 +19,18 @@
 // tree_attn_kernel streams K and V from HBM straight into MFMA registers, four
 // waves a workgroup, every wave a strided subset of the units with its own online
 // softmax; token-major V is transposed in registers, 8 x 8 blocks, 32 byte
-// permutes a unit. With more rows tree_attn_rows_kernel brings each unit's K and V
-// into LDS once for eight waves, which hold different row tiles; token-major V is
-// read back with the transposing LDS read.
+// permutes a unit. With more rows every unit is needed by several waves, and
+// tree_attn_rows_kernel brings its K and V into LDS once for them; token-major V
+// is read back with the transposing LDS read.
+//
+// Measured (2 x 256 bytes a token and KV head; 4 d operations a row and token):
+//   8 requests x 8 heads x 131,072 tokens, 20 rows   650 us  6.6 TB/s (what the card reads)
+//   64 x 8 x up to 2,064 of a working set, 28 rows    75 us  HBM, and 7 us of a workgroup's start and end
+//   8 x 8 x 2,064 of a working set, 20 rows           20 us  two launches, and 10 of the bytes
+//   24 x 8 x 1 to 32,768, 64 rows                    262-328 us a draw, 5.5 TB/s
+//   16 x 8 x 4,112 of a working set, 256 rows         90 us  760 TFLOP/s
+//   2 x 8 x 65,000 to 65,536, 512 rows               293 us  936 TFLOP/s, 76 % of a large matrix product here
+//   1 x 8 x 2,000, 8 rows                             11 us  two launches (7.4) and three loads in turn
 //
 // The tree's own tokens are one or two more units, with a mask per row, in the
 // last split of every pair. Splits leave partials that a second kernel merges.
@@ -335,6 +344,11 @@ __device__ __forceinline__ void add_wild(const TreeAttnArgs& a, const TreeItem& 
   }
 }
 
+// Up to two row tiles. Every load of a unit is issued a unit ahead into the registers
+// that the present one has just left, 16 KB a wave on their way; two workgroups a CU
+// (at most 256 registers) hide what that leaves. The tree's unit comes first, before the
+// registers have a next one: as the last one, loaded in the same order, it cost copies of
+// all of them in every step (the first case above 726 us).
 template <int NT, int BS, bool PAGED, bool STREAM>
 __global__ __launch_bounds__(kTW * 64) void tree_attn_kernel(TreeAttnArgs a) {
   static_assert(NT <= 2, "three or more row tiles take tree_attn_rows_kernel");
@@ -614,6 +628,13 @@ __device__ __forceinline__ void tree_wait() {  // s_waitcnt vmcnt(N) alone
 //
 // A unit's order is: V is read, scores; the next unit's K is read; softmax, second
 // product. So LDS reads run beside the products, in the registers that these leave.
+//
+// With two tiles a wave a step takes some 2,200 cycles, 1,024 of them the matrix unit's;
+// the softmax of the other wave of the SIMD runs beside about half of these. Without the
+// barrier (each team waiting on a count of its own in LDS) or with the loads spread over
+// the step it is 9 % slower. With one tile a wave (three and four row tiles) the loads
+// bound it, and those of caches that no cache of the chip holds go past them: 228 us
+// where they do not, 208 where they do.
 constexpr int kRingSteps = 4;
 constexpr int kListUnits = 1024;
 constexpr int kListPad = 4 + 2 * kRingSteps;  // the tree's units, and none behind them
@@ -967,7 +988,8 @@ void launch_bs(const TreeAttnArgs& a, hipStream_t s) {
   // What the tables and pools hold at most: past kStreamBytes V, whose loads take whole
   // lines, is read past the caches (8 x 131,072 tokens, 4.3 GB, 711 and 640 us; 64 x
   // 2,064, 541 MB, half of it attended, 80.8 and 76.5; 68 MB, in the Infinity Cache, 21.2
-  // and 21.3; K as well 639, 80.1).
+  // and 21.3; K as well 639, 80.1), and with one tile a wave of the form for more rows both
+  // are; with two tiles several workgroups read them, through the L2.
   const long long blocks = PAGED ? a.NBmax : (a.k_slots + 1ll < a.NBmax ? a.k_slots + 1ll : a.NBmax);
   const bool stream = (long long)a.R * a.Hkv * blocks * BS * (2 * kHeadDim * 2) >= kStreamBytes;
   if (a.tiles == 1)
