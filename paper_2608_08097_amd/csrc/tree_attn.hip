@@ -437,8 +437,9 @@ __global__ __launch_bounds__(kTW * 64) void tree_attn_kernel(TreeAttnArgs a) {
   __shared__ int s_wild[kTW];
   __shared__ __align__(16) float s_o[kTW][kRows][kPad];
 
-  // ---- the tree's own tokens: unit tu of them to wave tu of the last split ----
-  const int tu = wave;
+  // ---- the tree's own tokens, unit tu of them in the last split: to the last waves,
+  // which have a unit less of the cache than the first where they have not as many
+  const int tu = kTW - 1 - wave;
   const bool tree = t.split == a.nsplit - 1 && tu * 32 < t.tlen;
   int wild = 0;
   if (tree) {
@@ -454,7 +455,7 @@ __global__ __launch_bounds__(kTW * 64) void tree_attn_kernel(TreeAttnArgs a) {
       u.v[e] = ldg16(a.tree_v + t.tree_base + j * t.tree_row + i * 8);
     }
     const uint64_t anc = ancestors(tree_parent(a, t.r, t.tlen, lane), t.tlen, lane);
-    if (wave == 0) s_anc[lane] = anc;
+    if (tu == 0) s_anc[lane] = anc;
     transpose8(u.v);
     const int n = t.tlen - tu * 32 - 8 * g;
     clear_tokens(u.v, n < 0 ? 0 : (n > 8 ? 8 : n));
@@ -563,7 +564,7 @@ __global__ __launch_bounds__(kTW * 64) void tree_attn_kernel(TreeAttnArgs a) {
     f32x4 o = *reinterpret_cast<const f32x4*>(&s_o[0][row][c4 * 4]);
 #pragma unroll
     for (int w = 1; w < kTW; ++w) o += *reinterpret_cast<const f32x4*>(&s_o[w][row][c4 * 4]);
-    if (s_wild[0] | s_wild[1]) add_wild(a, t, s_anc[(t.row0 + row) / a.G], c4, o);
+    if (s_wild[kTW - 1] | s_wild[kTW - 2]) add_wild(a, t, s_anc[(t.row0 + row) / a.G], c4, o);
     if (a.nsplit == 1) {
       write_row(a, t.r, t.h, t.row0 + row, c4, o, s_ml[0][row], s_ml[1][row]);
     } else {
