@@ -643,8 +643,8 @@ constexpr int kRowsThreads = 512;
 constexpr int kRowPlaces = 4;  // waves of a team
 // A unit in LDS: K, then V, 8 KB each and a skew after every two pieces, so that the
 // lanes of one read meet no bank twice.
-constexpr int kSkewK = 16, kSkewV = 128;
-constexpr int kUnitV = 8 * 1024 + 64;
+constexpr int kSkewK = 128, kSkewV = 128;
+constexpr int kUnitV = 8 * 1024 + 4 * kSkewK;
 constexpr int kUnitBytes = kUnitV + 8 * 1024 + 4 * kSkewV;
 
 template <int NT, int BS, bool PAGED, bool STREAM>
@@ -840,8 +840,9 @@ __global__ __launch_bounds__(kRowsThreads) void tree_attn_rows_kernel(TreeAttnAr
       // cycles: each team's go out at another time, the list entry read ahead)
       const int4 ahead = entry_read((s + 3) * 2 + half);
       if (team == 0) {
-        if (s > 0) attend();
         issue(s + 3, ahead);
+        __builtin_amdgcn_sched_barrier(0);
+        if (s > 0) attend();
       }
       read_v(s, PAGED);
 #pragma unroll
@@ -873,8 +874,9 @@ __global__ __launch_bounds__(kRowsThreads) void tree_attn_rows_kernel(TreeAttnAr
         }
       }
       if (team == 1) {
-        attend();
         issue(s + 3, ahead);
+        __builtin_amdgcn_sched_barrier(0);
+        attend();
       }
       leave();
     }
