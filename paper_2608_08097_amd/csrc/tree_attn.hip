@@ -27,9 +27,9 @@
 //   8 requests x 8 heads x 131,072 tokens, 20 rows   650 us  6.6 TB/s (what the card reads)
 //   64 x 8 x up to 2,064 of a working set, 28 rows    75 us  HBM, and 7 us of a workgroup's start and end
 //   8 x 8 x 2,064 of a working set, 20 rows           20 us  two launches, and 10 of the bytes
-//   24 x 8 x 1 to 32,768, 64 rows                    262-328 us a draw, 5.5 TB/s
-//   16 x 8 x 4,112 of a working set, 256 rows         90 us  760 TFLOP/s
-//   2 x 8 x 65,000 to 65,536, 512 rows               293 us  936 TFLOP/s, 76 % of a large matrix product here
+//   24 x 8 x 1 to 32,768, 64 rows                    213-328 us a draw, 5.5 TB/s
+//   16 x 8 x 4,128 of a working set, 256 rows         86 us  810 TFLOP/s
+//   2 x 8 x 65,000 to 65,536, 512 rows               289 us  950 TFLOP/s, 77 % of a large matrix product here
 //   1 x 8 x 2,000, 8 rows                             11 us  two launches (7.4) and three loads in turn
 //
 // The tree's own tokens are one or two more units, with a mask per row, in the

@@ -145,6 +145,11 @@ def test_paged_more_workgroups_than_the_chip_holds(R, Hkv, G, T, hi):
     _paged(1200 + R, R, Hkv * G, Hkv, T, 16, list(ctx), lens=list(rng.integers(0, T + 1, R)))
 
 
+def test_paged_largest_rows_and_most_pairs():
+    _paged(1300, 1, 64, 1, 64, 16, [100], "random", [63])
+    _paged(1301, 2000, 8, 8, 1, 16, list(np.random.default_rng(3).integers(0, 18, 2000)))
+
+
 def test_paged_scale_and_no_lse():
     _paged(406, 2, 8, 2, 4, 16, [300, 20], lse=False, scale=0.05)
     _paged(407, 1, 8, 2, 4, 16, [300], scale=0.0)
@@ -419,6 +424,17 @@ def test_verification_of_many_requests():
     _assert_verified(_verify_case(1300, 300, 4, 5000, "beam", False))
 
 
+@pytest.mark.parametrize("certain", [False, True])
+@pytest.mark.parametrize("R,T", [(2, 6), (129, 2)])
+def test_verification_long_vocabulary(R, T, certain):
+    """Rows past 256 blocks of 1,024 entries, with several workgroups a request and with one."""
+    _assert_verified(_verify_case(2500 + R, R, T, 300_001, "random", certain, pad=3))
+
+
+def test_verification_of_thousands():
+    _assert_verified(_verify_case(2600, 3000, 1, 7, "chain", True, lens=[r % 2 for r in range(3000)]))
+
+
 def test_verification_borders():
     """Probabilities in powers of two and random numbers on the borders between tokens: sums are exact in any order."""
     R, T, V = 40, 3, 8192
@@ -607,6 +623,37 @@ def test_another_stream_and_two_calls_at_once():
     for m in ms:
         for a, b in zip(want, (m.dk, m.dv, *m.ints)):
             assert torch.equal(a, b)
+
+
+def test_a_stream_given_and_a_row_taken_twice():
+    """The stream argument, and an append that names a row twice."""
+    m = _Loop()
+    s, side = m.dev[0], torch.cuda.Stream()
+    for fast in (P._lib._fast, None):
+        keep, P._lib._fast = P._lib._fast, fast
+        try:
+            m.reset()
+            torch.cuda.synchronize()
+            note("calls on a given stream")
+            P.oasis_tree_attn(m.d, s["q"], m.T, m.dk, m.dv, m.dtable, m.ctx[0], s["k"], s["v"], m.dparent, None, None, m.out,
+                              None, m.ws, side)
+            path = torch.zeros((m.R, m.T), dtype=torch.int32, device="cuda")
+            path[:, 0] = 1
+            torch.cuda.synchronize()
+            n = torch.full((m.R,), 3, dtype=torch.int32, device="cuda")
+            torch.cuda.synchronize()
+            P.oasis_append_tokens(m.d, s["k"], s["v"], m.T, path, n, m.dk, m.dv, m.dtable, m.ctx[0], m.ctx[1], side)
+            side.synchronize()
+        finally:
+            P._lib._fast = keep
+        h = m.steps[0]
+        ref, ref_lse = O.tree_attend(h["q"], m.kp, m.vp, m.table, m.ctx0, h["k"], h["v"], m.parent, [m.T] * m.R, m.B)
+        ref_abs, _ = O.tree_attend(h["q"], m.kp, _magnitude(m.vp), m.table, m.ctx0, h["k"], _magnitude(h["v"]), m.parent,
+                                   [m.T] * m.R, m.B)
+        _check(m.out, None, ref, ref_abs, ref_lse, m.out)
+        kp, vp = m.kp.copy(), m.vp.copy()
+        O.append_tokens(h["k"], h["v"], path.cpu().numpy(), n.cpu().numpy(), kp, vp, m.table, m.ctx0, m.B)
+        assert np.array_equal(host_bits(m.dk), kp) and np.array_equal(host_bits(m.dv), vp)
 
 
 def test_binding_checks_on_the_device():
