@@ -140,10 +140,11 @@ oasis_status oasis_tree_attn(const oasis_dims* dims, const uint16_t* q, int32_t 
   REQUIRE_ALIGNED(k_pages, fn);
   REQUIRE_ALIGNED(v_pages, fn);
   REQUIRE_PTR(block_table, fn);
+  const oasis::TreePlan plan = oasis::paged_plan(dims, num_q_tokens);
   oasis::TreeAttnArgs a{};
   st = oasis::make_tree_args({dims, q, num_q_tokens, tree_k, tree_v, parent, tree_len, ctx_len, scale, out, lse,
                               workspace, workspace_bytes},
-                             oasis::paged_plan(dims, num_q_tokens), &a, fn);
+                             plan, &a, fn);
   if (st != OASIS_OK) return st;
   const void *kp = nullptr, *vp = nullptr;
   if ((st = oasis::device_view(k_pages, &kp, "k_pages", fn)) != OASIS_OK) return st;
@@ -152,7 +153,7 @@ oasis_status oasis_tree_attn(const oasis_dims* dims, const uint16_t* q, int32_t 
   a.v = static_cast<const uint16_t*>(vp);
   a.table = block_table;
   a.num_pages = num_pages;
-  a.by_length = oasis::tree_by_length(oasis::paged_plan(dims, num_q_tokens), dims->num_reqs, dims->num_kv_heads);
+  a.by_length = oasis::tree_by_length(plan, dims->num_reqs, dims->num_kv_heads);
   return hip_status(oasis::launch_tree_attn(a, true, static_cast<hipStream_t>(stream)), fn);
 }
 

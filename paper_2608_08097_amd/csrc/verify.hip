@@ -17,11 +17,13 @@
 // The acceptance tests need scalars only, read at once, a child per lane; every
 // wave walks by itself. What costs is reading rows of the vocabulary: one for the
 // next token, and with draft probabilities one for each rejected child that has a
-// sibling behind it. A CU reads some 120 GB/s of them, near the 64 bytes a cycle that it
-// can load (finer pieces for an even share of the waves: no gain), so a long row is shared by several workgroups and a
-// second launch (verify_groups). Measured, one request, chain, 131,072 entries with
-// draft probabilities (1 MB): 15.6 us with one workgroup, 8.3 with eight; 32,000
-// entries 8.9 and 7.0; 128 requests of 131,072 36 and, with two, 31.
+// sibling behind it. A CU reads some 120 GB/s of them, near the 64 bytes a cycle that
+// it can load (finer pieces, for an even share of the waves: no gain), so a long row is
+// shared by several workgroups and a second launch (verify_groups). Measured, one
+// request, chain, 131,072 entries with draft probabilities (1 MB): 15.6 us with one
+// workgroup, 8.3 with eight; 32,000 entries 8.9 and 7.0; 128 requests of 131,072 36 and,
+// with two, 31; 48 requests, 16 rows, 50,261 entries 25.3, the passes of rejected
+// siblings one after the other.
 #include "drafts_internal.h"
 
 namespace oasis {
