@@ -21,22 +21,23 @@ __global__ __launch_bounds__(kAT) void append_kernel(AppendArgs a) {
   n = n < 0 ? 0 : (n > a.T ? a.T : n);
   if (n > cap - ctx) n = (int)(cap - ctx);
   if (blockIdx.x == 0 && threadIdx.x == 0 && a.new_ctx_len) a.new_ctx_len[r] = (int)(ctx + n);
-  const int chunks = a.Hkv * (kHeadDim / 8);  // 16-byte pieces of a token
-  const long long at = (long long)blockIdx.x * kAT + threadIdx.x;
-  const int i = (int)(at / (2 * chunks));
+  constexpr int kPieces = kHeadDim / 8;  // of 16 bytes
+  const uint32_t at = blockIdx.x * kAT + threadIdx.x;  // below 2^31 (the entry point)
+  const uint32_t entry = at / kPieces;                 // K of every head of a token, then V
+  const int i = a.by_hkv(entry >> 1);
   if (i >= n) return;
-  int c = (int)(at - (long long)i * 2 * chunks);
-  const bool is_v = c >= chunks;
-  if (is_v) c -= chunks;
+  int h = (int)entry - 2 * i * a.Hkv;
+  const bool is_v = h >= a.Hkv;
+  if (is_v) h -= a.Hkv;
   const int row = a.path ? a.path[(long long)r * a.T + i] : i;
   if (row < 0 || row >= a.T) return;
   const long long pos = ctx + i;
-  const int page = a.table[(long long)r * a.NBmax + pos / a.B];
+  const int shift = a.B == 16 ? 4 : 5;
+  const int page = a.table[(long long)r * a.NBmax + (pos >> shift)];
   if (page < 0 || page >= a.num_pages) return;
-  const int h = c / (kHeadDim / 8);
-  const int piece = c % (kHeadDim / 8) * 8;
+  const int piece = at % kPieces * 8;
   const uint16_t* src = (is_v ? a.new_v : a.new_k) + (((long long)r * a.T + row) * a.Hkv + h) * kHeadDim + piece;
-  uint16_t* dst = (is_v ? a.v : a.k) + (((long long)page * a.Hkv + h) * a.B + pos % a.B) * kHeadDim + piece;
+  uint16_t* dst = (is_v ? a.v : a.k) + (((long long)page * a.Hkv + h) * a.B + (pos & (a.B - 1))) * kHeadDim + piece;
   *reinterpret_cast<u32x4*>(dst) = ldg16(src);
 }
 

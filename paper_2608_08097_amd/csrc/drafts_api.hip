@@ -107,6 +107,10 @@ oasis_status make_tree_args(const TreeCall& c, const TreePlan& p, TreeAttnArgs* 
   t.tiles = p.tiles;
   t.groups = p.groups;
   t.nsplit = p.nsplit;
+  t.by_groups = fast_div(p.groups);
+  t.by_nsplit = fast_div(p.nsplit);
+  t.by_hkv = fast_div(t.Hkv);
+  t.by_g = fast_div(t.G);
   *a = t;
   return OASIS_OK;
 }
@@ -272,7 +276,8 @@ oasis_status oasis_append_tokens(const oasis_dims* dims, const uint16_t* new_k, 
   if ((st = oasis::device_view(v_pages, &vp, "v_pages", fn)) != OASIS_OK) return st;
   const oasis::AppendArgs a{new_k, new_v, path, path_len, static_cast<uint16_t*>(const_cast<void*>(kp)),
                             static_cast<uint16_t*>(const_cast<void*>(vp)), num_pages, block_table, ctx_len, new_ctx_len,
-                            dims->num_reqs, dims->num_kv_heads, num_tokens, dims->block_size, dims->max_blocks};
+                            dims->num_reqs, dims->num_kv_heads, num_tokens, dims->block_size, dims->max_blocks,
+                            oasis::fast_div(dims->num_kv_heads)};
   return hip_status(oasis::launch_append(a, static_cast<hipStream_t>(stream)), fn);
 }
 

@@ -27,6 +27,7 @@ struct TreeAttnArgs {
   uint32_t q_and, q_xor;     // what makes up for that in the queries' bits
   int rows, tiles, groups, nsplit;
   int by_length;             // pages: the requests by length (tree_by_length)
+  FastDiv by_groups, by_nsplit, by_hkv, by_g;
 };
 hipError_t launch_tree_attn(const TreeAttnArgs& a, bool paged, hipStream_t s);
 
@@ -81,6 +82,7 @@ struct AppendArgs {
   const int32_t* ctx_len;
   int32_t* new_ctx_len;      // nullable
   int R, Hkv, T, B, NBmax;
+  FastDiv by_hkv;
 };
 hipError_t launch_append(const AppendArgs& a, hipStream_t s);
 

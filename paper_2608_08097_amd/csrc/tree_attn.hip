@@ -29,8 +29,8 @@
 //   8 x 8 x 2,064 of a working set, 20 rows           20 us  two launches, and 10 of the bytes
 //   24 x 8 x 1 to 32,768, 64 rows                    213-328 us a draw, 5.5 TB/s
 //   16 x 8 x 4,128 of a working set, 256 rows         86 us  810 TFLOP/s
-//   2 x 8 x 65,000 to 65,536, 512 rows               289 us  950 TFLOP/s, 77 % of a large matrix product here
-//   1 x 8 x 2,000, 8 rows                             11 us  two launches (7.4) and three loads in turn
+//   2 x 8 x 65,000 to 65,536, 512 rows               280 us  980 TFLOP/s, 80 % of a large matrix product here
+//   1 x 8 x 2,000, 8 rows                            9.6 us  two launches (7.4) and three loads in turn
 //
 // The tree's own tokens are one or two more units, with a mask per row, in the
 // last split of every pair. Splits leave partials that a second kernel merges.
@@ -50,10 +50,10 @@ __device__ __forceinline__ int tree_item(int wg, int items) {
 
 // The same where the requests are taken by length (tree_by_length): the n-th of `count`
 // runs of keys and values goes to XCD n % 8, its row groups one after the other there.
-__device__ __forceinline__ int tree_item_spread(int wg, int groups, int count, int& group) {
-  const int n = wg >> 3;
-  const int item = n / groups * 8 + (wg & 7);
-  group = n - n / groups * groups;
+__device__ __forceinline__ int tree_item_spread(int wg, const TreeAttnArgs& a, int count, int& group) {
+  const int n = wg >> 3, run = a.by_groups(n);
+  const int item = run * 8 + (wg & 7);
+  group = n - run * a.groups;
   return item < count ? item : -1;
 }
 // The request of rank k by length, and in `len` its length: the longest first, equal ones
@@ -220,7 +220,7 @@ __device__ __forceinline__ uint64_t ancestors(int up, int len, int lane) {
 
 // Normalised bf16 output of 4 dims of one row, and its log-sum-exp.
 __device__ __forceinline__ void write_row(const TreeAttnArgs& a, int r, int h, int row, int c4, f32x4 o, float M, float L) {
-  const int t = row / a.G;
+  const int t = a.by_g(row);
   const int qh = h * a.G + (row - t * a.G);
   const long long orow = ((long long)r * a.T + t) * a.Hq + qh;
   const float inv = L == 0.f ? 0.f : 1.f / L;  // a NaN sum stays one
@@ -251,18 +251,18 @@ template <int BS, bool PAGED>
 __device__ __forceinline__ bool tree_setup(const TreeAttnArgs& a, int group_rows, TreeItem& t) {
   int group, rs;
   if (PAGED && a.by_length) {
-    rs = tree_item_spread(blockIdx.x, a.groups, a.R * a.Hkv * a.nsplit, group);
+    rs = tree_item_spread(blockIdx.x, a, a.R * a.Hkv * a.nsplit, group);
     if (rs < 0) return false;
   } else {
     const int item = tree_item(blockIdx.x, a.R * a.Hkv * a.nsplit * a.groups);
     if (item < 0) return false;
-    rs = item / a.groups;
+    rs = a.by_groups(item);
     group = item - rs * a.groups;
   }
   t.row0 = group * group_rows;
-  t.rh = rs / a.nsplit;
+  t.rh = a.by_nsplit(rs);
   t.split = rs - t.rh * a.nsplit;
-  t.r = t.rh / a.Hkv;
+  t.r = a.by_hkv(t.rh);
   t.h = t.rh - t.r * a.Hkv;
   if (PAGED && a.by_length) {
     t.r = request_of_rank(a.ctx_len, a.R, t.r, t.ctx);
@@ -287,8 +287,9 @@ __device__ __forceinline__ Ctx tree_units(const TreeAttnArgs& a, const TreeItem&
   const Ctx c = ctx_blocks(t.ctx, BS, a.NBmax);
   L = c.nb ? c.n_cand * BS + c.local_len : 0;
   const int nu = PAGED ? (L + 31) / 32 : (BS == 16 ? (a.k_slots + 2) / 2 : a.k_slots + 1);
-  begin = (int)((long long)nu * t.split / a.nsplit);
-  end = (int)((long long)nu * (t.split + 1) / a.nsplit);
+  const int each = a.by_nsplit(nu), more = nu - each * a.nsplit;  // the first `more` splits have one more
+  begin = t.split * each + min(t.split, more);
+  end = begin + each + (t.split < more);
   return c;
 }
 
@@ -318,7 +319,7 @@ __device__ __forceinline__ void block_entry(const TreeAttnArgs& a, const Ctx& c,
 // q_xor), so that the scale that the scores meet is positive.
 __device__ __forceinline__ void load_q(const TreeAttnArgs& a, const TreeItem& t, int first, int g, int i, bf16x8 (&qb)[4]) {
   const int row = first + i;
-  const int tq = row < a.rows ? row / a.G : 0;
+  const int tq = row < a.rows ? a.by_g(row) : 0;
   const int qh = t.h * a.G + (row < a.rows ? row - tq * a.G : 0);
   const uint16_t* qrow = a.q + (((long long)t.r * a.T + tq) * a.Hq + qh) * kHeadDim;
 #pragma unroll
@@ -473,7 +474,7 @@ __global__ __launch_bounds__(kTW * 64) void tree_attn_kernel(TreeAttnArgs a) {
 #pragma unroll
     for (int v = 0; v < NT; ++v) {
       const int row = t.row0 + v * 16 + i;
-      const int tq = row < a.rows ? row / a.G : 0;
+      const int tq = row < a.rows ? a.by_g(row) : 0;
       const uint32_t half = __shfl((uint32_t)(anc >> (tu * 32)), tq);
       f32x4 sc[2];
       unit_scores(u.k, qb[v], sc);
@@ -564,7 +565,7 @@ __global__ __launch_bounds__(kTW * 64) void tree_attn_kernel(TreeAttnArgs a) {
     f32x4 o = *reinterpret_cast<const f32x4*>(&s_o[0][row][c4 * 4]);
 #pragma unroll
     for (int w = 1; w < kTW; ++w) o += *reinterpret_cast<const f32x4*>(&s_o[w][row][c4 * 4]);
-    if (s_wild[kTW - 1] | s_wild[kTW - 2]) add_wild(a, t, s_anc[(t.row0 + row) / a.G], c4, o);
+    if (s_wild[kTW - 1] | s_wild[kTW - 2]) add_wild(a, t, s_anc[a.by_g(t.row0 + row)], c4, o);
     if (a.nsplit == 1) {
       write_row(a, t.r, t.h, t.row0 + row, c4, o, s_ml[0][row], s_ml[1][row]);
     } else {
@@ -868,7 +869,7 @@ __global__ __launch_bounds__(kRowsThreads) void tree_attn_rows_kernel(TreeAttnAr
           uint32_t bits = (1u << keep) - 1;
           if (tree) {
             const int row = t.row0 + (rt + v * kRowPlaces) * 16 + i;
-            bits = (uint32_t)(s_anc[row < a.rows ? row / a.G : 0] >> (e.x * 32 + 8 * g));
+            bits = (uint32_t)(s_anc[row < a.rows ? a.by_g(row) : 0] >> (e.x * 32 + 8 * g));
           }
           mask_scores(sc[v], bits);
         }
@@ -928,7 +929,7 @@ __global__ __launch_bounds__(kRowsThreads) void tree_attn_rows_kernel(TreeAttnAr
     const int c4 = pos & 31;
     if (row >= last) break;
     f32x4 o = *reinterpret_cast<const f32x4*>(&s_o[row][c4 * 4]);
-    if (s_wild) add_wild(a, t, s_anc[(t.row0 + row) / a.G], c4, o);
+    if (s_wild) add_wild(a, t, s_anc[a.by_g(t.row0 + row)], c4, o);
     if (a.nsplit == 1) {
       write_row(a, t.r, t.h, t.row0 + row, c4, o, s_ml[0][row], s_ml[1][row]);
     } else {
@@ -943,12 +944,11 @@ __global__ __launch_bounds__(kRowsThreads) void tree_attn_rows_kernel(TreeAttnAr
 constexpr int kTreeMergeRows = 8;
 
 __global__ __launch_bounds__(kTreeMergeRows * 32) void tree_merge_kernel(TreeAttnArgs a) {
-  const int groups = (a.rows + kTreeMergeRows - 1) / kTreeMergeRows;
-  const int item = tree_item(blockIdx.x, a.R * a.Hkv * groups);
+  const int item = tree_item(blockIdx.x, a.R * a.Hkv * a.groups);  // a.groups, by_groups: of kTreeMergeRows rows
   if (item < 0) return;
-  const int rh = item / groups;
-  const int row = (item - rh * groups) * kTreeMergeRows + (threadIdx.x >> 5);
-  const int r = rh / a.Hkv;
+  const int rh = a.by_groups(item);
+  const int row = (item - rh * a.groups) * kTreeMergeRows + (threadIdx.x >> 5);
+  const int r = a.by_hkv(rh);
   if (row >= tree_length(a, r) * a.G) return;
   const int c4 = threadIdx.x & 31;
   const long long base = (long long)rh * a.nsplit * a.rows + row;
@@ -1017,8 +1017,11 @@ hipError_t launch_tree_attn(const TreeAttnArgs& a, bool paged, hipStream_t s) {
     paged ? launch_bs<32, true>(a, s) : launch_bs<32, false>(a, s);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.nsplit == 1) return e;
-  const long long items = (long long)a.R * a.Hkv * ((a.rows + kTreeMergeRows - 1) / kTreeMergeRows);
-  hipLaunchKernelGGL(tree_merge_kernel, dim3((unsigned)((items + 7) / 8 * 8)), dim3(kTreeMergeRows * 32), 0, s, a);
+  TreeAttnArgs m = a;
+  m.groups = (a.rows + kTreeMergeRows - 1) / kTreeMergeRows;
+  m.by_groups = fast_div(m.groups);
+  const long long items = (long long)a.R * a.Hkv * m.groups;
+  hipLaunchKernelGGL(tree_merge_kernel, dim3((unsigned)((items + 7) / 8 * 8)), dim3(kTreeMergeRows * 32), 0, s, m);
   return hipGetLastError();
 }
 

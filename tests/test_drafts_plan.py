@@ -17,6 +17,16 @@ extern "C" void plan(long long pairs, int G, int T, int units, int ragged, long 
   const oasis::TreePlan p = oasis::tree_plan(pairs, G, T, units, ragged);
   o[0] = p.rows; o[1] = p.tiles; o[2] = p.groups; o[3] = p.nsplit; o[4] = p.part_o_floats; o[5] = p.bytes;
 }
+extern "C" long long wrong_quotients(unsigned d) {
+  const oasis::FastDiv f = oasis::fast_div(d);
+  long long bad = 0;
+  const auto at = [&](unsigned long long n) { bad += n < 1ull << 31 && f((unsigned)n) != n / d; };
+  for (unsigned long long n = 0; n < 70000; ++n) at(n);
+  for (unsigned long long q = 1; q * d < 1ull << 31; q += 1 + q / 1000)  // around multiples
+    for (int e = -1; e <= 1; ++e) at(q * d + e);
+  for (unsigned long long e = 1; e < 1000; ++e) at((1ull << 31) - e);
+  return bad;
+}
 """
 
 
@@ -30,14 +40,21 @@ def plan(tmp_path_factory):
     subprocess.run([cxx, "-std=c++17", "-O1", "-shared", "-fPIC", "-I",
                     os.path.join(ROOT, "paper_2608_08097_amd", "csrc"), str(d / "shim.cpp"), "-o", str(d / "shim.so")],
                    check=True)
-    f = ctypes.CDLL(str(d / "shim.so")).plan
+    shim = ctypes.CDLL(str(d / "shim.so"))
+    f, shim.wrong_quotients.restype = shim.plan, ctypes.c_longlong
 
     def call(pairs, G, T, units, ragged):
         o = (ctypes.c_longlong * 6)()
         f(ctypes.c_longlong(pairs), G, T, units, ragged, o)
         return dict(zip(("rows", "tiles", "groups", "nsplit", "part_o", "bytes"), o))
 
+    call.wrong_quotients = shim.wrong_quotients
     return call
+
+
+def test_quotients_by_multiplication(plan):
+    for d in [*range(1, 300), 511, 512, 513, 1000, 4095, 4096, 4097, 65535, 65536, 1000003, 2 ** 30, 2 ** 31 - 1]:
+        assert plan.wrong_quotients(d) == 0, d
 
 
 def test_plans_cover_the_rows_and_fit_the_workspace(plan):
