@@ -173,16 +173,16 @@ struct Child {
 __device__ __forceinline__ Child load_child(const VerifyArgs& a, int r, int len, int lane) {
   Child c;
   if (!a.draft) c.qx = 1.0;
-  if (lane > 0 && lane < len) {
+  if (lane > 0 && lane < a.T) {  // read beside the length
     c.par = a.parent ? a.parent[(long long)r * a.T + lane] : lane - 1;
     c.x = a.tokens[(long long)r * a.T + lane];
     c.u = a.accept_u[(long long)r * a.T + lane];
-    if (c.par < 0 || c.par >= lane || c.x < 0 || c.x >= a.V) {
-      c.par = -1;  // not a child of any row, or no token: passed over
-    } else {
-      c.px = positive(row_of(a.target, a.target_stride, r, a.T, c.par)[c.x]);
-      if (a.draft) c.qx = positive(row_of(a.draft, a.draft_stride, r, a.T, c.par)[c.x]);
-    }
+  }
+  if (lane >= len || c.par < 0 || c.par >= lane || c.x < 0 || c.x >= a.V) {
+    c.par = -1;  // not a child of any row, or no token: passed over
+  } else {
+    c.px = positive(row_of(a.target, a.target_stride, r, a.T, c.par)[c.x]);
+    if (a.draft) c.qx = positive(row_of(a.draft, a.draft_stride, r, a.T, c.par)[c.x]);
   }
   return c;
 }
@@ -414,15 +414,13 @@ __device__ __forceinline__ Residual residual_of(const VerifyArgs& a, int r, cons
                   rejected, ch.x, a.V};
 }
 
-// The next token, from the masses of the last row's blocks; by the workgroup (the
+// The next token, from the block of the last row that it is in; by the workgroup (the
 // first wave's is the one that counts).
 template <bool DRAFT>
-__device__ __forceinline__ void write_next(const VerifyArgs& a, int r, int len, Residual res, const double* masses,
+__device__ __forceinline__ void write_next(const VerifyArgs& a, int r, int len, Residual res, BlockPick p, double u,
                                            VerifyShared& sh) {
   const int lane = threadIdx.x & 63;
-  const double u = (double)a.sample_u[r];
   int token = -1;
-  BlockPick p = pick_block(masses, blocks_of(a.V).count, u, lane);
   if (p.block >= 0) {
     if (threadIdx.x >= 64) return;
     token = pick_token<DRAFT>(res, p, u, lane);
@@ -455,8 +453,9 @@ __global__ __launch_bounds__(kVT) void verify_kernel(VerifyArgs a) {
   if (threadIdx.x < 64) write_path(a, r, lane, w, ch.x);
   if (len < 1) return;
   const Residual res = residual_of(a, r, ch, w.node, w.coef, w.rejected);
+  const double u = (double)a.sample_u[r];
   row_masses<DRAFT>(res, sh);
-  write_next<DRAFT>(a, r, w.len, res, sh.mass, sh);
+  write_next<DRAFT>(a, r, w.len, res, pick_block(sh.mass, blocks_of(a.V).count, u, lane), u, sh);
 }
 
 // Several workgroups for a request: each walks by itself (over whole rows where a
@@ -484,12 +483,14 @@ __global__ __launch_bounds__(kVT) void verify_pick_kernel(VerifyArgs a) {
   __shared__ VerifyShared sh;
   const int r = blockIdx.x;
   const int lane = threadIdx.x & 63;
+  // all that is read here at once; the masses of a request without a row are not defined
   const VerifyState st = a.state[r];
-  if (st.len < 1) return;
+  const double u = (double)a.sample_u[r];
   Child ch;
-  ch.x = lane < verify_len(a, r) ? a.tokens[(long long)r * a.T + lane] : -1;
-  write_next<DRAFT>(a, r, st.len, residual_of(a, r, ch, st.node, st.coef, st.rejected),
-                    a.part + (long long)r * kVerifyBlocks, sh);
+  ch.x = lane < a.T ? a.tokens[(long long)r * a.T + lane] : -1;
+  const BlockPick p = pick_block(a.part + (long long)r * kVerifyBlocks, blocks_of(a.V).count, u, lane);
+  if (st.len < 1) return;
+  write_next<DRAFT>(a, r, st.len, residual_of(a, r, ch, st.node, st.coef, st.rejected), p, u, sh);
 }
 
 template <bool DRAFT>
