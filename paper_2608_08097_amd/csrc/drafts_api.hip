@@ -243,6 +243,7 @@ oasis_status oasis_verify_drafts(int32_t num_reqs, int32_t num_q_tokens, int32_t
   a.R = num_reqs;
   a.T = num_q_tokens;
   a.V = vocab;
+  a.cut = oasis::verify_cut(vocab);
   a.groups = oasis::verify_groups(num_reqs, vocab, draft_probs != nullptr);
   a.part = static_cast<double*>(workspace);
   a.state = reinterpret_cast<oasis::VerifyState*>(a.part + (size_t)num_reqs * oasis::kVerifyBlocks);

@@ -31,6 +31,14 @@ struct TreeAttnArgs {
 };
 hipError_t launch_tree_attn(const TreeAttnArgs& a, bool paged, hipStream_t s);
 
+constexpr int kVerifyBlocks = 256;  // blocks of a row at most
+struct VerifyCut {
+  int size, count;  // entries of a block (a multiple of 1,024), blocks
+};
+inline VerifyCut verify_cut(int V) {
+  const int size = ((V + kVerifyBlocks - 1) / kVerifyBlocks + 1023) / 1024 * 1024;
+  return VerifyCut{size, (V + size - 1) / size};
+}
 struct VerifyArgs {
   const float* target;       // [R][T] rows of V, target_stride apart
   const float* draft;        // the same, draft_stride apart; NULL: drafts without probabilities
@@ -46,6 +54,7 @@ struct VerifyArgs {
   double* part;              // [R][kVerifyBlocks] masses
   struct VerifyState* state; // [R]
   int R, T, V, groups;       // workgroups per request
+  VerifyCut cut;
 };
 // Where a request's walk ended: coefficient, rejected siblings, node, rows on the path.
 struct VerifyState {
@@ -53,7 +62,6 @@ struct VerifyState {
   unsigned long long rejected;
   int node, len;
 };
-constexpr int kVerifyBlocks = 256;  // blocks of a row at most
 constexpr int kVerifyGroups = 16;   // workgroups per request at most
 // Workgroups per request: one (a single launch), or as many as the CUs allow with
 // 32 KB of the last row, or rows, for each, where that is 128 KB and more. Measured

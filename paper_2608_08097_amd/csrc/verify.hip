@@ -80,6 +80,7 @@ struct Residual {
   unsigned long long rejected;
   int tokens;      // lane c: row c's token
   int V;
+  VerifyCut cut;
 
   template <bool DRAFT>
   __device__ __forceinline__ double at(float pv, float qv) const {
@@ -261,20 +262,12 @@ __device__ __forceinline__ int verify_len(const VerifyArgs& a, int r) {
 constexpr int kVT = 1024;
 constexpr int kWaves = kVT / 64;
 
-struct Blocks {
-  int size, count;  // entries (a multiple of 1,024), blocks
-};
-__device__ __forceinline__ Blocks blocks_of(int V) {
-  const int size = ((V + kVerifyBlocks - 1) / kVerifyBlocks + 1023) / 1024 * 1024;
-  return Blocks{size, (V + size - 1) / size};
-}
-
 // Masses of the blocks that this wave takes (number `wave` of `waves`), into
 // out[block]. Two buffers of 1,024 entries in turn: one is on its way while the other
 // is added up.
 template <bool DRAFT>
 __device__ __forceinline__ void block_masses(const Residual& res, int wave, int waves, int lane, double* out) {
-  const Blocks bl = blocks_of(res.V);
+  const VerifyCut bl = res.cut;
   f32x4u p0[4], q0[4], p1[4], q1[4];
   double s = 0.0;
   int b = wave, v = b * bl.size;  // v: the entries to fetch next, of block b
@@ -371,7 +364,7 @@ __device__ __forceinline__ double total_of(const double* masses, int n, int lane
 // block's last one of any mass.
 template <bool DRAFT>
 __device__ __forceinline__ int pick_token(const Residual& res, const BlockPick& p, double u, int lane) {
-  const Blocks bl = blocks_of(res.V);
+  const VerifyCut bl = res.cut;
   const int end = min((p.block + 1) * bl.size, res.V);
   const double border = u * p.total;
   double ahead = p.ahead;
@@ -411,7 +404,7 @@ __device__ __forceinline__ int pick_token(const Residual& res, const BlockPick& 
 __device__ __forceinline__ Residual residual_of(const VerifyArgs& a, int r, const Child& ch, int node, double coef,
                                                 unsigned long long rejected) {
   return Residual{row_of(a.target, a.target_stride, r, a.T, node), row_of(a.draft, a.draft_stride, r, a.T, node), coef,
-                  rejected, ch.x, a.V};
+                  rejected, ch.x, a.V, a.cut};
 }
 
 // The next token, from the block of the last row that it is in; by the workgroup (the
@@ -427,7 +420,7 @@ __device__ __forceinline__ void write_next(const VerifyArgs& a, int r, int len, 
   } else {  // a residual without mass: the target's row itself
     res.rejected = 0;
     row_masses<false>(res, sh);
-    p = pick_block(sh.mass, blocks_of(a.V).count, u, lane);
+    p = pick_block(sh.mass, a.cut.count, u, lane);
     if (p.block >= 0) token = pick_token<false>(res, p, u, lane);
   }
   if (threadIdx.x == 0) a.out_tokens[(long long)r * a.T + len - 1] = token;
@@ -437,7 +430,7 @@ __device__ __forceinline__ void write_next(const VerifyArgs& a, int r, int len, 
 template <bool DRAFT>
 __device__ __forceinline__ double walk_mass(const Residual& res, VerifyShared& sh) {
   row_masses<DRAFT>(res, sh);
-  return total_of(sh.mass, blocks_of(res.V).count, threadIdx.x & 63);
+  return total_of(sh.mass, res.cut.count, threadIdx.x & 63);
 }
 
 // One workgroup for all of a request.
@@ -455,7 +448,7 @@ __global__ __launch_bounds__(kVT) void verify_kernel(VerifyArgs a) {
   const Residual res = residual_of(a, r, ch, w.node, w.coef, w.rejected);
   const double u = (double)a.sample_u[r];
   row_masses<DRAFT>(res, sh);
-  write_next<DRAFT>(a, r, w.len, res, pick_block(sh.mass, blocks_of(a.V).count, u, lane), u, sh);
+  write_next<DRAFT>(a, r, w.len, res, pick_block(sh.mass, a.cut.count, u, lane), u, sh);
 }
 
 // Several workgroups for a request: each walks by itself (over whole rows where a
@@ -488,7 +481,7 @@ __global__ __launch_bounds__(kVT) void verify_pick_kernel(VerifyArgs a) {
   const double u = (double)a.sample_u[r];
   Child ch;
   ch.x = lane < a.T ? a.tokens[(long long)r * a.T + lane] : -1;
-  const BlockPick p = pick_block(a.part + (long long)r * kVerifyBlocks, blocks_of(a.V).count, u, lane);
+  const BlockPick p = pick_block(a.part + (long long)r * kVerifyBlocks, a.cut.count, u, lane);
   if (st.len < 1) return;
   write_next<DRAFT>(a, r, st.len, residual_of(a, r, ch, st.node, st.coef, st.rejected), p, u, sh);
 }
