@@ -24,13 +24,13 @@
 // is read back with the transposing LDS read.
 //
 // Measured (2 x 256 bytes a token and KV head; 4 d operations a row and token):
-//   8 requests x 8 heads x 131,072 tokens, 20 rows   650 us  6.6 TB/s (what the card reads)
-//   64 x 8 x up to 2,064 of a working set, 28 rows    75 us  HBM, and 7 us of a workgroup's start and end
-//   8 x 8 x 2,064 of a working set, 20 rows           20 us  two launches, and 10 of the bytes
+//   8 requests x 8 heads x 131,072 tokens, 20 rows   655 us  6.6 TB/s (what the card reads)
+//   64 x 8 x up to 2,064 of a working set, 28 rows    74 us  HBM, and 7 us of a workgroup's start and end
+//   8 x 8 x 2,064 of a working set, 20 rows           19 us  two launches, and 10 of the bytes
 //   24 x 8 x 1 to 32,768, 64 rows                    213-328 us a draw, 5.5 TB/s
-//   16 x 8 x 4,128 of a working set, 256 rows         86 us  810 TFLOP/s
-//   2 x 8 x 65,000 to 65,536, 512 rows               280 us  980 TFLOP/s, 80 % of a large matrix product here
-//   1 x 8 x 2,000, 8 rows                            9.6 us  two launches (7.4) and three loads in turn
+//   16 x 8 x 4,128 of a working set, 256 rows         83 us  830 TFLOP/s
+//   2 x 8 x 65,000 to 65,536, 512 rows               276 us  990 TFLOP/s, 81 % of a large matrix product here
+//   1 x 8 x 2,000, 8 rows                            9.2 us  two launches (7.4) and three loads in turn
 //
 // The tree's own tokens are one or two more units, with a mask per row, in the
 // last split of every pair. Splits leave partials that a second kernel merges.

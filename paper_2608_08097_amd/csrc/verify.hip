@@ -22,7 +22,7 @@
 // shared by several workgroups and a second launch (verify_groups). Measured, one
 // request, chain, 131,072 entries with draft probabilities (1 MB): 15.6 us with one
 // workgroup, 8.3 with eight; 32,000 entries 8.9 and 7.0; 128 requests of 131,072 36 and,
-// with two, 31; 48 requests, 16 rows, 50,261 entries 25.3, the passes of rejected
+// with two, 31; 48 requests, 16 rows, 50,261 entries 24.8, the passes of rejected
 // siblings one after the other.
 #include "drafts_internal.h"
 
