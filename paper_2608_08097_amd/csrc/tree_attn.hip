@@ -631,7 +631,7 @@ __device__ __forceinline__ void tree_wait() {  // s_waitcnt vmcnt(N) alone
 // A unit's order is: V is read, scores; the next unit's K is read; softmax, second
 // product. So LDS reads run beside the products, in the registers that these leave.
 //
-// With two tiles a wave a step takes some 2,200 cycles, 1,024 of them the matrix unit's;
+// With two tiles a wave a step takes some 2,000 cycles, 1,024 of them the matrix unit's;
 // the softmax of the other wave of the SIMD runs beside about half of these. Without the
 // barrier (each team waiting on a count of its own in LDS) or with the loads spread over
 // the step it is 9 % slower. With one tile a wave (three and four row tiles) the loads
