@@ -21,7 +21,8 @@
 // softmax; token-major V is transposed in registers, 8 x 8 blocks, 32 byte
 // permutes a unit. With more rows every unit is needed by several waves, and
 // tree_attn_rows_kernel brings its K and V into LDS once for them; token-major V
-// is read back with the transposing LDS read.
+// is read back with the transposing LDS read. Small calls with more rows take the
+// first form in several groups of rows (kTreeSmallUnits).
 //
 // Measured (2 x 256 bytes a token and KV head; 4 d operations a row and token):
 //   8 requests x 8 heads x 131,072 tokens, 20 rows   655 us  6.6 TB/s (what the card reads)

@@ -37,6 +37,15 @@ inline FastDiv fast_div(uint32_t d) {
 constexpr int kTreeWaves = 4;     // waves per workgroup of the form for up to two row tiles
 constexpr int kTreeRegisterTiles = 2;  // 16-row tiles up to which K and V go straight into registers
 constexpr int kTreeTiles = 8;     // 16-row tiles per workgroup at most
+// More row tiles than kTreeRegisterTiles go two by two through that form all the same where
+// its loads, each group's own, are at most 16 KB times this: its workgroups start and end
+// faster. Measured over the working set, us with the form for more rows and this one: 64
+// rows, 8 pairs of 129 units (2,064 loads) 16.1 and 13.5, 64 of 33 (4,224) 19.2 and 17.3, 16
+// of 257 (8,224) 23.9 and 28.3; 128 rows, 8 of 129 (4,128) 20.1 and 15.3, 16 of 129 (8,256)
+// 25.5 and 24.6, 32 of 129 (16,512) 29.3 and 33.7; 256 rows, 8 of 65 (4,160) 20.2 and 15.1,
+// 16 of 65 (8,320) 22.4 and 23.4, 32 of 65 (16,640) 28.4 and 34.7. And only where the CUs
+// hold them at once: 256 rows, 128 pairs of 2 (1,024 workgroups) 16.3 and 23.0.
+constexpr int kTreeSmallUnits = 6000;
 constexpr int kTreeMaxTokens = 64;  // a row's ancestors are one 64-bit mask
 constexpr int kTreeMaxRows = 4096;  // G * T
 constexpr int kTreeMaxSplits = 256;
@@ -70,8 +79,11 @@ inline TreePlan tree_plan(long long pairs, int G, int T, int units, bool ragged)
   TreePlan p{};
   p.rows = G * T;
   const int tiles = (p.rows + 15) / 16;
-  p.groups = (tiles + kTreeTiles - 1) / kTreeTiles;
-  p.tiles = (tiles + p.groups - 1) / p.groups;
+  const int twos = (tiles + 1) / 2;
+  const bool small =
+      tiles > kTreeRegisterTiles && pairs * twos <= 512 && pairs * units * twos <= kTreeSmallUnits;
+  p.groups = small ? twos : (tiles + kTreeTiles - 1) / kTreeTiles;
+  p.tiles = small ? kTreeRegisterTiles : (tiles + p.groups - 1) / p.groups;
   p.units = units;
   const long long items = pairs * p.groups;
   const bool rows_form = p.tiles > kTreeRegisterTiles;

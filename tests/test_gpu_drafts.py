@@ -65,7 +65,8 @@ def _inputs(seed, R, Hq, Hkv, T, kind, lens):
     return rng, q, tk, tv, parent, n
 
 
-def _paged(seed, R, Hq, Hkv, T, B, ctx, kind="random", lens=None, bad_pages=False, lse=True, scale=None, pinned=False):
+def _paged(seed, R, Hq, Hkv, T, B, ctx, kind="random", lens=None, bad_pages=False, lse=True, scale=None, pinned=False,
+           spare=0):
     rng, q, tk, tv, parent, n = _inputs(seed, R, Hq, Hkv, T, kind, lens)
     ctx = np.array(ctx, np.int32)
     NB = max(1, (max(ctx.max(), 1) + B - 1) // B + int(rng.integers(0, 3)))
@@ -80,6 +81,9 @@ def _paged(seed, R, Hq, Hkv, T, B, ctx, kind="random", lens=None, bad_pages=Fals
         x.transpose(0, 2, 1, 3)[~held] = _unused(rng, (int((~held).sum()), Hkv, 128))
     if bad_pages:
         table[rng.random((R, NB)) < 0.2] = rng.choice([-1, -2 ** 31, NP, 2 ** 31 - 1])
+    if spare:  # a table far longer than the contexts
+        table = np.concatenate([table, rng.choice([-1, NP, 2 ** 31 - 1], (R, spare)).astype(np.int32)], 1)
+        NB += spare
     d = P.dims(R, Hq, Hkv, 128, B, NB)
     note(f"tree attention paged seed={seed} R={R} Hq={Hq} Hkv={Hkv} T={T} B={B} ctx={ctx.tolist()[:6]} {kind} {n[:6]}")
     before = dev_bf16(random_bf16(seed + 6, (R, T, Hq, 128)))
@@ -150,6 +154,36 @@ def test_paged_largest_rows_and_most_pairs():
     _paged(1301, 2000, 8, 8, 1, 16, list(np.random.default_rng(3).integers(0, 18, 2000)))
 
 
+LONG = 6000  # blocks: so many that more than two row tiles take the form that shares its loads
+
+
+@pytest.mark.parametrize("G,T", [(4, 9), (3, 13), (4, 16), (5, 13), (8, 16), (4, 33), (16, 16), (9, 63), (64, 5)])
+def test_paged_shared_loads_rows(G, T):
+    """Three, four and more row tiles, in one group and in several, with rows left over."""
+    _paged(1400 + G * T, 2, G * 2, 2, T, 16, [777, 40], "random", [T, (T + 1) // 2], spare=LONG)
+
+
+@pytest.mark.parametrize("B", [16, 32])
+@pytest.mark.parametrize("ctx", [[0], [1], [15, 16, 17], [31, 32, 33], [0, 1000, 64], [-4, 500, 333], [4097]])
+def test_paged_shared_loads_lengths(B, ctx):
+    _paged(1500 + B + len(ctx), len(ctx), 24, 2, 5, B, ctx, spare=LONG)
+    _paged(1600 + B + len(ctx), len(ctx), 16, 2, 20, B, ctx, "beam", spare=LONG)
+
+
+def test_paged_shared_loads_masks():
+    _paged(1700, 3, 16, 2, 9, 16, [300, 555, 90], bad_pages=True, spare=LONG)
+    _paged(1701, 2, 32, 2, 17, 32, [300, 555], "roots", [17, 0], bad_pages=True, spare=LONG)
+    _paged(1702, 1, 16, 2, 20, 32, [300], scale=-0.07, spare=LONG)
+    _paged(1703, 1, 16, 2, 6, 32, [45], scale=0.0, lse=False, spare=LONG)
+    _paged(1704, 2, 16, 2, 7, 16, [300, 20], pinned=True, spare=LONG)
+
+
+@pytest.mark.parametrize("G,T", [(4, 10), (8, 17)])
+@pytest.mark.parametrize("B,ks", [(16, 2600), (32, 1300)])
+def test_sparse_shared_loads(G, T, B, ks):
+    _sparse(1800 + G * T, 2, G * 2, 2, T, B, ks, [1000, 37], lens=[T, (T + 1) // 2], free=0.9)
+
+
 def test_paged_scale_and_no_lse():
     _paged(406, 2, 8, 2, 4, 16, [300, 20], lse=False, scale=0.05)
     _paged(407, 1, 8, 2, 4, 16, [300], scale=0.0)
@@ -207,8 +241,8 @@ def test_sparse_all_free_and_none_free():
     _sparse(802, 1, 64, 4, 32, 32, 128, [9000], "beam", free=0.0)
 
 
-@pytest.mark.parametrize("paged", [True, False])
-def test_rows_off_the_path_have_no_influence(paged):
+@pytest.mark.parametrize("paged,spare", [(True, 0), (False, 0), (True, LONG), (False, 2000)])
+def test_rows_off_the_path_have_no_influence(paged, spare):
     """Infinities and NaN in the keys and values of some rows: rows that attend them take them up, the others are what
     they are with finite values there."""
     R, Hq, Hkv, T, B, L = 1, 8, 2, 40, 16, 100
@@ -221,7 +255,8 @@ def test_rows_off_the_path_have_no_influence(paged):
     tk2[0, 7, :, 5], tv2[0, 7, :, 3], tv2[0, 20, 1, 100], tv2[0, 33] = NAN, INF, NAN, INF | 0x8000
     NB = (L + B - 1) // B
     kp, vp = random_bf16(901, (NB, Hkv, B, 128)), random_bf16(902, (NB, Hkv, B, 128))
-    d = P.dims(R, Hq, Hkv, 128, B, NB)
+    d = P.dims(R, Hq, Hkv, 128, B, NB + spare)
+    junk = np.full((spare, Hkv, B, 128), NAN, np.uint16)  # free slots
     outs = []
     for k, v in ((tk, tv), (tk2, tv2)):
         out, lse = torch.zeros((R, T, Hq, 128), dtype=torch.bfloat16, device="cuda"), torch.zeros((R, T, Hq), device="cuda")
@@ -229,13 +264,15 @@ def test_rows_off_the_path_have_no_influence(paged):
         tree = (dev_bf16(k), dev_bf16(v), dev_i32(parent), None, None, out, lse)
         if paged:
             ws = torch.zeros(P.oasis_tree_attn_workspace_bytes(d, T), dtype=torch.uint8, device="cuda")
-            P.oasis_tree_attn(d, dev_bf16(q), T, dev_bf16(kp), dev_bf16(vp), dev_i32(np.arange(NB)[None]), dev_i32([L]),
-                              *tree, ws)
+            P.oasis_tree_attn(d, dev_bf16(q), T, dev_bf16(kp), dev_bf16(vp), dev_i32([[*range(NB), *[-1] * spare]]),
+                              dev_i32([L]), *tree, ws)
         else:
-            ws = torch.zeros(P.oasis_sparse_tree_attn_workspace_bytes(d, T, NB - 1), dtype=torch.uint8, device="cuda")
-            smap = np.broadcast_to(np.arange(NB - 1), (1, Hkv, NB - 1))
-            P.oasis_sparse_tree_attn(d, dev_bf16(q), T, dev_bf16(kp), dev_bf16(pool_v_from_htd(vp)), dev_i32(smap), NB - 1,
-                                     dev_i32([L]), *tree, ws)
+            ks = NB - 1 + spare
+            pools = [np.concatenate([x[:-1], junk, x[-1:]]) for x in (kp, vp)]
+            ws = torch.zeros(P.oasis_sparse_tree_attn_workspace_bytes(d, T, ks), dtype=torch.uint8, device="cuda")
+            smap = np.broadcast_to(np.array([*range(NB - 1), *[-1] * spare]), (1, Hkv, ks))
+            P.oasis_sparse_tree_attn(d, dev_bf16(q), T, dev_bf16(pools[0]), dev_bf16(pool_v_from_htd(pools[1])),
+                                     dev_i32(smap), ks, dev_i32([L]), *tree, ws)
         outs.append((out.float().cpu()[0], lse.cpu()[0]))
     (o0, l0), (o1, l1) = outs
     assert torch.equal(o0[~hit], o1[~hit]) and torch.equal(l0[~hit], l1[~hit])
