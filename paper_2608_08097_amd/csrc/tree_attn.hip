@@ -106,6 +106,9 @@ __device__ __forceinline__ void clear_tokens(u32x4 (&v)[8], int keep) {
 // taken out of the product (true: there were some) and added to the rows that
 // attend them when those are written (add_wild).
 __device__ __forceinline__ bool wild_bf16(uint32_t b) { return (b & 0x7F80u) == 0x7F80u; }
+__device__ __forceinline__ bool wild_f32(float x) {
+  return (__builtin_bit_cast(uint32_t, x) & 0x7F800000u) == 0x7F800000u;
+}
 __device__ __forceinline__ bool take_wild(u32x4 (&v)[8]) {
   uint32_t any = 0;  // an exponent of ones carries into the sign's place
 #pragma unroll
@@ -973,14 +976,27 @@ __global__ __launch_bounds__(kTreeMergeRows * 32) void tree_merge_kernel(TreeAtt
     o *= keep;
 #pragma unroll
     for (int s = 0; s < kBatch; ++s) {
-      // a split without an attended token (maximum -inf) weighs nothing
-      if (s0 + s < a.nsplit && ml[s].x != -INFINITY) {
-        const float f = fast_exp2(ml[s].x - mn);
+      if (s0 + s < a.nsplit) {
+        // a split without an attended token (maximum -inf) weighs nothing
+        const float f = ml[s].x == -INFINITY ? 0.f : fast_exp2(ml[s].x - mn);
         S += ml[s].y * f;
         o += os[s] * f;
       }
     }
     M = mn;
+  }
+  // An infinity in a split whose weight is too small for a float meets a factor of 0
+  // above, and is NaN: its weight is positive, so the row takes it up as it is, as it
+  // does where one split holds everything. Rare, and so read again.
+  if (__builtin_amdgcn_ballot_w64(o[0] != o[0] || o[1] != o[1] || o[2] != o[2] || o[3] != o[3])) {
+    f32x4 w = {0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < a.nsplit; ++s) {
+      const f32x4 x = *reinterpret_cast<const f32x4*>(a.part_o + (base + (long long)s * a.rows) * kHeadDim + c4 * 4);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] += wild_f32(x[e]) ? x[e] : 0.f;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = wild_f32(w[e]) ? w[e] : o[e];
   }
   write_row(a, r, rh - r * a.Hkv, row, c4, o, M, S);
 }
