@@ -57,6 +57,18 @@ struct TreePlan {
   std::size_t part_o_floats, bytes;
 };
 
+// How far a row's reference lies above its scores, in powers of two, in a call of at most
+// `units` units of cached tokens and two of the tree: the four lanes of a row each add
+// eight probabilities of a unit, at most 2^(8 - lift) together, and the sums of all of
+// them shall stay below 1/2. A lift of the most tokens that any call can have (38) would
+// cost values below 2^-88 their last bits; this one costs them little more than dividing
+// a probability by that many tokens does.
+inline int tree_lift(int units) {
+  int lift = 11;
+  while ((1ll << (lift - 11)) < (long long)units + 2) ++lift;
+  return lift;
+}
+
 inline long long tree_slots(const TreePlan& p) {  // workgroups that the CUs hold at once
   return p.tiles > kTreeRegisterTiles ? 256 : 512;
 }

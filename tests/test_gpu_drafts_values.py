@@ -1,5 +1,5 @@
-"""Tree attention on values at the ends of their range: infinities of negligible weight. Against the formula in float64,
-in every form of the kernels and however the cache is split."""
+"""Tree attention on values at the ends of their range: infinities of negligible weight, the largest finite values.
+Against the formula in float64, in every form of the kernels and however the cache is split."""
 import numpy as np
 import pytest
 import torch
@@ -12,6 +12,8 @@ from workloads import random_bf16
 
 pytestmark = pytest.mark.gpu
 
+ONE = 0x3F80
+BIG = 0x7F7F  # the largest finite value, (2 - 2^-7) 2^127
 MINUS = 0x8000
 
 # paged, G, T, B, blocks of the table (or slots) past the context: one and two row tiles of the register form, one and two
@@ -107,3 +109,41 @@ def test_opposite_infinities_in_one_path():
         x["tv"][0, 1, :, 5], x["tv"][0, 2, :, 5] = INF, INF | MINUS
         o = _Call(form, 60, **x).run()[0][0, :, :, 5]
         assert torch.isfinite(o[0]).all() and (o[1] == torch.inf).all() and torch.isnan(o[2:]).all()
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("L", [0, 1, 47, 2500])
+def test_largest_values(form, L):
+    """A mean of finite values is finite: values of the largest magnitude, of one sign and of both."""
+    for signs in (False, True):
+        x = _random(form, L, 4200 + L)
+        for v in ("vp", "tv"):
+            x[v][:] = BIG | (x[v] & MINUS if signs else 0)
+        _Call(form, L, **x).check()
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_largest_values_behind_rising_logits(form):
+    """Logits that rise by less than moves a row's reference, from unit to unit: the sums are at their largest."""
+    x = _random(form, 2500, 4300)
+    B, rise = form[3], np.arange(len(x["kp"]) * form[3]) // 32
+    x["q"][:], x["kp"][:] = 0, 0
+    x["q"][..., 0] = ONE
+    # 128 / sqrt(128) nats a step of 1 in q k; bf16 steps of the key's one entry
+    steps = torch.tensor(np.minimum(rise * 0.75, 48.0), dtype=torch.bfloat16).view(torch.int16).numpy().view(np.uint16)
+    x["kp"][..., 0] = steps.reshape(-1, B)[:, None, :]
+    x["vp"][:], x["tv"][:] = BIG, BIG
+    _Call(form, 2500, **x).check()
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_small_values(form):
+    """Values of 2^-80: a sum whose terms are scaled down by some 2^20 keeps them."""
+    x = _random(form, 2500, 4400)
+    for v in ("vp", "tv"):
+        x[v][:] = (x[v] & np.uint16(0x807F)) | np.uint16((127 - 80) << 7)
+    c = _Call(form, 2500, **x)
+    out, lse = c.run()
+    ref, ref_lse = c.reference()
+    up = 2.0 ** 80  # compared at the size that the tolerances are made for
+    _check((out.float() * up).bfloat16(), lse, ref * up, c.reference(_magnitude)[0] * up, ref_lse, out)
