@@ -103,7 +103,6 @@ oasis_status make_tree_args(const TreeCall& c, const TreePlan& p, TreeAttnArgs* 
   t.scale_log2 = c.scale == 0.f ? 1.f : std::fabs(c.scale) * kLog2e;
   t.q_and = c.scale == 0.f ? 0u : ~0u;
   t.q_xor = c.scale < 0.f ? 0x80008000u : 0u;
-  t.lift = (float)tree_lift(p.units);
   t.top = std::ldexp(1.f, 8 - tree_lift(p.units));
   t.rows = p.rows;
   t.tiles = p.tiles;

@@ -25,7 +25,7 @@ struct TreeAttnArgs {
   int R, Hq, Hkv, G, T, B, NBmax, k_slots;
   float scale_log2;          // |scale| * log2(e), 1 for a scale of 0
   uint32_t q_and, q_xor;     // what makes up for that in the queries' bits
-  float lift, top;           // of a row's reference, and of eight probabilities (tree_lift)
+  float top;                 // most of eight probabilities, 2^(8 - tree_lift)
   int rows, tiles, groups, nsplit;
   int by_length;             // pages: the requests by length (tree_by_length)
   FastDiv by_groups, by_nsplit, by_hkv, by_g;

@@ -147,24 +147,27 @@ __device__ __forceinline__ void mask_scores(f32x4 (&sc)[2], uint32_t bits) {
 // them unrounded), the row's reference (negated: +inf before its first token) and
 // the lane's partial sum updated. A probability is 2^(score - reference), and the
 // reference follows the row's maximum only when a lane's eight probabilities pass
-// a.top together: that needs no maximum of every unit's scores, and values far
+// `top` together: that needs no maximum of every unit's scores, and values far
 // above the reference show as large, infinite or NaN sums. The accumulators are
 // rescaled then, in a branch that is rare after a wave's first unit. The reference
-// lies a.lift above the maximum that it was taken from, and a.top as far below 2^8
+// lies a lift above the maximum that it was taken from, and `top` as far below 2^8
 // (tree_lift): the sums of all the tokens that the call can attend stay below 1/2,
 // so that no finite value overflows in them.
+// (Taken from `top` where it is needed: with it as an argument of its own, live through
+// the loops, wide trees took 1 % more.)
+__device__ __forceinline__ float tree_lift_of(float top) { return (float)(9 - __builtin_amdgcn_frexp_expf(top)); }
+
 __device__ __forceinline__ float unit_exp(const f32x4 (&s)[2], float scale, float m_neg, float (&p)[8]) {
 #pragma unroll
   for (int e = 0; e < 8; ++e) p[e] = fast_exp2(__builtin_fmaf(s[e >> 2][e & 3], scale, m_neg));
   return ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
 }
 
-__device__ __forceinline__ bf16x8 unit_softmax(const TreeAttnArgs& a, const f32x4 (&s)[2], float& m_neg, float& l_part,
+__device__ __forceinline__ bf16x8 unit_softmax(const f32x4 (&s)[2], float scale, float top, float& m_neg, float& l_part,
                                                f32x4 (&acc)[8]) {
-  const float scale = a.scale_log2;
   float p[8];
   float psum = unit_exp(s, scale, m_neg, p);
-  const uint64_t past = __builtin_amdgcn_ballot_w64(!(psum <= a.top));
+  const uint64_t past = __builtin_amdgcn_ballot_w64(!(psum <= top));
   if (__builtin_expect(past != 0, 0)) {
     // the rows that passed it in one of their four lanes; the others stay as they are
     const uint64_t rows = past | past >> 16 | past >> 32 | past >> 48;
@@ -172,7 +175,7 @@ __device__ __forceinline__ bf16x8 unit_softmax(const TreeAttnArgs& a, const f32x
     const float lmax = scale * fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
                                      fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
     float m = fmaxf(lmax, __shfl_xor(lmax, 16));
-    m = fmaxf(fmaxf(m, __shfl_xor(m, 32)) + a.lift, -m_neg);
+    m = fmaxf(fmaxf(m, __shfl_xor(m, 32)) + tree_lift_of(top), -m_neg);
     m = mine ? m : -m_neg;
     const float alpha = m == -INFINITY ? 1.f : fast_exp2(-m_neg - m);
     l_part *= alpha;
@@ -493,7 +496,7 @@ __global__ __launch_bounds__(kTW * 64) void tree_attn_kernel(TreeAttnArgs a) {
       f32x4 sc[2];
       unit_scores(u.k, qb[v], sc);
       mask_scores(sc, half >> (8 * g) & 0xFF);
-      unit_pv(u.v, unit_softmax(a, sc, m_neg[v], l_run[v], acc[v]), acc[v]);
+      unit_pv(u.v, unit_softmax(sc, a.scale_log2, a.top, m_neg[v], l_run[v], acc[v]), acc[v]);
     }
   }
   if (lane == 0) s_wild[wave] = wild;
@@ -522,7 +525,7 @@ __global__ __launch_bounds__(kTW * 64) void tree_attn_kernel(TreeAttnArgs a) {
       for (int v = 0; v < NT; ++v) mask_scores(sc[v], (1u << keep) - 1);
     }
 #pragma unroll
-    for (int v = 0; v < NT; ++v) unit_pv(u.v, unit_softmax(a, sc[v], m_neg[v], l_run[v], acc[v]), acc[v]);
+    for (int v = 0; v < NT; ++v) unit_pv(u.v, unit_softmax(sc[v], a.scale_log2, a.top, m_neg[v], l_run[v], acc[v]), acc[v]);
     __builtin_amdgcn_sched_barrier(0);
     load_v(nxt);
     cur = nxt;
@@ -842,7 +845,7 @@ __global__ __launch_bounds__(kRowsThreads) void tree_attn_rows_kernel(TreeAttnAr
     f32x4 sc[NT][2];
     auto attend = [&]() __attribute__((always_inline)) {
 #pragma unroll
-      for (int v = 0; v < NT; ++v) unit_pv(u.v, unit_softmax(a, sc[v], m_neg[v], l_run[v], acc[v]), acc[v]);
+      for (int v = 0; v < NT; ++v) unit_pv(u.v, unit_softmax(sc[v], a.scale_log2, a.top, m_neg[v], l_run[v], acc[v]), acc[v]);
       __builtin_amdgcn_sched_barrier(0);  // no reads ahead of it, into registers that are then spilled
     };
     // The two waves of a SIMD are of different teams, and do a step's parts in
