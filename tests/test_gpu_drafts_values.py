@@ -1,5 +1,5 @@
-"""Tree attention on values at the ends of their range: infinities of negligible weight, the largest finite values.
-Against the formula in float64, in every form of the kernels and however the cache is split."""
+"""Tree attention on values at the ends of their range: infinities of negligible weight, the largest finite values, NaN
+behind a scale of 0. Against the formula in float64, in every form of the kernels and however the cache is split."""
 import numpy as np
 import pytest
 import torch
@@ -147,3 +147,22 @@ def test_small_values(form):
     ref, ref_lse = c.reference()
     up = 2.0 ** 80  # compared at the size that the tolerances are made for
     _check((out.float() * up).bfloat16(), lse, ref * up, c.reference(_magnitude)[0] * up, ref_lse, out)
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_a_scale_of_zero_keeps_nan(form):
+    """0 times a NaN or an infinity in q is a NaN score of every token; the other rows weigh all tokens alike."""
+    x = _random(form, 60, 4500)
+    x["q"][0, 1, 0, 3], x["q"][0, 2, 1, 4], x["q"][0, 0, -1, 127] = NAN, INF, INF | MINUS
+    c = _Call(form, 60, **x, scale=0.0)
+    out, lse = c.run()
+    bad = torch.zeros(out.shape[:3], dtype=torch.bool)
+    bad[0, 1, 0] = bad[0, 2, 1] = bad[0, 0, -1] = True
+    assert torch.isnan(out.cpu()[bad]).all() and torch.isnan(lse.cpu()[bad]).all()
+    with np.errstate(invalid="ignore"):
+        ref, ref_lse = c.reference()
+        ref_abs = c.reference(_magnitude)[0]
+    good = ~bad.numpy()
+    assert np.isfinite(ref_lse[good]).all()
+    _check(out.cpu()[torch.from_numpy(good)], lse.cpu()[torch.from_numpy(good)], ref[good], ref_abs[good], ref_lse[good],
+           out.cpu()[torch.from_numpy(good)])
