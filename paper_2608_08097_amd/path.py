@@ -11,6 +11,7 @@ memory, pinned host memory, streams and events.
 from __future__ import annotations
 
 import math
+import weakref
 
 import torch
 
@@ -53,6 +54,8 @@ class LayerState:
         self.ev_attended = None  # recorded after the last attention of this layer
         self.layer_id = None    # id in the native issuer of the DecodePath that runs it
         self.pipe_token = None  # the native issuer this layer is registered with
+        # pages of the layer's own (DecodePath.new_layer); None: the path's
+        self.host_k = self.host_v = self.local_source = None
 
     def reset(self):
         self.slot_map.fill_(-1)
@@ -132,7 +135,9 @@ class DecodePath:
     ``[NPhys][Hkv][B][d]``), ``block_table`` the device page table
     ``[R][NBmax]``. The layers from ``new_layer`` share one attention
     workspace, so their attention calls must run in order (the schedules
-    below issue them all on the caller's current stream).
+    below issue them all on the caller's current stream). They share the tier
+    too unless they are given pages of their own, which layers that ``commit``
+    need.
     """
 
     def __init__(self, d: L.OasisDims, num_q_tokens: int, k: int, host_k: torch.Tensor, host_v: torch.Tensor,
@@ -169,8 +174,16 @@ class DecodePath:
         self.local_source = None
         self._ws_attn = None  # the attention workspace of every layer (new_layer)
         self._spec = None     # workspace and outputs of the speculative step (_speculative)
+        self._layers = weakref.WeakSet()  # the layers known to run on this path
+        self._alone = weakref.WeakSet()   # those of them found to have a tier to themselves (commit)
 
-    def new_layer(self) -> LayerState:
+    def new_layer(self, host_k: torch.Tensor | None = None, host_v: torch.Tensor | None = None,
+                  local_source: tuple | None = None) -> LayerState:
+        """A layer of the path: on the path's tier and local-block source, or on pages of its own (``host_k`` and
+        ``host_v``, addressed by the path's block table; ``local_source`` as in ``set_local_source``, by default those
+        pages). The pipelined steps of a layer with pages of its own are issued call by call from here."""
+        if (host_k is None) != (host_v is None) or (local_source is not None and host_k is None):
+            raise ValueError("a layer's own pages are host_k and host_v, with or without a local_source")
         # One attention workspace for all layers of the path: it is scratch of a
         # single call, their attention calls run in order on the foreground stream,
         # and a workspace that every call reuses can stay in the caches (8 x 9.4 MB
@@ -178,7 +191,22 @@ class DecodePath:
         if self._ws_attn is None:
             self._ws_attn = torch.zeros(max(1, L.oasis_attn_workspace_bytes(self.dims, self.T, self.k)),
                                         dtype=torch.uint8, device=self.block_table.device)
-        return LayerState(self.dims, self.T, self.k, self.block_table.device, ws_attn=self._ws_attn)
+        st = LayerState(self.dims, self.T, self.k, self.block_table.device, ws_attn=self._ws_attn)
+        st.host_k, st.host_v, st.local_source = host_k, host_v, local_source
+        self._layers.add(st)
+        self._alone.clear()
+        return st
+
+    def _tier(self, st: LayerState):
+        """(k pages, v pages, block table) of the layer's host tier."""
+        if st.host_k is not None:
+            return st.host_k, st.host_v, self.block_table
+        return self.host_k, self.host_v, self.block_table
+
+    def _local(self, st: LayerState):
+        """The same of its local-block source."""
+        own = st.local_source if st.host_k is not None else self.local_source
+        return own if own is not None else self._tier(st)
 
     def _native_layer(self, st: LayerState) -> int:
         """Handle of the native issuer and the layer id of ``st`` (registered on first use)."""
@@ -261,7 +289,7 @@ class DecodePath:
     # -- individual steps (all asynchronous on `stream`) ----------------------
     def build_summaries(self, st: LayerState, ctx_len: torch.Tensor, k_pages: torch.Tensor | None = None,
                         stream=None):
-        L.oasis_build_summaries(self.dims, self.host_k if k_pages is None else k_pages, self.block_table,
+        L.oasis_build_summaries(self.dims, self._tier(st)[0] if k_pages is None else k_pages, self.block_table,
                                 ctx_len, st.kmax, st.kmin, stream)
 
     def predict(self, st: LayerState, q: torch.Tensor, ctx_len: torch.Tensor, stream=None):
@@ -271,16 +299,14 @@ class DecodePath:
 
     def stage(self, st: LayerState, ctx_len: torch.Tensor, step: int, stream=None, fetch_cap: int | None = None,
               copy_local: bool = True):
-        L.oasis_stage_blocks(self.dims, self.host_k, self.host_v, self.block_table, ctx_len, st.sel, st.sel_count,
+        L.oasis_stage_blocks(self.dims, *self._tier(st), ctx_len, st.sel, st.sel_count,
                              st.scores, self.k, st.slot_map, st.slot_stamp, step,
                              self.fetch_cap if fetch_cap is None else fetch_cap, copy_local, st.pool_k, st.pool_v,
                              st.moved, stream)
 
     def refresh_local(self, st: LayerState, ctx_len: torch.Tensor, stream=None):
         """Write the active local block into slot k (stands in for the model's KV write)."""
-        hk, hv, bt = self.local_source if self.local_source is not None else (self.host_k, self.host_v,
-                                                                               self.block_table)
-        L.oasis_stage_blocks(self.dims, hk, hv, bt, ctx_len, None, None, None,
+        L.oasis_stage_blocks(self.dims, *self._local(st), ctx_len, None, None, None,
                              self.k, None, None, 0, self.k, True, st.pool_k, st.pool_v, None, stream)
 
     def attend(self, st: LayerState, q: torch.Tensor, ctx_len: torch.Tensor, stream=None):
@@ -315,8 +341,8 @@ class DecodePath:
                           tree_v: torch.Tensor, parent: torch.Tensor | None = None,
                           tree_len: torch.Tensor | None = None, pages: tuple | None = None, stream=None):
         """The same over every cached token, for requests below the sparsification threshold (§5.2): ``pages`` are
-        (k_pages, v_pages, block_table) that hold all of them, the host tier by default."""
-        kp, vp, bt = pages if pages is not None else (self.host_k, self.host_v, self.block_table)
+        (k_pages, v_pages, block_table) that hold all of them, the layer's host tier by default."""
+        kp, vp, bt = pages if pages is not None else self._tier(st)
         L.oasis_tree_attn(self.dims, q, self.T, kp, vp, bt, ctx_len, tree_k, tree_v, parent, tree_len, self.scale,
                           st.out, st.lse, self._speculative()[0], stream)
 
@@ -331,18 +357,25 @@ class DecodePath:
 
     def commit(self, st: LayerState, tree_k: torch.Tensor, tree_v: torch.Tensor, path: torch.Tensor,
                path_len: torch.Tensor, ctx_len: torch.Tensor, new_ctx_len: torch.Tensor, stream=None):
-        """Append the accepted rows' keys and values at ``ctx_len`` to the host tier (and to the local-block source),
-        write the lengths that follow, and bring the layer's compressed keys and local block up to them. Before it, no
-        step of the layer may be under way on the background streams (``join``)."""
-        L.oasis_append_tokens(self.dims, tree_k, tree_v, self.T, path, path_len, self.host_k, self.host_v,
-                              self.block_table, ctx_len, new_ctx_len, stream)
-        kp, bt = self.host_k, self.block_table
-        if self.local_source is not None:
-            kp, vp, bt = self.local_source
-            L.oasis_append_tokens(self.dims, tree_k, tree_v, self.T, path, path_len, kp, vp, bt, ctx_len, None,
-                                  stream)
-        L.oasis_update_summaries(self.dims, kp, bt, ctx_len, new_ctx_len, -(-self.T // self.dims.block_size), st.kmax,
-                                 st.kmin, stream)
+        """Append the accepted rows' keys and values at ``ctx_len`` to the layer's host tier (and to its local-block
+        source), write the lengths that follow, and bring the layer's compressed keys and local block up to them. Before
+        it, no step of the layer may be under way on the background streams (``join``). Of several layers on one path
+        each needs pages of its own (``new_layer``): on one tier each would write over the keys and values of the
+        others, so that is refused."""
+        tier, local = self._tier(st), self._local(st)
+        if st not in self._alone:
+            if st not in self._layers:
+                self._layers.add(st)
+                self._alone.clear()
+            if any(o is not st and self._tier(o)[0].data_ptr() == tier[0].data_ptr() for o in self._layers):
+                raise RuntimeError("commit: several layers on one tier would write over each other's keys and values; "
+                                   "give each its own pages (new_layer(host_k, host_v))")
+            self._alone.add(st)
+        L.oasis_append_tokens(self.dims, tree_k, tree_v, self.T, path, path_len, *tier, ctx_len, new_ctx_len, stream)
+        if any(a is not b for a, b in zip(local, tier)):
+            L.oasis_append_tokens(self.dims, tree_k, tree_v, self.T, path, path_len, *local, ctx_len, None, stream)
+        L.oasis_update_summaries(self.dims, local[0], local[2], ctx_len, new_ctx_len, -(-self.T // self.dims.block_size),
+                                 st.kmax, st.kmin, stream)
         self.refresh_local(st, new_ctx_len, stream)
 
     # -- schedules --------------------------------------------------------------
@@ -375,10 +408,11 @@ class DecodePath:
         compressed keys of the blocks completed since then are added on the
         prediction stream before the scoring, read from the local-block source.
         Without a timer the step goes through the library's native issuer (one
-        C call); with one it is issued call by call from here. Switching between
+        C call); with one, or with pages of the layer's own, it is issued call by
+        call from here. Switching between
         the two for one layer needs a device synchronization in between.
         """
-        if timer is None and self.native:
+        if timer is None and self.native and st.host_k is None:
             lid = self._native_layer(st)
             L.oasis_pipeline_step(self._pipe, lid, q, ctx_len, step, growing, moved, torch.cuda.current_stream(),
                                   prev_ctx_len, max_new_blocks)
@@ -400,8 +434,7 @@ class DecodePath:
         ev_attn = torch.cuda.Event()
         ev_attn.record(fg)
         if prev_ctx_len is not None:
-            hk, _, bt = self.local_source if self.local_source is not None else (self.host_k, self.host_v,
-                                                                                 self.block_table)
+            hk, _, bt = self._local(st)
             L.oasis_update_summaries(self.dims, hk, bt, prev_ctx_len, ctx_len, max_new_blocks, st.kmax, st.kmin,
                                      pred)
         e = tm.begin("score", pred)
@@ -416,7 +449,7 @@ class DecodePath:
         xfer.wait_event(ev_pred)
         xfer.wait_event(ev_attn)  # the gather overwrites slots the attention reads
         e = tm.begin("stage", xfer)
-        L.oasis_stage_blocks(self.dims, self.host_k, self.host_v, self.block_table, ctx_len, st.sel, st.sel_count,
+        L.oasis_stage_blocks(self.dims, *self._tier(st), ctx_len, st.sel, st.sel_count,
                              st.scores, self.k, st.slot_map, st.slot_stamp, step, self.fetch_cap, False,
                              st.pool_k, st.pool_v, st.moved if moved is None else moved, xfer)
         tm.end("stage", xfer, e)
