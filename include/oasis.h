@@ -343,7 +343,8 @@ OASIS_API oasis_status oasis_sparse_decode_attn_noalloc(const oasis_dims* dims, 
  *   tree_k, tree_v  bf16 [R][T][Hkv][d]  the rows' own keys and values, which are
  *                           in no cache yet (ctx_len does not count them)
  * Pointers to bf16 tensors and workspaces are 16-byte aligned. All pointers are
- * device pointers, except pages (device memory or pinned host memory).
+ * device pointers, except pages (device memory or pinned host memory). What a call
+ * writes overlaps nothing else that it reads or writes.
  */
 
 /*

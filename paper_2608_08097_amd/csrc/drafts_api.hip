@@ -1,6 +1,7 @@
 // C ABI of the speculative step: argument checks, workspace carving and kernel
 // launches (conventions of api.hip: nothing here allocates memory or throws).
 #include <cmath>
+#include <initializer_list>
 
 #include "drafts_internal.h"
 
@@ -25,6 +26,27 @@ oasis_status need16(const void* p, const char* name, const char* fn) {
   } while (0)
 #define REQUIRE_PTR(p, fn) REQUIRE_AS(need, p, #p, fn)
 #define REQUIRE_ALIGNED(p, fn) REQUIRE_AS(need16, p, #p, fn)
+
+// What a call writes must not be what it reads, or writes elsewhere: the waves and
+// workgroups of a launch read at times of their own.
+struct Buffer {
+  const void* at;
+  long long bytes;
+  const char* name;
+};
+oasis_status apart(std::initializer_list<Buffer> written, std::initializer_list<Buffer> read, const char* fn) {
+  auto meet = [](const Buffer& x, const Buffer& y) {
+    const uintptr_t a = (uintptr_t)x.at, b = (uintptr_t)y.at;
+    return a && b && a < b + (uintptr_t)y.bytes && b < a + (uintptr_t)x.bytes;
+  };
+  for (const Buffer* w = written.begin(); w != written.end(); ++w) {
+    for (const Buffer* o = written.begin(); o != w; ++o)
+      if (meet(*w, *o)) return fail(OASIS_ERR_INVALID_ARG, "%s: %s overlaps %s", fn, w->name, o->name);
+    for (const Buffer& r : read)
+      if (meet(*w, r)) return fail(OASIS_ERR_INVALID_ARG, "%s: %s overlaps %s", fn, w->name, r.name);
+  }
+  return OASIS_OK;
+}
 
 // Sizes of a tree of drafted tokens over any cache.
 oasis_status check_tree(const oasis_dims* d, int32_t T, const char* fn) {
@@ -228,6 +250,13 @@ oasis_status oasis_verify_drafts(int32_t num_reqs, int32_t num_q_tokens, int32_t
   if (!workspace || workspace_bytes < bytes)
     return fail(OASIS_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", fn, workspace_bytes, bytes);
   if ((uintptr_t)workspace & 15) return fail(OASIS_ERR_INVALID_ARG, "%s: workspace is not 16-byte aligned", fn);
+  const long long ints = 4ll * num_reqs * num_q_tokens, reqs = 4ll * num_reqs;
+  const oasis_status st = oasis::apart(
+      {{path, ints, "path"}, {path_len, reqs, "path_len"}, {out_tokens, ints, "out_tokens"}},
+      {{tokens, ints, "tokens"}, {parent, ints, "parent"}, {tree_len, reqs, "tree_len"},
+       {accept_u, ints, "accept_u"}, {sample_u, reqs, "sample_u"}, {workspace, (long long)bytes, "workspace"}},
+      fn);
+  if (st != OASIS_OK) return st;
   oasis::VerifyArgs a{};
   a.target = target_probs;
   a.draft = draft_probs;
@@ -273,6 +302,12 @@ oasis_status oasis_append_tokens(const oasis_dims* dims, const uint16_t* new_k, 
   REQUIRE_PTR(ctx_len, fn);
   if (path && !path_len) return fail(OASIS_ERR_INVALID_ARG, "%s: path without path_len", fn);
   if (new_ctx_len == ctx_len) return fail(OASIS_ERR_INVALID_ARG, "%s: new_ctx_len is ctx_len", fn);
+  const long long reqs = 4ll * dims->num_reqs;
+  st = oasis::apart({{new_ctx_len, reqs, "new_ctx_len"}},
+                    {{ctx_len, reqs, "ctx_len"}, {path_len, reqs, "path_len"}, {path, reqs * num_tokens, "path"},
+                     {block_table, reqs * dims->max_blocks, "block_table"}},
+                    fn);
+  if (st != OASIS_OK) return st;
   const void *kp = nullptr, *vp = nullptr;
   if ((st = oasis::device_view(k_pages, &kp, "k_pages", fn)) != OASIS_OK) return st;
   if ((st = oasis::device_view(v_pages, &vp, "v_pages", fn)) != OASIS_OK) return st;
