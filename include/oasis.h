@@ -357,7 +357,11 @@ OASIS_API oasis_status oasis_sparse_decode_attn_noalloc(const oasis_dims* dims, 
  * This is also the dense attention of a request below the sparsification
  * threshold (§5.2), whose blocks are all in device pages. Arithmetic as
  * oasis_sparse_decode_attn. A row of the tree that is not on another's path has
- * no influence on it, whatever it holds. G * T <= 4096. lse is nullable.
+ * no influence on it, whatever it holds. Finite scores and finite values, of any
+ * size, give finite outputs. An infinite or NaN value of a row of the tree reaches
+ * the rows that attend it however little it weighs; one in the cache reaches every
+ * row, as an infinity or, where its weight is too small for a float, as NaN.
+ * G * T <= 4096. lse is nullable.
  * workspace: oasis_tree_attn_workspace_bytes (0: may be NULL); calls that run at
  * the same time need separate workspaces.
  */
@@ -386,9 +390,15 @@ OASIS_API oasis_status oasis_sparse_tree_attn(const oasis_dims* dims, const uint
 
 /*
  * Verification of the drafted tokens against the target's probabilities, from
- * given random numbers (rejection sampling over a tree: the tokens emitted are
- * distributed as the target's own where the drafted ones were drawn from
- * draft_probs, or chosen without regard to the random numbers).
+ * given random numbers (rejection sampling over a tree). The tokens emitted are
+ * distributed as the target's own where
+ *   with draft_probs, the children of a row were drawn from its draft row, each
+ *     without regard to the others (with replacement: the same token twice is two
+ *     rows), and stand in the order of the draws. Children drawn without
+ *     replacement, sorted by probability or without their repetitions shift that
+ *     distribution, and no call can see it;
+ *   without them, the tokens were chosen in any way that does not look at the
+ *     random numbers.
  *
  *   target_probs  fp32 [R][T] rows of vocab, target_stride elements apart: row t
  *                 is the target's distribution of the token after row t
