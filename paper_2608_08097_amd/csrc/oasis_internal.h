@@ -67,26 +67,6 @@ __device__ __forceinline__ Ctx ctx_blocks(int L, int B, int max_blocks) {
 
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// XCD-aware placement of the `parts` items of each (request, KV head) pair:
-// workgroup ids are dealt round-robin over the 8 XCDs, so id i works on item
-// (i % 8) * ceil(items / 8) + i / 8 and every XCD takes one contiguous run of
-// the items in pair order. The parts of a pair share query rows and partials
-// in one L2, the heads of a request, whose slots are adjacent in the pools,
-// share its XCD, and any number of pairs spreads over all XCDs. (Pairs dealt
-// modulo 8, as before: 90 requests x 8 KV heads, 761 MB, 143 against 124 us a
-// call, 116 with V past the caches; 64 x 8, 544 MB, 103 and 94.) With fewer than 8 pairs each takes an
-// XCD of its own, so that its merge reads the partials from the L2 that holds
-// them (1 pair: 9.3 us, spread over the XCDs 10.2). Returns -1 past the last item.
-__device__ __forceinline__ int xcd_item(int wg, int pairs, int parts) {
-  const int items = pairs * parts;
-  const int per = pairs < 8 ? parts : (items + 7) >> 3;
-  const int item = (wg & 7) * per + (wg >> 3);
-  return item < items ? item : -1;
-}
-inline unsigned xcd_grid(long long pairs, long long parts) {
-  return (unsigned)(pairs < 8 ? parts * 8 : (pairs * parts + 7) / 8 * 8);
-}
-
 // --- host-side launchers (one per .hip translation unit) ---------------------
 
 // Optional timing of one launch: when set, the events take the start / end
