@@ -4,7 +4,8 @@
 // A (token, head) entry is 256 contiguous bytes on both sides, 16 lanes of 16
 // bytes; the pages may be device memory or pinned host memory (posted writes). It is a
 // copy: four chunks of 8,192 tokens (268 MB both ways) 51 us, 5.3 TB/s; a batch's accepted
-// rows (2.4 MB) the time of a launch.
+// rows (2.4 MB) the time of a launch. To pinned pages it runs at the link's rate: 1.2 MB of
+// accepted rows 23 us, 51 GB/s; a chunk of 8,192 tokens 614 us, 55 GB/s.
 #include "drafts_internal.h"
 
 namespace oasis {

@@ -22,16 +22,22 @@
 // permutes a unit. With more rows every unit is needed by several waves, and
 // tree_attn_rows_kernel brings its K and V into LDS once for them; token-major V
 // is read back with the transposing LDS read. Small calls with more rows take the
-// first form in several groups of rows (kTreeSmallUnits).
+// first form in several groups of rows (kTreeSmallUnits). Both forms compute whole
+// tiles, the second one four or eight of them: 2 x 8 x 65,536 tokens take 107 to 112 us
+// with 5 to 8 tiles and 155 to 160 with 9 to 16.
 //
 // Measured (2 x 256 bytes a token and KV head; 4 d operations a row and token):
-//   8 requests x 8 heads x 131,072 tokens, 20 rows   655 us  6.6 TB/s (what the card reads)
-//   64 x 8 x up to 2,064 of a working set, 28 rows    74 us  HBM, and 7 us of a workgroup's start and end
-//   8 x 8 x 2,064 of a working set, 20 rows           19 us  two launches, and 10 of the bytes
+//   8 requests x 8 heads x 131,072 tokens, 20 rows   653 us  6.6 TB/s
+//   64 x 8 x up to 2,064 of a working set, 28 rows   73-75 us  HBM, and 7 us of a workgroup's start and end
+//   8 x 8 x 2,064 of a working set, 20 rows          18.8 us  two launches, and 10 of the bytes
 //   24 x 8 x 1 to 32,768, 64 rows                    213-328 us a draw, 5.5 TB/s
-//   16 x 8 x 4,128 of a working set, 256 rows         83 us  830 TFLOP/s
-//   2 x 8 x 65,000 to 65,536, 512 rows               276 us  990 TFLOP/s, 81 % of a large matrix product here
-//   1 x 8 x 2,000, 8 rows                            9.2 us  two launches (7.4) and three loads in turn
+//   16 x 8 x 4,128 of a working set, 256 rows        82-89 us  780-840 TFLOP/s
+//   2 x 8 x 65,000 to 65,536, 512 rows               276-297 us  920-990 TFLOP/s
+//   1 x 8 x 2,000, 8 rows                            8.9-9.2 us  two launches (7.4) and three loads in turn
+// (a 16,384-cubed bf16 product of the library runs at 1,360 to 1,600 TFLOP/s here.) These
+// block tables fit the contexts. The cut goes by the table's width, not by the lengths:
+// with one for 131,072 tokens 8 x 8 x 2,064 paged tokens take 29 us instead of 20 (20
+// rows) or 55 instead of 40 (256 rows).
 //
 // The tree's own tokens are one or two more units, with a mask per row, in the
 // last split of every pair. Splits leave partials that a second kernel merges.
@@ -957,7 +963,7 @@ __global__ __launch_bounds__(kRowsThreads) void tree_attn_rows_kernel(TreeAttnAr
 }
 
 // Merge of the splits: 8 rows of one pair per workgroup, 32 threads a row, 4 dims a
-// thread; the splits are read kMergeBatch at a time.
+// thread; the splits are read kBatch at a time.
 constexpr int kTreeMergeRows = 8;
 
 __global__ __launch_bounds__(kTreeMergeRows * 32) void tree_merge_kernel(TreeAttnArgs a) {
