@@ -31,6 +31,8 @@ struct TreeAttnArgs {
   FastDiv by_groups, by_nsplit, by_hkv, by_g;
 };
 hipError_t launch_tree_attn(const TreeAttnArgs& a, bool paged, hipStream_t s);
+// What follows an attention kernel: the merge of its splits, and the rows of wild queries under a scale of 0.
+hipError_t launch_tree_finish(const TreeAttnArgs& a, hipStream_t s);
 
 constexpr int kVerifyBlocks = 256;  // blocks of a row at most
 struct VerifyCut {
