@@ -15,13 +15,14 @@
  * oasis_copy_blocks, which moves blocks between the GPU pages and the full host
  * tier (§4.3, dense-to-sparse transition and appends); oasis_tree_attn,
  * oasis_sparse_tree_attn, oasis_verify_drafts and oasis_append_tokens, the
- * speculative step of a drafted token tree; and oasis_pipeline_*, the native
- * issuer of the layer-pipelined step (§4.2.2).
+ * speculative step of a drafted token tree; oasis_rotate, oasis_append_tokens_q4,
+ * oasis_update_summaries_q4 and oasis_tree_attn_q4, the same over a cache held in four
+ * bits; and oasis_pipeline_*, the native issuer of the layer-pipelined step (§4.2.2).
  *
  * General conventions
  * -------------------
  * - Every pointer is owned by the caller. The single-call entry points
- *   (oasis_build_summaries ... oasis_append_tokens) allocate no memory; the
+ *   (oasis_build_summaries ... oasis_tree_attn_q4) allocate no memory; the
  *   scratch that the attention calls and the verification need is a
  *   caller-provided workspace whose size comes from the call's
  *   *_workspace_bytes. The step issuer does allocate,
@@ -454,6 +455,135 @@ OASIS_API oasis_status oasis_append_tokens(const oasis_dims* dims, const uint16_
                                            uint16_t* k_pages, uint16_t* v_pages, int64_t num_pages,
                                            const int32_t* block_table, const int32_t* ctx_len, int32_t* new_ctx_len,
                                            void* stream);
+
+/*
+ * The cache in four bits. A page of B tokens holds Hkv * B * 68 bytes instead of
+ * Hkv * B * 256 of bf16, so that a context 3.7 times as long stays in HBM, and the
+ * selected blocks are read where they lie: nothing is staged.
+ *
+ *   4-bit pages   uint8 [num_pages][oasis_q4_page_bytes], keys and values in pages of
+ *                 their own. A page: codes [Hkv][B][64], then powers [Hkv][B/16][4][4][4].
+ *   codes         dims 2j and 2j + 1 of a token in the low and high half of its byte j;
+ *                 bit 3 a sign, bits 0..2 one of 0, 0.5, 1, 1.5, 2, 3, 4, 6
+ *   powers        a byte s for 32 dims of a token, at [t / 16][t % 4][dim / 32]
+ *                 [t % 16 / 4] for token t of the page: they are code * 2^(s - 127).
+ *                 255, with codes of 0: 32 NaN.
+ *
+ * A step over it: oasis_rotate (queries, and keys that a tree's rows attend),
+ * oasis_score_blocks and oasis_select_topk as for any cache, oasis_tree_attn_q4,
+ * then oasis_append_tokens_q4 and oasis_update_summaries_q4. Block tables, lengths,
+ * trees and summaries are those of the bf16 cache. All pointers are device pointers,
+ * except pages (device memory or pinned host memory); pages, rows, summaries and
+ * workspaces are 16-byte aligned. What a call writes overlaps nothing else that it
+ * reads or writes (INVALID_ARG, but for oasis_rotate in place).
+ */
+OASIS_API size_t oasis_q4_page_bytes(const oasis_dims* dims);
+
+/*
+ * Rotary positions. Of a head's dims the first rotary_dim turn, in pairs (a, b):
+ *   (a, b) -> amplitude * (a cos - b sin, b cos + a sin),
+ *   angle of pair i at position p = 2 pi p turns[i], reduced in 64 bits.
+ * Pair i is dims i and i + rotary_dim / 2, or 2i and 2i + 1 where interleaved. The
+ * other dims stay as they are.
+ */
+typedef struct {
+  const double* turns;   /* device [rotary_dim / 2]: turns of a pair a position */
+  int32_t rotary_dim;    /* even, 2 to head_dim */
+  int32_t interleaved;   /* 0 or 1 */
+  double amplitude;      /* 1, or what a scaling for long contexts asks for */
+} oasis_rotary;
+
+/*
+ * The turns of each pair (host, [rotary_dim / 2]) and the amplitude (nullable), from
+ * the frequencies base^(-2i / rotary_dim) / (2 pi), scaled for long contexts:
+ *   PLAIN      as they are
+ *   LINEAR     divided by factor
+ *   STRETCHED  of the base base * factor^(rotary_dim / (rotary_dim - 2))
+ *   BY_TURNS   divided by factor where a pair makes at most `low` turns in first_len
+ *              positions, as they are from `high` turns on, between them in proportion
+ *              to the turns
+ *   BY_INDEX   the same in proportion to the pair's index, from the pair (rounded down)
+ *              that makes `high` turns to the one (rounded up) that makes `low`; the
+ *              amplitude is 0.1 ln(factor) + 1 where factor > 1, else 1 (as in the others)
+ * Arguments that a scaling does not name are not looked at.
+ */
+#define OASIS_ROTARY_PLAIN 0
+#define OASIS_ROTARY_LINEAR 1
+#define OASIS_ROTARY_STRETCHED 2
+#define OASIS_ROTARY_BY_TURNS 3
+#define OASIS_ROTARY_BY_INDEX 4
+OASIS_API oasis_status oasis_rotary_turns(int32_t rotary_dim, double base, int32_t scaling, double factor,
+                                          double first_len, double low, double high, double* turns, double* amplitude);
+
+/*
+ * Rotary positions of query and key rows, in one launch: for every request r, row
+ * t < num_tokens and head, q_out / k_out = the row turned to position positions[r][t]
+ * (int32 [R][T]; NULL: ctx_len[r] + t, a length below 0 counting as 0). Row (r, t) of
+ * q begins q_stride elements after row (r, t - 1), so that rows may lie in the output
+ * of a joint projection; a row holds its heads [Hq][d] (k: [Hkv][d]) densely. Strides are
+ * multiples of 8. q or k may be NULL (not both). An output may be its own input (the
+ * same address and stride); outputs and inputs of one stride may lie side by side.
+ * inverse != 0 turns back, by the negative angle and with the same amplitude: the
+ * gradient of the rows from that of the turned ones. Sines and cosines are rounded to
+ * 32 bits, products and sums in 32 bits, to bf16 once.
+ */
+OASIS_API oasis_status oasis_rotate(const oasis_dims* dims, const oasis_rotary* rotary, int32_t num_tokens,
+                                    const int32_t* positions, const int32_t* ctx_len, int32_t inverse,
+                                    const uint16_t* q, int64_t q_stride, uint16_t* q_out, int64_t q_out_stride,
+                                    const uint16_t* k, int64_t k_stride, uint16_t* k_out, int64_t k_out_stride,
+                                    void* stream);
+
+/*
+ * oasis_append_tokens into 4-bit pages, with the same path, path_len and lengths; rows
+ * of new_k and new_v [R][num_tokens] are k_stride and v_stride elements apart (as in
+ * oasis_rotate). rotary (nullable): the keys are turned to their position in the cache,
+ * ctx_len[r] + i, first, in 64 bits up to their code. Each 32 dims of a token get the
+ * smallest power 2^e, e in [-126, 125], with max |x| <= 7 * 2^e (125 where none is), and
+ * each dim the nearest code, of two as near the even one; beyond 6 it is 6. A NaN or an
+ * infinity among them: 32 NaN.
+ * read_k, read_v (nullable, bf16 [R][num_tokens][Hkv][d]): row (r, i) = the row appended
+ * at ctx_len[r] + i as the cache holds it, for a chunk's attention among its own rows.
+ * Rows that were not appended are left as they were.
+ */
+OASIS_API oasis_status oasis_append_tokens_q4(const oasis_dims* dims, const oasis_rotary* rotary,
+                                              const uint16_t* new_k, int64_t k_stride, const uint16_t* new_v,
+                                              int64_t v_stride, int32_t num_tokens, const int32_t* path,
+                                              const int32_t* path_len, uint8_t* k_pages, uint8_t* v_pages,
+                                              int64_t num_pages, const int32_t* block_table, const int32_t* ctx_len,
+                                              int32_t* new_ctx_len, uint16_t* read_k, uint16_t* read_v, void* stream);
+
+/*
+ * Compressed keys of 4-bit pages: oasis_update_summaries, and with prev_ctx_len NULL
+ * oasis_build_summaries (max_new_blocks is not looked at then), of the keys as the cache
+ * holds them. Exact. NaN keys do not count (a coordinate of nothing but NaN: kmax
+ * -infinity, kmin infinity).
+ */
+OASIS_API oasis_status oasis_update_summaries_q4(const oasis_dims* dims, const uint8_t* k_pages, int64_t num_pages,
+                                                 const int32_t* block_table, const int32_t* prev_ctx_len,
+                                                 const int32_t* ctx_len, int32_t max_new_blocks, uint16_t* kmax,
+                                                 uint16_t* kmin, void* stream);
+
+/*
+ * Attention over the 4-bit cache: oasis_tree_attn, over the values that the pages stand
+ * for. sel, sel_count and k (the output of oasis_select_topk, 1 <= k <= 65536): of the
+ * cache each KV head attends the blocks sel[r][h][0..sel_count) and the local block,
+ * read from the pages; ids outside [0, n_cand_r) are left out. sel and sel_count NULL
+ * and k = 0: every block. tree_k and tree_v both NULL: the T rows attend the cache
+ * alone (parent is not looked at), each without a mask among them, as in
+ * oasis_sparse_decode_attn. A row without an attended token gives out = 0, lse = -inf.
+ * A NaN in the cache reaches the rows that attend its token. Values below 2^-96 lose
+ * precision.
+ * workspace: oasis_tree_attn_q4_workspace_bytes (0: may be NULL); calls that run at
+ * the same time need separate workspaces.
+ */
+OASIS_API size_t oasis_tree_attn_q4_workspace_bytes(const oasis_dims* dims, int32_t num_q_tokens, int32_t k);
+OASIS_API oasis_status oasis_tree_attn_q4(const oasis_dims* dims, const uint16_t* q, int32_t num_q_tokens,
+                                          const uint8_t* k_pages, const uint8_t* v_pages, int64_t num_pages,
+                                          const int32_t* block_table, const int32_t* ctx_len, const int32_t* sel,
+                                          const int32_t* sel_count, int32_t k, const uint16_t* tree_k,
+                                          const uint16_t* tree_v, const int32_t* parent, const int32_t* tree_len,
+                                          float scale, uint16_t* out, float* lse, void* workspace,
+                                          size_t workspace_bytes, void* stream);
 
 /*
  * Native step issuer for the layer-pipelined schedule (paper §4.2.2, the

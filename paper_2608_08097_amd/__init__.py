@@ -16,4 +16,7 @@ from ._lib import (  # noqa: F401
     PLAN_ON_PREDICTION, oasis_pipeline_set_fused_prediction, FUSED_PREDICTION_AUTO, FUSED_PREDICTION_OFF,
     FUSED_PREDICTION_ON, oasis_tree_attn, oasis_tree_attn_workspace_bytes, oasis_sparse_tree_attn,
     oasis_sparse_tree_attn_workspace_bytes, oasis_verify_drafts, oasis_verify_workspace_bytes, oasis_append_tokens,
+    OasisRotary, Rotary, oasis_rotary_turns, ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_STRETCHED, ROTARY_BY_TURNS, ROTARY_BY_INDEX,
+    oasis_rotate, oasis_q4_page_bytes, oasis_append_tokens_q4, oasis_update_summaries_q4,
+    oasis_tree_attn_q4_workspace_bytes, oasis_tree_attn_q4,
 )

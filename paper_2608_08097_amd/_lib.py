@@ -35,6 +35,8 @@ EXPORTS = (
     "oasis_union_selection",
     "oasis_tree_attn_workspace_bytes", "oasis_tree_attn", "oasis_sparse_tree_attn_workspace_bytes",
     "oasis_sparse_tree_attn", "oasis_verify_workspace_bytes", "oasis_verify_drafts", "oasis_append_tokens",
+    "oasis_q4_page_bytes", "oasis_rotary_turns", "oasis_rotate", "oasis_append_tokens_q4", "oasis_update_summaries_q4",
+    "oasis_tree_attn_q4_workspace_bytes", "oasis_tree_attn_q4",
     "oasis_pipeline_create", "oasis_pipeline_set_layer", "oasis_pipeline_set_local_source",
     "oasis_pipeline_set_plan_stream", "oasis_pipeline_set_fused_prediction", "oasis_pipeline_step",
     "oasis_pipeline_join", "oasis_pipeline_check", "oasis_pipeline_set_wait_limit",
@@ -62,6 +64,11 @@ class OasisLayerBuffers(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("kmax", "kmin", "scores", "sel", "sel_count", "slot_map",
                                                "slot_stamp", "pool_k", "pool_v", "moved", "out", "lse",
                                                "workspace")] + [("workspace_bytes", ctypes.c_size_t)]
+
+
+class OasisRotary(ctypes.Structure):
+    _fields_ = [("turns", ctypes.c_void_p), ("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("amplitude", ctypes.c_double)]
 
 
 def dims(num_reqs, num_q_heads, num_kv_heads, head_dim, block_size, max_blocks) -> OasisDims:
@@ -137,6 +144,23 @@ def lib() -> ctypes.CDLL:
                                           _P]
         L.oasis_append_tokens.restype = _I32
         L.oasis_append_tokens.argtypes = [_DIMS, _P, _P, _I32, _P, _P, _P, _P, _I64, _P, _P, _P, _P]
+        rot, f64 = ctypes.POINTER(OasisRotary), ctypes.c_double
+        L.oasis_q4_page_bytes.restype = _SZ
+        L.oasis_q4_page_bytes.argtypes = [_DIMS]
+        L.oasis_rotary_turns.restype = _I32
+        L.oasis_rotary_turns.argtypes = [_I32, f64, _I32, f64, f64, f64, f64, _P, ctypes.POINTER(f64)]
+        L.oasis_rotate.restype = _I32
+        L.oasis_rotate.argtypes = [_DIMS, rot, _I32, _P, _P, _I32, _P, _I64, _P, _I64, _P, _I64, _P, _I64, _P]
+        L.oasis_append_tokens_q4.restype = _I32
+        L.oasis_append_tokens_q4.argtypes = [_DIMS, rot, _P, _I64, _P, _I64, _I32, _P, _P, _P, _P, _I64, _P, _P, _P, _P,
+                                             _P, _P]
+        L.oasis_update_summaries_q4.restype = _I32
+        L.oasis_update_summaries_q4.argtypes = [_DIMS, _P, _I64, _P, _P, _P, _I32, _P, _P, _P]
+        L.oasis_tree_attn_q4_workspace_bytes.restype = _SZ
+        L.oasis_tree_attn_q4_workspace_bytes.argtypes = [_DIMS, _I32, _I32]
+        L.oasis_tree_attn_q4.restype = _I32
+        L.oasis_tree_attn_q4.argtypes = [_DIMS, _P, _I32, _P, _P, _I64, _P, _P, _P, _P, _I32, _P, _P, _P, _P,
+                                         ctypes.c_float, _P, _P, _P, _SZ, _P]
         L.oasis_pipeline_create.restype = _I32
         L.oasis_pipeline_create.argtypes = [_DIMS, _I32, _I32, _I32, _I32, _I32, ctypes.c_float, _P, _P, _I64, _P,
                                             _I32, _P, _P, ctypes.POINTER(_P)]
@@ -184,7 +208,8 @@ def _bind_fast(L: ctypes.CDLL) -> None:
     try:
         fast = _load_fast()
         built_for = fast.abi_version
-        bind_drafts = fast.bind_drafts if built_for == ABI_VERSION else None
+        fits = built_for == ABI_VERSION
+        bind_drafts, bind_q4 = (fast.bind_drafts, fast.bind_q4) if fits else (None, None)
     except (ImportError, AttributeError) as e:
         warnings.warn(f"native marshalling not loaded ({e}): calls go through the slower Python binding. {_BUILD_HINT}",
                       RuntimeWarning, stacklevel=2)
@@ -198,6 +223,8 @@ def _bind_fast(L: ctypes.CDLL) -> None:
         L.oasis_stage_blocks)))
     bind_drafts(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
         L.oasis_tree_attn, L.oasis_sparse_tree_attn, L.oasis_verify_drafts, L.oasis_append_tokens)))
+    bind_q4(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
+        L.oasis_rotate, L.oasis_append_tokens_q4, L.oasis_update_summaries_q4, L.oasis_tree_attn_q4)))
     _fast = fast
 
 
@@ -628,6 +655,194 @@ def oasis_append_tokens(d: OasisDims, new_k, new_v, num_tokens: int, path, path_
         _host_or_dev(k_pages, "k_pages", _BF16), _host_or_dev(v_pages, "v_pages", _BF16), _pages(d, k_pages, "k_pages"),
         _dev(block_table, "block_table", _I32T), _dev(ctx_len, "ctx_len", _I32T),
         _dev(new_ctx_len, "new_ctx_len", _I32T, nullable=True), _stream(stream)))
+
+
+# --- the cache in four bits --------------------------------------------------------
+
+ROTARY_PLAIN = 0      # OASIS_ROTARY_PLAIN
+ROTARY_LINEAR = 1     # OASIS_ROTARY_LINEAR
+ROTARY_STRETCHED = 2  # OASIS_ROTARY_STRETCHED
+ROTARY_BY_TURNS = 3   # OASIS_ROTARY_BY_TURNS
+ROTARY_BY_INDEX = 4   # OASIS_ROTARY_BY_INDEX
+
+
+def oasis_rotary_turns(rotary_dim: int, base: float = 10000.0, scaling: int = ROTARY_PLAIN, factor: float = 1.0,
+                       first_len: float = 0.0, low: float = 1.0, high: float = 32.0) -> tuple[list[float], float]:
+    """Turns of each pair a position, and the amplitude, of rotary positions scaled for long contexts."""
+    n = int(rotary_dim)
+    turns, amplitude = (ctypes.c_double * max(1, n // 2))(), ctypes.c_double()
+    _check("oasis_rotary_turns", lib().oasis_rotary_turns(n, base, int(scaling), factor, first_len, low, high, turns,
+                                                          ctypes.byref(amplitude)))
+    return list(turns), amplitude.value
+
+
+class Rotary:
+    """Rotary positions: the table of turns on the device, and how pairs lie in a head. Kept by the caller, for as long
+    as calls that it was given to are under way."""
+
+    def __init__(self, rotary_dim: int = 128, base: float = 10000.0, interleaved: bool = False,
+                 scaling: int = ROTARY_PLAIN, factor: float = 1.0, first_len: float = 0.0, low: float = 1.0,
+                 high: float = 32.0, device: str | torch.device = "cuda"):
+        turns, amplitude = oasis_rotary_turns(rotary_dim, base, scaling, factor, first_len, low, high)
+        self._set(torch.tensor(turns, dtype=torch.float64, device=device), interleaved, amplitude)
+
+    @classmethod
+    def from_turns(cls, turns: torch.Tensor, interleaved: bool = False, amplitude: float = 1.0) -> "Rotary":
+        """From a float64 device tensor of turns a position, one for each pair."""
+        self = cls.__new__(cls)
+        self._set(turns, interleaved, amplitude)
+        return self
+
+    def _set(self, turns, interleaved, amplitude):
+        self.turns = turns
+        self.struct = OasisRotary(_dev(turns, "turns", (torch.float64,)) if turns.is_cuda else None, 2 * turns.numel(),
+                                  1 if interleaved else 0, float(amplitude))
+
+
+def _rows(t: torch.Tensor, name: str, shape):
+    """Address and row stride of heads [R][T][H][d]: contiguous, or 4-dimensional with dense heads and rows evenly
+    spaced (a slice of a joint projection's output)."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if t.dtype not in _BF16:
+        raise TypeError(f"{name}: dtype {t.dtype} not in {_BF16}")
+    R, T, H, D = shape
+    if t.is_contiguous():
+        _need(t, R * T * H * D, name)
+        return t.data_ptr(), H * D
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, {tuple(shape)} expected")
+    row = t.stride(1) if T > 1 else (t.stride(0) if R > 1 else H * D)
+    if (D > 1 and t.stride(3) != 1) or (H > 1 and t.stride(2) != D) or (R > 1 and t.stride(0) != T * row):
+        raise ValueError(f"{name}: heads must be contiguous and rows evenly spaced")
+    return t.data_ptr(), row
+
+
+def oasis_q4_page_bytes(d: OasisDims) -> int:
+    """Bytes of a 4-bit page: pages are uint8 tensors of whole ones, [num_pages][page bytes]."""
+    return int(lib().oasis_q4_page_bytes(ctypes.byref(d)))
+
+
+def _q4_pages(d: OasisDims, t: torch.Tensor, name: str) -> int:
+    per = d.num_kv_heads * d.block_size * 68
+    if t.dim() < 1 or per < 1 or t.numel() % per:
+        raise ValueError(f"{name}: not whole pages of {per} bytes")
+    return t.numel() // per
+
+
+_U8 = (torch.uint8,)
+
+
+def oasis_rotate(d: OasisDims, rotary: Rotary, num_tokens: int, positions, ctx_len, q, q_out, k, k_out,
+                 inverse: bool = False, stream=None) -> None:
+    """Rotary positions of query rows [R][T][Hq][d] and key rows [R][T][Hkv][d] (either may be None) at positions [R][T]
+    (None: ctx_len[r] + t); an output may be its own input. inverse: backwards, which takes a gradient of the turned
+    rows to that of the rows."""
+    if _fast is not None and type(d) is OasisDims:
+        st = _fast.rotate(ctypes.addressof(d), ctypes.addressof(rotary.struct), rotary.turns, num_tokens, positions, ctx_len,
+                          q, q_out, k, k_out, inverse, _handle(stream))
+        if st is not None:
+            return _check("oasis_rotate", st)
+    R, T, D = d.num_reqs, int(num_tokens), d.head_dim
+    _need(positions, R * T, "positions")
+    _need(ctx_len, R, "ctx_len")
+    if (q is None) != (q_out is None) or (k is None) != (k_out is None):
+        raise ValueError("q and q_out, and k and k_out, go together")
+    args = []
+    for t, n, h in ((q, "q", d.num_q_heads), (q_out, "q_out", d.num_q_heads), (k, "k", d.num_kv_heads),
+                    (k_out, "k_out", d.num_kv_heads)):
+        args += (None, 0) if t is None else _rows(t, n, (R, T, h, D))
+    _one_device(turns=rotary.turns, positions=positions, ctx_len=ctx_len, q=q, q_out=q_out, k=k, k_out=k_out)
+    _check("oasis_rotate", lib().oasis_rotate(
+        ctypes.byref(d), ctypes.byref(rotary.struct), T, _dev(positions, "positions", _I32T, nullable=True),
+        _dev(ctx_len, "ctx_len", _I32T, nullable=True), 1 if inverse else 0, *args, _stream(stream)))
+
+
+def oasis_append_tokens_q4(d: OasisDims, rotary: Rotary | None, new_k, new_v, num_tokens: int, path, path_len, k_pages,
+                           v_pages, block_table, ctx_len, new_ctx_len, read_k=None, read_v=None, stream=None) -> None:
+    """oasis_append_tokens into 4-bit pages (uint8), the keys turned to their positions first (rotary None: as they
+    are); read_k and read_v receive the rows as the cache holds them."""
+    if _fast is not None and type(d) is OasisDims:
+        st = _fast.append_tokens_q4(ctypes.addressof(d), 0 if rotary is None else ctypes.addressof(rotary.struct),
+                                    None if rotary is None else rotary.turns, new_k, new_v, num_tokens, path, path_len,
+                                    k_pages, v_pages, block_table, ctx_len, new_ctx_len, read_k, read_v, _handle(stream))
+        if st is not None:
+            return _check("oasis_append_tokens_q4", st)
+    if k_pages.shape != v_pages.shape:
+        raise ValueError("k_pages and v_pages differ in shape")
+    R, H, D, N = d.num_reqs, d.num_kv_heads, d.head_dim, int(num_tokens)
+    for t, n, name in ((path, R * N, "path"), (path_len, R, "path_len"), (block_table, R * d.max_blocks, "block_table"),
+                       (ctx_len, R, "ctx_len"), (new_ctx_len, R, "new_ctx_len"), (read_k, R * N * H * D, "read_k"),
+                       (read_v, R * N * H * D, "read_v")):
+        _need(t, n, name)
+    rows = (*_rows(new_k, "new_k", (R, N, H, D)), *_rows(new_v, "new_v", (R, N, H, D)))
+    _one_device(turns=None if rotary is None else rotary.turns, new_k=new_k, new_v=new_v, path=path, path_len=path_len,
+                k_pages=k_pages, v_pages=v_pages, block_table=block_table, ctx_len=ctx_len, new_ctx_len=new_ctx_len,
+                read_k=read_k, read_v=read_v)
+    _check("oasis_append_tokens_q4", lib().oasis_append_tokens_q4(
+        ctypes.byref(d), None if rotary is None else ctypes.byref(rotary.struct), *rows, N,
+        _dev(path, "path", _I32T, nullable=True), _dev(path_len, "path_len", _I32T, nullable=True),
+        _host_or_dev(k_pages, "k_pages", _U8), _host_or_dev(v_pages, "v_pages", _U8), _q4_pages(d, k_pages, "k_pages"),
+        _dev(block_table, "block_table", _I32T), _dev(ctx_len, "ctx_len", _I32T),
+        _dev(new_ctx_len, "new_ctx_len", _I32T, nullable=True), _dev(read_k, "read_k", _BF16, nullable=True),
+        _dev(read_v, "read_v", _BF16, nullable=True), _stream(stream)))
+
+
+def oasis_update_summaries_q4(d: OasisDims, k_pages, block_table, prev_ctx_len, ctx_len, max_new_blocks: int, kmax, kmin,
+                              stream=None) -> None:
+    """Compressed keys of 4-bit pages: of the blocks completed since prev_ctx_len, or (None) of every block."""
+    if _fast is not None and type(d) is OasisDims:
+        st = _fast.update_summaries_q4(ctypes.addressof(d), k_pages, block_table, prev_ctx_len, ctx_len, max_new_blocks,
+                                       kmax, kmin, _handle(stream))
+        if st is not None:
+            return _check("oasis_update_summaries_q4", st)
+    R, H, NB, D = d.num_reqs, d.num_kv_heads, d.max_blocks, d.head_dim
+    for t, n, name in ((block_table, R * NB, "block_table"), (prev_ctx_len, R, "prev_ctx_len"), (ctx_len, R, "ctx_len"),
+                       (kmax, R * H * NB * D, "kmax"), (kmin, R * H * NB * D, "kmin")):
+        _need(t, n, name)
+    _one_device(k_pages=k_pages, block_table=block_table, prev_ctx_len=prev_ctx_len, ctx_len=ctx_len, kmax=kmax, kmin=kmin)
+    _check("oasis_update_summaries_q4", lib().oasis_update_summaries_q4(
+        ctypes.byref(d), _host_or_dev(k_pages, "k_pages", _U8), _q4_pages(d, k_pages, "k_pages"),
+        _dev(block_table, "block_table", _I32T), _dev(prev_ctx_len, "prev_ctx_len", _I32T, nullable=True),
+        _dev(ctx_len, "ctx_len", _I32T), int(max_new_blocks), _dev(kmax, "kmax", _BF16), _dev(kmin, "kmin", _BF16),
+        _stream(stream)))
+
+
+def oasis_tree_attn_q4_workspace_bytes(d: OasisDims, num_q_tokens: int, k: int) -> int:
+    return int(lib().oasis_tree_attn_q4_workspace_bytes(ctypes.byref(d), int(num_q_tokens), int(k)))
+
+
+def oasis_tree_attn_q4(d: OasisDims, q, num_q_tokens: int, k_pages, v_pages, block_table, ctx_len, sel, sel_count, k: int,
+                       tree_k, tree_v, parent, tree_len, scale: float | None, out, lse, workspace, stream=None) -> None:
+    """Attention over the 4-bit cache: of the blocks selected for each KV head (sel, sel_count, k: the selection's
+    output) and the local one, or (None, None, 0) of every block, and of a drafted tree's rows (tree_k and tree_v None:
+    the cache alone; parent None: a chain; tree_len None: every row)."""
+    if _fast is not None and type(d) is OasisDims:
+        st = _fast.tree_attn_q4(ctypes.addressof(d), q, num_q_tokens, k_pages, v_pages, block_table, sel, sel_count, k, ctx_len,
+                                tree_k, tree_v, parent, tree_len, scale, out, lse, workspace, _handle(stream))
+        if st is not None:
+            return _check("oasis_tree_attn_q4", st)
+    if scale is None:
+        scale = 1.0 / math.sqrt(d.head_dim)
+    if k_pages.shape != v_pages.shape:
+        raise ValueError("k_pages and v_pages differ in shape")
+    RH = d.num_reqs * d.num_kv_heads
+    _tree_needs(d, int(num_q_tokens), q, ctx_len, tree_k, tree_v, parent, tree_len, out, lse)
+    _need(block_table, d.num_reqs * d.max_blocks, "block_table")
+    _need(sel, RH * int(k), "sel")
+    _need(sel_count, RH, "sel_count")
+    _one_device(q=q, k_pages=k_pages, v_pages=v_pages, block_table=block_table, ctx_len=ctx_len, sel=sel,
+                sel_count=sel_count, tree_k=tree_k, tree_v=tree_v, parent=parent, tree_len=tree_len, out=out, lse=lse,
+                workspace=workspace)
+    _check("oasis_tree_attn_q4", lib().oasis_tree_attn_q4(
+        ctypes.byref(d), _dev(q, "q", _BF16), int(num_q_tokens), _host_or_dev(k_pages, "k_pages", _U8),
+        _host_or_dev(v_pages, "v_pages", _U8), _q4_pages(d, k_pages, "k_pages"), _dev(block_table, "block_table", _I32T),
+        _dev(ctx_len, "ctx_len", _I32T), _dev(sel, "sel", _I32T, nullable=True),
+        _dev(sel_count, "sel_count", _I32T, nullable=True), int(k), _dev(tree_k, "tree_k", _BF16, nullable=True),
+        _dev(tree_v, "tree_v", _BF16, nullable=True), _dev(parent, "parent", _I32T, nullable=True),
+        _dev(tree_len, "tree_len", _I32T, nullable=True), float(scale), _dev(out, "out", _BF16),
+        _dev(lse, "lse", _F32, nullable=True), _dev(workspace, "workspace", _U8, nullable=True), _bytes(workspace),
+        _stream(stream)))
 
 
 # --- native step issuer --------------------------------------------------------

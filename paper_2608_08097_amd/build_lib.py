@@ -38,11 +38,11 @@ def flags() -> list[str]:
     ]
 
 
-# Extra compiler flags of single sources. attn.hip and tree_attn.hip: keep MFMA
+# Extra compiler flags of single sources. The attention kernels: keep MFMA
 # accumulators and results in VGPRs; otherwise the compiler parks the attention's
 # accumulators in AGPRs and copies all 64 of them to VGPRs on every unit for the
 # rare rescale path.
-FILE_FLAGS = {f: ["-mllvm", "-amdgpu-mfma-vgpr-form"] for f in ("attn.hip", "tree_attn.hip")}
+FILE_FLAGS = {f: ["-mllvm", "-amdgpu-mfma-vgpr-form"] for f in ("attn.hip", "tree_attn.hip", "attn_q4.hip")}
 
 
 FASTCALL_PATH = os.path.join(PKG_DIR, "_fastcall.so")

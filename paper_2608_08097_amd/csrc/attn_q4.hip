@@ -1,0 +1,474 @@
+// Attention of a step's rows, a drafted tree or not, over the 4-bit paged cache: over
+// every cached token, or over the blocks selected for each KV head, read where they lie.
+//
+// out = softmax(scale q K^T) V in one pass with a running maximum and sum, as tree_attn.hip,
+// whose row references, merge and treatment of the tree's wild values are used here. A unit
+// is 64 tokens of one KV head, four sub-blocks of 16; for one 16-row tile
+//   S^T (tokens x rows) = K . Q^T     16 of v_mfma_f32_16x16x32_bf16
+//   O^T (d x rows)     += V^T . P^T   16 of them
+//
+// Keys go straight from memory into the first product's operand: a lane has 32 dims of a
+// token in 16 bytes, whose codes the hardware turns into bf16 with the token's power, two
+// at a time; the queries are dealt to the same dims. The tokens are dealt to MFMA rows so
+// that lane (g, n) ends up with row n's scores of sub-block g's 16 tokens.
+//
+// Values need 16 tokens of one dim in a lane: their codes go through LDS, 4 KB a wave and
+// unit, and come back through the transposing read of 16 x 16 codes. Their powers differ
+// from token to token of a lane and cannot go into that conversion: the probabilities take
+// them up, once for each group of dims, which rounds nothing (a power of two).
+//
+// The tree's rows, keys and values in bf16, are a unit of their own in the last split of
+// every pair.
+#include "tree_core.h"
+#include "q4_internal.h"
+
+namespace oasis {
+namespace {
+
+constexpr int kQW = kQ4Waves;
+constexpr int kUnitTokens = kQ4Unit;  // four sub-blocks of 16
+
+struct Q4Item {
+  int r, h, rh, split, row0, tlen, ctx;
+  const int32_t* tab;   // the request's block table
+  const int32_t* sel;   // the pair's selection, `selected` of them
+  int selected;
+  long long tree_row, tree_base;  // elements between the tree's rows, and to this head's first one
+};
+
+template <bool SELECT>
+__device__ __forceinline__ bool q4_setup(const AttnQ4Args& a, int group_rows, Q4Item& t) {
+  int group, rs;
+  if (!SELECT && a.by_length) {
+    rs = tree_item_spread(blockIdx.x, a, a.R * a.Hkv * a.nsplit, group);
+    if (rs < 0) return false;
+  } else {
+    const int item = tree_item(blockIdx.x, a.R * a.Hkv * a.nsplit * a.groups);
+    if (item < 0) return false;
+    rs = a.by_groups(item);
+    group = item - rs * a.groups;
+  }
+  t.row0 = group * group_rows;
+  t.rh = a.by_nsplit(rs);
+  t.split = rs - t.rh * a.nsplit;
+  t.r = a.by_hkv(t.rh);
+  t.h = t.rh - t.r * a.Hkv;
+  if (!SELECT && a.by_length) {
+    t.r = request_of_rank(a.ctx_len, a.R, t.r, t.ctx);
+    t.rh = t.r * a.Hkv + t.h;
+  } else {
+    t.ctx = a.ctx_len[t.r];
+  }
+  t.tab = a.table + (long long)t.r * a.NBmax;
+  t.selected = 0;
+  if constexpr (SELECT) {
+    t.sel = a.sel + (long long)t.rh * a.k_sel;
+    const int n = a.sel_count[t.rh];
+    t.selected = n < 0 ? 0 : (n > a.k_sel ? a.k_sel : n);
+  }
+  t.tree_row = (long long)a.Hkv * kHeadDim;
+  t.tree_base = (long long)t.r * a.T * t.tree_row + (long long)t.h * kHeadDim;
+  t.tlen = tree_length(a, t.r);
+  return t.row0 < t.tlen * a.G;  // else no row of this group is in use
+}
+
+// Entry b of the pair's list of blocks: its page, and in `count` its attended tokens (0: none
+// such, and page 0 stands in).
+template <int BS, bool SELECT>
+__device__ __forceinline__ void q4_block(const AttnQ4Args& a, const Q4Item& t, const Ctx& c, int b, int& page, int& count) {
+  int id = b;
+  bool ok;
+  if constexpr (SELECT) {
+    ok = b < t.selected;
+    id = ok ? t.sel[b] : c.n_cand;
+    ok = ok ? id >= 0 && id < c.n_cand : b == t.selected && c.nb > 0;
+  } else {
+    ok = b < c.nb;
+  }
+  const int raw = ok ? t.tab[id] : -1;
+  ok = raw >= 0 && raw < a.num_pages;
+  page = ok ? raw : 0;
+  count = ok ? (id == c.n_cand ? c.local_len : BS) : 0;
+}
+
+__device__ __forceinline__ float power_f32(uint32_t w, int u) { return __uint_as_float((w >> (8 * u) & 255u) << 23); }
+
+template <int SEL>
+__device__ __forceinline__ uint32_t two_bf16(uint32_t codes, float scale) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, SEL));
+}
+__device__ __forceinline__ bf16x8 eight_bf16(uint32_t codes, float scale) {
+  const u32x4 v = {two_bf16<0>(codes, scale), two_bf16<1>(codes, scale), two_bf16<2>(codes, scale),
+                   two_bf16<3>(codes, scale)};
+  return as_bf16x8(v);
+}
+
+// Q^T operand of the tile whose first row is `first`: lane (g, n) holds row first + n, dims
+// 32 g + 8 st .. +7 of step st (signs and a scale of 0 as load_q of tree_attn.hip).
+__device__ __forceinline__ void load_q4_queries(const TreeAttnArgs& a, const Q4Item& t, int first, int g, int n,
+                                                bf16x8 (&qb)[4]) {
+  const int row = first + n;
+  const int tq = row < a.rows ? a.by_g(row) : 0;
+  const int qh = t.h * a.G + (row < a.rows ? row - tq * a.G : 0);
+  const uint16_t* qrow = a.q + (((long long)t.r * a.T + tq) * a.Hq + qh) * kHeadDim;
+#pragma unroll
+  for (int st = 0; st < 4; ++st) {
+    const u32x4 x = ldg16(qrow + g * 32 + st * 8);
+    u32x4 y;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) y[w] = row < a.rows ? (x[w] & a.q_and) ^ a.q_xor : 0u;
+    qb[st] = as_bf16x8(y);
+  }
+}
+
+// The online softmax of tree_attn.hip over a lane's 16 scores: probabilities not yet rounded.
+__device__ __forceinline__ float exp16(const f32x4 (&s)[4], float scale, float m_neg, float (&p)[16]) {
+  float sum[4];
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) p[4 * u + e] = fast_exp2(__builtin_fmaf(s[u][e], scale, m_neg));
+    sum[u] = (p[4 * u] + p[4 * u + 1]) + (p[4 * u + 2] + p[4 * u + 3]);
+  }
+  return (sum[0] + sum[1]) + (sum[2] + sum[3]);
+}
+__device__ __forceinline__ void softmax16(const f32x4 (&s)[4], float scale, float top, float& m_neg, float& l_part,
+                                          f32x4 (&acc)[8], float (&p)[16]) {
+  float psum = exp16(s, scale, m_neg, p);
+  const uint64_t past = __builtin_amdgcn_ballot_w64(!(psum <= top));
+  if (__builtin_expect(past != 0, 0)) {
+    const uint64_t rows = past | past >> 16 | past >> 32 | past >> 48;
+    const bool mine = rows >> (threadIdx.x & 15) & 1;
+    float m = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) m = fmaxf(m, fmaxf(fmaxf(s[u][0], s[u][1]), fmaxf(s[u][2], s[u][3])));
+    m *= scale;
+    m = fmaxf(m, __shfl_xor(m, 16));
+    m = fmaxf(fmaxf(m, __shfl_xor(m, 32)) + (float)(9 - __builtin_amdgcn_frexp_expf(top)), -m_neg);
+    m = mine ? m : -m_neg;
+    const float alpha = m == -INFINITY ? 1.f : fast_exp2(-m_neg - m);
+    l_part *= alpha;
+#pragma unroll
+    for (int dt = 0; dt < 8; ++dt) acc[dt] *= alpha;
+    m_neg = -m;
+    psum = exp16(s, scale, m == -INFINITY ? 0.f : m_neg, p);
+  }
+  l_part += psum;
+}
+
+template <int NT, int BS, bool SELECT>
+__global__ __launch_bounds__(kQW * 64) void q4_attn_kernel(AttnQ4Args a) {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63;
+  const int g = lane >> 4;
+  const int i = lane & 15;
+  Q4Item t;
+  if (!q4_setup<SELECT>(a, NT * 16, t)) return;
+  const Ctx c = ctx_blocks(t.ctx, BS, a.NBmax);
+  constexpr int kPer = kUnitTokens / BS;  // blocks of a unit
+  const int blocks = SELECT ? t.selected + (c.nb > 0) : c.nb;
+  const int nu = (blocks + kPer - 1) / kPer;
+  const int each = a.by_nsplit(nu), more = nu - each * a.nsplit;  // the first `more` splits have one more
+  const int u_begin = t.split * each + min(t.split, more);
+  const int u_end = u_begin + each + (t.split < more);
+
+  // A wave's units are u_begin + wave + n * kQW; for kChunk of them at a time lane e holds
+  // block e % kPer of unit e / kPer.
+  constexpr int kChunk = 64 / kPer;
+  const int u_first = u_begin + wave;
+  const int nt = u_first < u_end ? (u_end - u_first + kQW - 1) / kQW : 0;
+  int n0 = 0, place, count;
+  uint64_t live;
+  auto chunk_set = [&]() __attribute__((always_inline)) {
+    const int n = n0 + lane / kPer;
+    if (n < nt) q4_block<BS, SELECT>(a, t, c, (u_first + n * kQW) * kPer + lane % kPer, place, count);
+    else place = count = 0;
+    live = __builtin_amdgcn_ballot_w64(count > 0);
+  };
+  // The wave's next unit with an attended token: where its first block's lane is, -1 without one.
+  auto next = [&]() __attribute__((always_inline)) {
+    while (!live && n0 + kChunk < nt) {
+      n0 += kChunk;
+      chunk_set();
+    }
+    if (!live) return -1;
+    const int p = __builtin_ctzll(live) / kPer * kPer;
+    live &= ~(((1ull << kPer) - 1) << p);
+    return p;
+  };
+  struct Loaded {
+    u32x4 k[4], v[4];       // codes: keys of tile u, values of sub-block u
+    uint32_t k_pow, v_pow;
+    int keep;               // attended tokens of sub-block g
+    bool whole;             // of every sub-block
+  };
+  const long long codes_h = (long long)t.h * BS * kQ4Codes;
+  const long long powers_h = (long long)a.Hkv * BS * kQ4Codes + (long long)t.h * BS * kQ4Powers;
+  Loaded u;
+  // (for a wave without a next unit the first unit's block 0 of page 0 stands in)
+  auto load_k = [&](int p) __attribute__((always_inline)) {
+    const int s = i >> 2;  // the sub-block of this lane's tokens
+    const int pg = __shfl(place, p < 0 ? 0 : p + (BS == 16 ? s : s >> 1));
+    const uint8_t* at = a.k4 + (p < 0 ? 0 : pg) * a.page_bytes;
+    const int sub = BS == 16 ? 0 : s & 1;
+    const uint8_t* codes = at + codes_h + sub * 1024 + (i & 3) * 64 + g * 16;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) u.k[q] = ldg16(codes + q * 256);
+    u.k_pow = *reinterpret_cast<const uint32_t*>(at + powers_h + sub * 64 + ((i & 3) * 4 + g) * 4);
+  };
+  auto load_v = [&](int p) __attribute__((always_inline)) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int pg = p < 0 ? 0 : __builtin_amdgcn_readlane(place, p + (BS == 16 ? q : q >> 1));
+      u.v[q] = ldg16(a.v4 + pg * a.page_bytes + codes_h + (BS == 16 ? 0 : q & 1) * 1024 + lane * 16);
+    }
+    const int from = p < 0 ? 0 : p + (BS == 16 ? g : g >> 1);
+    const int pg = p < 0 ? 0 : __shfl(place, from);
+    u.v_pow = *reinterpret_cast<const uint32_t*>(a.v4 + pg * a.page_bytes + powers_h + (BS == 16 ? 0 : g & 1) * 64 + i * 4);
+    const int n = p < 0 ? 0 : __shfl(count, from) - (BS == 16 ? 0 : (g & 1) * 16);
+    u.keep = n < 0 ? 0 : (n > 16 ? 16 : n);
+    u.whole = __builtin_amdgcn_ballot_w64(u.keep == 16) == ~0ull;
+  };
+
+  bf16x8 qb[NT][4];
+#pragma unroll
+  for (int v = 0; v < NT; ++v) load_q4_queries(a, t, t.row0 + v * 16, g, i, qb[v]);
+  float m_neg[NT], l_run[NT];
+  f32x4 acc[NT][8];
+#pragma unroll
+  for (int v = 0; v < NT; ++v) {
+    m_neg[v] = INFINITY;
+    l_run[v] = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < 8; ++dt) acc[v][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  constexpr int kRows = NT * 16;
+  constexpr int kPad = kHeadDim + 4;
+  __shared__ float s_m[kQW][kRows], s_l[kQW][kRows], s_ml[2][kRows];
+  __shared__ uint64_t s_anc[kTreeMaxTokens];
+  __shared__ int s_wild;
+  // a wave's values of a unit, its part of the tree's, and its rows at the end
+  __shared__ __align__(16) float s_o[kQW][kRows][kPad];
+  static_assert(sizeof(float) * kRows * kPad >= 8192, "half the tree's values");
+
+  // ---- the tree's own rows: one unit, of the last wave of the last split ----
+  const bool tree_split = t.split == a.nsplit - 1 && a.tree_k != nullptr;
+  bool wild = false;
+  if (tree_split && wave == kQW - 1) {
+    u32x4 tk[4][4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int j = min(16 * (i >> 2) + 4 * q + (i & 3), t.tlen - 1);
+#pragma unroll
+      for (int st = 0; st < 4; ++st) tk[q][st] = ldg16(a.tree_k + t.tree_base + j * t.tree_row + g * 32 + st * 8);
+    }
+    const uint64_t anc = ancestors(tree_parent(a, t.r, t.tlen, lane), t.tlen, lane);
+    s_anc[lane] = anc;
+    float p[NT][16];
+#pragma unroll
+    for (int v = 0; v < NT; ++v) {
+      f32x4 sc[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        sc[q] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int st = 0; st < 4; ++st)
+          sc[q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(tk[q][st]), qb[v][st], sc[q], 0, 0, 0);
+      }
+      const int row = t.row0 + v * 16 + i;
+      const int tq = row < a.rows ? a.by_g(row) : 0;
+      const uint32_t lo = __shfl((uint32_t)anc, tq), hi = __shfl((uint32_t)(anc >> 32), tq);
+      const uint32_t bits = (g < 2 ? lo : hi) >> (16 * (g & 1));
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sc[q][e] = bits >> (4 * q + e) & 1 ? sc[q][e] : -INFINITY;
+      softmax16(sc, a.scale_log2, a.top, m_neg[v], l_run[v], acc[v], p[v]);
+    }
+    u32x4* sv = reinterpret_cast<u32x4*>(&s_o[wave][0][0]);  // [dim][group of tokens], 8 tokens each
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      u32x4 tv[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int j = min(16 * g + 8 * half + e, t.tlen - 1);
+        tv[e] = ldg16(a.tree_v + t.tree_base + j * t.tree_row + i * 8);
+      }
+      transpose8(tv);
+      const int n = t.tlen - 16 * g - 8 * half;
+      clear_tokens(tv, n < 0 ? 0 : (n > 8 ? 8 : n));
+      wild |= take_wild(tv);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sv[(8 * i + j) * 4 + g] = tv[j];
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+      for (int dt = 0; dt < 8; ++dt) tv[dt] = sv[(16 * dt + i) * 4 + g];
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+      for (int v = 0; v < NT; ++v) {
+        bf16x8 pb;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) pb[e] = (__bf16)p[v][8 * half + e];
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt)
+          acc[v][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(tv[dt]), pb, acc[v][dt], 0, 0, 0);
+      }
+    }
+  }
+  if (threadIdx.x == (kQW - 1) * 64) s_wild = wild;
+
+  // ---- the cache ----
+  typedef int i32x2 __attribute__((ext_vector_type(2)));
+  char* sw = reinterpret_cast<char*>(&s_o[wave][0][0]);  // codes [sub-block][32 dims][16 tokens][16 bytes], powers
+  char* s_pow = sw + 4096;
+  chunk_set();
+  int cur = next();
+  load_k(cur);
+  load_v(cur);
+  while (cur >= 0) {
+    const int nxt = next();
+    // values into LDS
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      *reinterpret_cast<u32x4*>(sw + q * 1024 + (lane & 3) * 256 + (lane >> 2) * 16) = u.v[q];
+    const int keep = u.keep;
+    const bool whole = u.whole;
+    uint32_t v_pow = u.v_pow;
+    if (!whole) {  // token i / 4 + 4 u at byte u
+      uint32_t m = 0;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) m |= 4 * q + (i >> 2) < keep ? 0xFFu << (8 * q) : 0;
+      v_pow &= m;  // 0 times what an unused place holds stays 0
+    }
+    *reinterpret_cast<uint32_t*>(s_pow + g * 64 + i * 4) = v_pow;
+    // scores
+    f32x4 sc[NT][4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const float s = power_f32(u.k_pow, q);
+#pragma unroll
+      for (int v = 0; v < NT; ++v) sc[v][q] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int st = 0; st < 4; ++st) {
+        const bf16x8 kb = eight_bf16(u.k[q][st], s);
+#pragma unroll
+        for (int v = 0; v < NT; ++v) sc[v][q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kb, qb[v][st], sc[v][q], 0, 0, 0);
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    load_k(nxt);
+    load_v(nxt);
+    __builtin_amdgcn_sched_barrier(0);
+    float p[NT][16];
+#pragma unroll
+    for (int v = 0; v < NT; ++v) {
+      if (!whole) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sc[v][q][e] = 4 * q + e < keep ? sc[v][q][e] : -INFINITY;
+      }
+      softmax16(sc[v], a.scale_log2, a.top, m_neg[v], l_run[v], acc[v], p[v]);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    u32x4 pw[4];  // powers of tokens e + 4 u: group of dims, byte u
+#pragma unroll
+    for (int e = 0; e < 4; ++e) pw[e] = *reinterpret_cast<const u32x4*>(s_pow + g * 64 + e * 16);
+#pragma unroll
+    for (int gd = 0; gd < 4; ++gd) {
+      bf16x8 pb[NT][2];
+#pragma unroll
+      for (int v = 0; v < NT; ++v)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) pb[v][q >> 1][(q & 1) * 4 + e] = (__bf16)(p[v][4 * q + e] * power_f32(pw[e][gd], q));
+#pragma unroll
+      for (int d2 = 0; d2 < 2; ++d2) {
+        const int dt = 2 * gd + d2;
+        const i32x2 w = __builtin_amdgcn_ds_read_tr4_b64_v2i32(
+            (__attribute__((address_space(3))) i32x2*)(sw + g * 1024 + gd * 256 + i * 16 + d2 * 8));
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const bf16x8 vb = eight_bf16((uint32_t)w[half], 1.f);
+#pragma unroll
+          for (int v = 0; v < NT; ++v)
+            acc[v][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vb, pb[v][half], acc[v][dt], 0, 0, 0);
+        }
+      }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    cur = nxt;
+  }
+  float m_run[NT];
+#pragma unroll
+  for (int v = 0; v < NT; ++v) m_run[v] = finish_row(m_neg[v], l_run[v]);
+
+  // ---- merge the waves through LDS ----
+  if (g == 0) {
+#pragma unroll
+    for (int v = 0; v < NT; ++v) {
+      s_m[wave][v * 16 + i] = m_run[v];
+      s_l[wave][v * 16 + i] = l_run[v];
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int v = 0; v < NT; ++v) {
+    const int row = v * 16 + i;
+    float M = s_m[0][row];
+#pragma unroll
+    for (int w = 1; w < kQW; ++w) M = fmaxf(M, s_m[w][row]);
+    float S = 0.f;
+#pragma unroll
+    for (int w = 0; w < kQW; ++w) S += s_m[w][row] == -INFINITY ? 0.f : s_l[w][row] * fast_exp2(s_m[w][row] - M);
+    const float f = m_run[v] == -INFINITY ? 0.f : fast_exp2(m_run[v] - M);
+    if (wave == 0 && g == 0) {
+      s_ml[0][row] = M;
+      s_ml[1][row] = S;
+    }
+#pragma unroll
+    for (int dt = 0; dt < 8; ++dt) *reinterpret_cast<f32x4*>(&s_o[wave][row][16 * dt + 4 * g]) = acc[v][dt] * f;
+  }
+  __syncthreads();
+  const long long pbase = ((long long)t.rh * a.nsplit + t.split) * a.rows + t.row0;
+  const int last = min(t.tlen * a.G, a.rows) - t.row0;  // rows of this group in use
+  for (int pos = threadIdx.x; pos < kRows * (kHeadDim / 4); pos += kQW * 64) {
+    const int row = pos >> 5;
+    const int c4 = pos & 31;
+    if (row >= last) break;
+    f32x4 o = *reinterpret_cast<const f32x4*>(&s_o[0][row][c4 * 4]);
+#pragma unroll
+    for (int w = 1; w < kQW; ++w) o += *reinterpret_cast<const f32x4*>(&s_o[w][row][c4 * 4]);
+    if (s_wild) add_wild(a, t, s_anc[a.by_g(t.row0 + row)], c4, o);
+    if (a.nsplit == 1) {
+      write_row(a, t.r, t.h, t.row0 + row, c4, o, s_ml[0][row], s_ml[1][row]);
+    } else {
+      *reinterpret_cast<f32x4*>(a.part_o + (pbase + row) * kHeadDim + c4 * 4) = o;
+      if (c4 == 0) *reinterpret_cast<float2*>(a.part_ml + (pbase + row) * 2) = make_float2(s_ml[0][row], s_ml[1][row]);
+    }
+  }
+}
+
+template <int BS, bool SELECT>
+void launch_bs_q4(const AttnQ4Args& a, hipStream_t s) {
+  const long long runs = (long long)a.R * a.Hkv * a.nsplit;
+  const dim3 grid((unsigned)(a.by_length ? (runs + 7) / 8 * 8 * a.groups : (runs * a.groups + 7) / 8 * 8));
+  if (a.tiles == 1)
+    hipLaunchKernelGGL((q4_attn_kernel<1, BS, SELECT>), grid, dim3(kQW * 64), 0, s, a);
+  else
+    hipLaunchKernelGGL((q4_attn_kernel<2, BS, SELECT>), grid, dim3(kQW * 64), 0, s, a);
+}
+
+}  // namespace
+
+hipError_t launch_attn_q4(const AttnQ4Args& a, hipStream_t s) {
+  if (a.B == 16)
+    a.sel ? launch_bs_q4<16, true>(a, s) : launch_bs_q4<16, false>(a, s);
+  else
+    a.sel ? launch_bs_q4<32, true>(a, s) : launch_bs_q4<32, false>(a, s);
+  const hipError_t e = hipGetLastError();
+  return e != hipSuccess ? e : launch_tree_finish(a, s);
+}
+
+}  // namespace oasis

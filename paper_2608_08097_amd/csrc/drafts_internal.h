@@ -13,7 +13,7 @@ struct TreeAttnArgs {
   const uint16_t* v;         // pages as k, or pool_v [R][k_slots+1][Hkv][d][B]
   const int32_t* table;      // block table [R][NBmax], or slot_map [R][Hkv][k_slots]
   const int32_t* ctx_len;
-  const uint16_t* tree_k;    // [R][T][Hkv][d]
+  const uint16_t* tree_k;    // [R][T][Hkv][d]; NULL (4-bit cache): no tree
   const uint16_t* tree_v;
   const int32_t* parent;     // [R][T]; NULL: a chain
   const int32_t* tree_len;   // [R]; NULL: T

@@ -31,6 +31,10 @@ decltype(&oasis_tree_attn) f_tree;
 decltype(&oasis_sparse_tree_attn) f_sparse_tree;
 decltype(&oasis_verify_drafts) f_verify;
 decltype(&oasis_append_tokens) f_append;
+decltype(&oasis_rotate) f_rotate;
+decltype(&oasis_append_tokens_q4) f_append_q4;
+decltype(&oasis_update_summaries_q4) f_summaries_q4;
+decltype(&oasis_tree_attn_q4) f_tree_q4;
 
 enum Kind { kBf16, kI32, kF32, kU8 };
 
@@ -291,9 +295,12 @@ struct Tree {
   float scale;
 };
 // ctx_len, tree_k, tree_v, parent, tree_len, scale, out, lse, workspace, stream from a[0] on
-bool tree_args(const oasis_dims* d, int32_t T, Args a, Tree* t) {
+// (cache_only: tree_k and tree_v may be None)
+bool tree_args(const oasis_dims* d, int32_t T, Args a, Tree* t, bool cache_only = false) {
   const int64_t R = d->num_reqs, D = d->head_dim, rows = count({R, T, d->num_q_heads}), kv = count({R, T, d->num_kv_heads, D});
-  return tensor(a[0], R, kI32, &t->ctx) && tensor(a[1], kv, kBf16, &t->tk) && tensor(a[2], kv, kBf16, &t->tv) &&
+  t->tk = t->tv = nullptr;
+  const bool none = cache_only && a[1] == Py_None && a[2] == Py_None;
+  return tensor(a[0], R, kI32, &t->ctx) && (none || (tensor(a[1], kv, kBf16, &t->tk) && tensor(a[2], kv, kBf16, &t->tv))) &&
          optional(a[3], count({R, T}), kI32, &t->parent) && optional(a[4], R, kI32, &t->len) &&
          scale_at(a[5], D, &t->scale) && tensor(a[6], count({rows, D}), kBf16, &t->out) &&
          optional(a[7], rows, kF32, &t->lse) && workspace_at(a[8], &t->ws, &t->bytes) && stream_at(a[9], &t->s) &&
@@ -405,6 +412,141 @@ PyObject* append_tokens(PyObject*, Args a, Py_ssize_t n) {
   });
 }
 
+// Rows of heads [R][T][H][d], contiguous or evenly spaced: their address and stride; or None.
+bool rows_at(PyObject* o, int64_t R, int64_t T, int64_t H, int64_t D, void** p, int64_t* row, bool nullable = false) {
+  *p = nullptr;
+  *row = 0;
+  if (nullable && o == Py_None) return true;
+  if (!THPVariable_CheckExact(o)) return false;
+  const at::Tensor& t = THPVariable_Unpack(o);
+  if (!t.is_cuda() || !dtype_is(t.scalar_type(), kBf16) || t.numel() != count({R, T, H, D})) return false;
+  if (t.is_contiguous()) {
+    *row = H * D;
+  } else {
+    if (t.dim() != 4 || t.size(0) != R || t.size(1) != T || t.size(2) != H) return false;
+    *row = T > 1 ? t.stride(1) : (R > 1 ? t.stride(0) : H * D);
+    if (t.stride(3) != 1 || (H > 1 && t.stride(2) != D) || (R > 1 && t.stride(0) != T * *row)) return false;
+  }
+  *p = t.data_ptr();
+  return true;
+}
+
+// A rotation's structure and its table of turns, which the binding takes from one object.
+const oasis_rotary* rotary_at(PyObject* o, PyObject* turns) {
+  const auto* r = static_cast<const oasis_rotary*>(PyLong_AsVoidPtr(o));
+  return r && THPVariable_CheckExact(turns) && THPVariable_Unpack(turns).is_cuda() ? r : nullptr;
+}
+
+// Pages of the 4-bit cache: their number.
+bool q4_pages_at(PyObject* o, const oasis_dims* d, void** p, int64_t* pages) {
+  const int64_t per = count({d->num_kv_heads, d->block_size, 68});
+  if (!any_count(o, kU8, p, true)) return false;
+  const at::Tensor& t = THPVariable_Unpack(o);
+  if (per < 1 || t.dim() < 1 || t.numel() % per) return false;
+  *pages = t.numel() / per;
+  return true;
+}
+
+// dims, rotary, turns, num_tokens, positions, ctx_len, q, q_out, k, k_out, inverse, stream
+PyObject* rotate(PyObject*, Args a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    if (n != 12) FALLBACK;
+    const oasis_dims* d = dims_at(a[0]);
+    const oasis_rotary* rot = rotary_at(a[1], a[2]);
+    int32_t T;
+    if (!d || !rot || !int32(a[3], &T) || (a[10] != Py_True && a[10] != Py_False) ||
+        (a[6] == Py_None) != (a[7] == Py_None) || (a[8] == Py_None) != (a[9] == Py_None))
+      FALLBACK;
+    const int64_t R = d->num_reqs, D = d->head_dim;
+    void *pos, *ctx, *x[4], *s;
+    int64_t row[4];
+    if (!optional(a[4], count({R, T}), kI32, &pos) || !optional(a[5], R, kI32, &ctx)) FALLBACK;
+    for (int i = 0; i < 4; ++i)
+      if (!rows_at(a[6 + i], R, T, i < 2 ? d->num_q_heads : d->num_kv_heads, D, &x[i], &row[i], true)) FALLBACK;
+    if (!stream_at(a[11], &s) || !on_current(a, {2, 4, 5, 6, 7, 8, 9})) FALLBACK;
+    const int32_t inverse = a[10] == Py_True;
+    return run([&] {
+      return f_rotate(d, rot, T, (const int32_t*)pos, (const int32_t*)ctx, inverse, (const uint16_t*)x[0], row[0],
+                      (uint16_t*)x[1], row[1], (const uint16_t*)x[2], row[2], (uint16_t*)x[3], row[3], s);
+    });
+  });
+}
+
+// dims, rotary or 0, turns, new_k, new_v, num_tokens, path, path_len, k_pages, v_pages, block_table, ctx_len,
+// new_ctx_len, read_k, read_v, stream
+PyObject* append_tokens_q4(PyObject*, Args a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    if (n != 16) FALLBACK;
+    const oasis_dims* d = dims_at(a[0]);
+    const oasis_rotary* rot = a[2] == Py_None ? nullptr : rotary_at(a[1], a[2]);
+    int32_t N;
+    if (!d || (a[2] != Py_None && !rot) || !int32(a[5], &N)) FALLBACK;
+    const int64_t R = d->num_reqs, H = d->num_kv_heads, D = d->head_dim, kv = count({R, N, H, D});
+    void *nk, *nv, *path, *plen, *k, *v, *table, *ctx, *end, *rk, *rv, *s;
+    int64_t ks, vs, pages, v_pages;
+    if (!rows_at(a[3], R, N, H, D, &nk, &ks) || !rows_at(a[4], R, N, H, D, &nv, &vs) ||
+        !optional(a[6], count({R, N}), kI32, &path) || !optional(a[7], R, kI32, &plen) ||
+        !q4_pages_at(a[8], d, &k, &pages) || !q4_pages_at(a[9], d, &v, &v_pages) || pages != v_pages ||
+        THPVariable_Unpack(a[8]).sizes() != THPVariable_Unpack(a[9]).sizes() ||
+        !tensor(a[10], count({R, d->max_blocks}), kI32, &table) || !tensor(a[11], R, kI32, &ctx) ||
+        !optional(a[12], R, kI32, &end) || !optional(a[13], kv, kBf16, &rk) || !optional(a[14], kv, kBf16, &rv) ||
+        !stream_at(a[15], &s) || !on_current(a, {2, 3, 4, 6, 7, 8, 9, 10, 11, 12, 13, 14}))
+      FALLBACK;
+    return run([&] {
+      return f_append_q4(d, rot, (const uint16_t*)nk, ks, (const uint16_t*)nv, vs, N, (const int32_t*)path,
+                         (const int32_t*)plen, (uint8_t*)k, (uint8_t*)v, pages, (const int32_t*)table,
+                         (const int32_t*)ctx, (int32_t*)end, (uint16_t*)rk, (uint16_t*)rv, s);
+    });
+  });
+}
+
+// dims, k_pages, block_table, prev_ctx_len, ctx_len, max_new_blocks, kmax, kmin, stream
+PyObject* update_summaries_q4(PyObject*, Args a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    if (n != 9) FALLBACK;
+    const oasis_dims* d = dims_at(a[0]);
+    int32_t most;
+    if (!d || !int32(a[5], &most)) FALLBACK;
+    const int64_t R = d->num_reqs, sum = count({R, d->num_kv_heads, d->max_blocks, d->head_dim});
+    void *k, *table, *prev, *ctx, *mx, *mn, *s;
+    int64_t pages;
+    if (!q4_pages_at(a[1], d, &k, &pages) || !tensor(a[2], count({R, d->max_blocks}), kI32, &table) ||
+        !optional(a[3], R, kI32, &prev) || !tensor(a[4], R, kI32, &ctx) || !tensor(a[6], sum, kBf16, &mx) ||
+        !tensor(a[7], sum, kBf16, &mn) || !stream_at(a[8], &s) || !on_current(a, {1, 2, 3, 4, 6, 7}))
+      FALLBACK;
+    return run([&] {
+      return f_summaries_q4(d, (const uint8_t*)k, pages, (const int32_t*)table, (const int32_t*)prev,
+                            (const int32_t*)ctx, most, (uint16_t*)mx, (uint16_t*)mn, s);
+    });
+  });
+}
+
+// dims, q, num_q_tokens, k_pages, v_pages, block_table, sel, sel_count, k, ctx_len, tree_k, tree_v, parent, tree_len,
+// scale, out, lse, workspace, stream
+PyObject* tree_attn_q4(PyObject*, Args a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    if (n != 19) FALLBACK;
+    const oasis_dims* d = dims_at(a[0]);
+    int32_t T, ks;
+    if (!d || !int32(a[2], &T) || !int32(a[8], &ks)) FALLBACK;
+    const int64_t R = d->num_reqs, H = d->num_kv_heads, RH = count({R, H});
+    int64_t pages, v_pages;
+    void *q, *k, *v, *table, *sel, *cnt;
+    Tree t;
+    if (!tensor(a[1], count({R, T, d->num_q_heads, d->head_dim}), kBf16, &q) || !q4_pages_at(a[3], d, &k, &pages) ||
+        !q4_pages_at(a[4], d, &v, &v_pages) || THPVariable_Unpack(a[3]).sizes() != THPVariable_Unpack(a[4]).sizes() ||
+        !tensor(a[5], count({R, d->max_blocks}), kI32, &table) || !optional(a[6], count({RH, ks}), kI32, &sel) ||
+        !optional(a[7], RH, kI32, &cnt) || !tree_args(d, T, a + 9, &t, true) || !on_current(a, {1, 3, 4, 5, 6, 7}))
+      FALLBACK;
+    return run([&] {
+      return f_tree_q4(d, (const uint16_t*)q, T, (const uint8_t*)k, (const uint8_t*)v, pages, (const int32_t*)table,
+                       (const int32_t*)t.ctx, (const int32_t*)sel, (const int32_t*)cnt, ks, (const uint16_t*)t.tk,
+                       (const uint16_t*)t.tv, (const int32_t*)t.parent, (const int32_t*)t.len, t.scale,
+                       (uint16_t*)t.out, (float*)t.lse, t.ws, t.bytes, t.s);
+    });
+  });
+}
+
 // bind(attn, score, topk, score_select, stage): addresses of the library's entry points
 PyObject* bind(PyObject*, Args a, Py_ssize_t n) {
   void* p[5];
@@ -436,10 +578,27 @@ PyObject* bind_drafts(PyObject*, Args a, Py_ssize_t n) {
   Py_RETURN_NONE;
 }
 
+// bind_q4(rotate, append, summaries, attention): addresses of the library's entry points
+PyObject* bind_q4(PyObject*, Args a, Py_ssize_t n) {
+  void* p[4];
+  if (n != 4) return PyErr_Format(PyExc_TypeError, "bind_q4 takes 4 addresses");
+  for (int i = 0; i < 4; ++i) {
+    p[i] = PyLong_AsVoidPtr(a[i]);
+    if (!p[i]) return PyErr_Occurred() ? nullptr : PyErr_Format(PyExc_ValueError, "bind_q4: null address");
+  }
+  f_rotate = reinterpret_cast<decltype(f_rotate)>(p[0]);
+  f_append_q4 = reinterpret_cast<decltype(f_append_q4)>(p[1]);
+  f_summaries_q4 = reinterpret_cast<decltype(f_summaries_q4)>(p[2]);
+  f_tree_q4 = reinterpret_cast<decltype(f_tree_q4)>(p[3]);
+  Py_RETURN_NONE;
+}
+
 #define METHOD(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(bind),         METHOD(sparse_decode_attn), METHOD(score_blocks), METHOD(select_topk),
                          METHOD(score_select), METHOD(stage_blocks),       METHOD(bind_drafts),  METHOD(tree_attn),
-                         METHOD(sparse_tree_attn), METHOD(verify_drafts),  METHOD(append_tokens), {nullptr, nullptr, 0, nullptr}};
+                         METHOD(sparse_tree_attn), METHOD(verify_drafts),  METHOD(append_tokens),
+                         METHOD(bind_q4),      METHOD(rotate),             METHOD(append_tokens_q4), METHOD(update_summaries_q4),
+                         METHOD(tree_attn_q4), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

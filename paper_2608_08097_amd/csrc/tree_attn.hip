@@ -876,6 +876,7 @@ __global__ __launch_bounds__(kTreeMergeRows * 32) void wild_queries_kernel(TreeA
   const int row = blockIdx.x * kTreeMergeRows + (threadIdx.x >> 5);  // of R x T x Hq
   const int rt = row / a.Hq, r = rt / a.T;
   if (r >= a.R || rt - r * a.T >= tree_length(a, r)) return;
+  if (!a.tree_k && a.ctx_len[r] <= 0) return;  // nothing attended
   const int c4 = threadIdx.x & 31;
   const long long at = (long long)row * kHeadDim + c4 * 4;
   const uint2 w = *reinterpret_cast<const uint2*>(a.q + at);
