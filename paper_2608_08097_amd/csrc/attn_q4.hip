@@ -450,14 +450,279 @@ __global__ __launch_bounds__(kQW * 64) void q4_attn_kernel(AttnQ4Args a) {
   }
 }
 
+// More than two row tiles. Eight waves in two teams share every unit: each wave turns a
+// sixteenth of its codes, 16 tokens of keys or of values, into bf16 in LDS, and then attends
+// with its own one or two of the group's row tiles, team 0 the unit's first 32 tokens and
+// team 1 the others. Keys lie there as the first product's operand, values a token after the
+// other, 16 dims apart, for the transposing read.
+//
+// Loads of a unit's codes, 16 bytes a lane, go out kAhead units ahead of their conversion,
+// that one unit ahead of the products; two units are in LDS, one barrier a unit.
+constexpr int kRowsThreads = 512;
+constexpr int kRowPlaces = 4;   // waves of a team
+constexpr int kListBlocks = 1024;
+constexpr int kAhead = 3;
+constexpr int kKeysBytes = 16 * 1024;
+constexpr int kValuesPart = 4 * 1024 + 16;  // 32 dims of the unit's tokens, and a skew for the writes
+constexpr int kUnitBytes = kKeysBytes + 4 * kValuesPart;
+
+template <int NT, int BS, bool SELECT>
+__global__ __launch_bounds__(kRowsThreads) void q4_attn_rows_kernel(AttnQ4Args a) {
+  constexpr int kRows = NT * kRowPlaces * 16;
+  constexpr int kPad = kHeadDim + 4;
+  constexpr int kPer = kUnitTokens / BS;
+  constexpr int kMerge = (int)sizeof(float) * kRows * kPad;
+  __shared__ __align__(16) char s_buf[2 * kUnitBytes > kMerge ? 2 * kUnitBytes : kMerge];
+  __shared__ int2 s_list[kListBlocks];  // page and attended tokens of the segment's blocks
+  __shared__ uint64_t s_anc[kTreeMaxTokens];
+  __shared__ float s_ml[2][kRows];
+  __shared__ int s_wild;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63;
+  const int g = lane >> 4;
+  const int i = lane & 15;
+  const int team = wave / kRowPlaces;
+  const int rt = wave % kRowPlaces;  // this wave's tiles: rt and rt + 4 of the group's
+  Q4Item t;
+  if (!q4_setup<SELECT>(a, a.tiles * 16, t)) return;
+  const Ctx c = ctx_blocks(t.ctx, BS, a.NBmax);
+  const int blocks = SELECT ? t.selected + (c.nb > 0) : c.nb;
+  const int nu = (blocks + kPer - 1) / kPer;
+  const int each = a.by_nsplit(nu), more = nu - each * a.nsplit;
+  const int u_begin = t.split * each + min(t.split, more);
+  const int u_end = u_begin + each + (t.split < more);
+
+  bf16x8 qb[NT][4];
+#pragma unroll
+  for (int v = 0; v < NT; ++v) load_q4_queries(a, t, t.row0 + (rt + v * kRowPlaces) * 16, g, i, qb[v]);
+  float m_neg[NT], l_run[NT];
+  f32x4 acc[NT][8];
+#pragma unroll
+  for (int v = 0; v < NT; ++v) {
+    m_neg[v] = INFINITY;
+    l_run[v] = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < 8; ++dt) acc[v][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  if (threadIdx.x == 0) s_wild = 0;
+
+  // ---- what this wave converts: sub-block `sub` of keys or of values, lane (g, i) its token
+  // i, dims 32 g .. +31
+  const bool is_v = wave >= 4;
+  const int sub = wave & 3;
+  const uint8_t* const src = is_v ? a.v4 : a.k4;
+  const int sub_in = BS == 16 ? 0 : sub & 1;  // of its block
+  const long long codes_at = (long long)t.h * BS * kQ4Codes + sub_in * 1024 + i * kQ4Codes + g * 16;
+  const long long power_at = (long long)a.Hkv * BS * kQ4Codes + (long long)t.h * BS * kQ4Powers + sub_in * 64 +
+                             ((i & 3) * 4 + g) * 4 + (i >> 2);
+  // 32 dims of a token (quads of 8) to their place
+  const uint32_t put_at = is_v ? kKeysBytes + g * kValuesPart + (sub * 16 + i) * 32 : sub * 4096 + g * 256 + i * 16;
+  auto put = [&](int buf, int q, u32x4 x) __attribute__((always_inline)) {
+    *reinterpret_cast<u32x4*>(s_buf + buf * kUnitBytes + put_at + (is_v ? (q >> 1) * 2048 + (q & 1) * 16 : q * 1024)) = x;
+  };
+  struct Codes {
+    u32x4 x;
+    uint32_t power;
+    int keep;  // attended tokens
+  };
+  // ---- the products of one unit: `keep` attended tokens of the team's two sub-blocks (16: all)
+  auto attend = [&](int buf, int keep0, int keep1, bool tree) __attribute__((always_inline)) {
+    const char* kb = s_buf + buf * kUnitBytes + team * 8192 + lane * 16;
+    u32x4 kf[2][4];
+#pragma unroll
+    for (int tau = 0; tau < 2; ++tau)
+#pragma unroll
+      for (int st = 0; st < 4; ++st) kf[tau][st] = *reinterpret_cast<const u32x4*>(kb + tau * 4096 + st * 1024);
+    f32x4 sc[NT][2];
+#pragma unroll
+    for (int v = 0; v < NT; ++v) {
+      sc[v][0] = sc[v][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int st = 0; st < 4; ++st)
+#pragma unroll
+        for (int tau = 0; tau < 2; ++tau)
+          sc[v][tau] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(kf[tau][st]), qb[v][st], sc[v][tau], 0, 0, 0);
+    }
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+    char* vb = s_buf + buf * kUnitBytes + kKeysBytes + (team * 32 + 4 * g + (i >> 2)) * 32 + (i & 3) * 8;
+    u32x4 vf[8];
+#pragma unroll
+    for (int dt = 0; dt < 8; ++dt)
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        const u32x2 w = __builtin_bit_cast(
+            u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(
+                       vb + (dt >> 1) * kValuesPart + (dt & 1) * 2048 + q * 512)));
+        vf[dt][2 * q] = w[0];
+        vf[dt][2 * q + 1] = w[1];
+      }
+    if (keep0 < 16 || keep1 < 16 || tree) {
+#pragma unroll
+      for (int v = 0; v < NT; ++v) {
+        const int k0 = keep0 - 4 * g, k1 = keep1 - 4 * g;
+        uint32_t bits = (k0 <= 0 ? 0u : k0 >= 4 ? 15u : (1u << k0) - 1) | (k1 <= 0 ? 0u : k1 >= 4 ? 15u : (1u << k1) - 1) << 4;
+        if (tree) {
+          const int row = t.row0 + (rt + v * kRowPlaces) * 16 + i;
+          const uint64_t anc = s_anc[row < a.rows ? a.by_g(row) : 0];
+          bits = (uint32_t)(anc >> (team * 32 + 4 * g)) & 15u;
+          bits |= ((uint32_t)(anc >> (team * 32 + 16 + 4 * g)) & 15u) << 4;
+        }
+        mask_scores(sc[v], bits);
+      }
+    }
+#pragma unroll
+    for (int v = 0; v < NT; ++v) {
+      const bf16x8 pb = unit_softmax(sc[v], a.scale_log2, a.top, m_neg[v], l_run[v], acc[v]);
+#pragma unroll
+      for (int dt = 0; dt < 8; ++dt)
+        acc[v][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(vf[dt]), pb, acc[v][dt], 0, 0, 0);
+    }
+  };
+
+  for (int seg = u_begin; seg < u_end; seg += kListBlocks / kPer) {
+    const int units = min(kListBlocks / kPer, u_end - seg);
+    for (int n = threadIdx.x; n < units * kPer; n += kRowsThreads) {
+      int2 e;
+      q4_block<BS, SELECT>(a, t, c, seg * kPer + n, e.x, e.y);
+      s_list[n] = e;
+    }
+    __syncthreads();
+    auto load = [&](int s) __attribute__((always_inline)) {
+      const int2 e = s_list[min(s, units - 1) * kPer + (BS == 16 ? sub : sub >> 1)];
+      const int page = __builtin_amdgcn_readfirstlane(e.x);
+      Codes x;
+      x.keep = __builtin_amdgcn_readfirstlane(e.y) - sub_in * 16;
+      const uint8_t* at = src + page * a.page_bytes;
+      x.x = ldg16(at + codes_at);
+      x.power = at[power_at];
+      return x;
+    };
+    auto convert = [&](int buf, const Codes& x) __attribute__((always_inline)) {
+      float s = __uint_as_float(x.power << 23);
+      u32x4 codes = x.x;
+      if (x.keep < 16 && i >= x.keep) {  // what an unused place holds may be NaN
+        s = 1.f;
+        codes = u32x4{0, 0, 0, 0};
+      }
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const u32x4 y = {two_bf16<0>(codes[q], s), two_bf16<1>(codes[q], s), two_bf16<2>(codes[q], s), two_bf16<3>(codes[q], s)};
+        put(buf, q, y);
+      }
+    };
+    auto keep_of = [&](int s, int b) __attribute__((always_inline)) {  // sub-block b of unit s
+      const int n = __builtin_amdgcn_readfirstlane(s_list[s * kPer + (BS == 16 ? b : b >> 1)].y) - (BS == 16 ? 0 : (b & 1) * 16);
+      return n > 16 ? 16 : n;
+    };
+    Codes x[kAhead];
+#pragma unroll
+    for (int p = 0; p < kAhead; ++p) x[p] = load(p);
+    convert(0, x[0]);
+    x[0] = load(kAhead);
+    __syncthreads();
+    for (int s0 = 0; s0 < units; s0 += kAhead) {
+#pragma unroll
+      for (int p = 0; p < kAhead; ++p) {
+        const int s = s0 + p;
+        if (s >= units) break;
+        Codes& nx = x[(p + 1) % kAhead];
+        if (s + 1 < units) {
+          convert((s + 1) & 1, nx);
+          nx = load(s + 1 + kAhead);
+        }
+        attend(s & 1, keep_of(s, 2 * team), keep_of(s, 2 * team + 1), false);
+        __syncthreads();
+      }
+    }
+  }
+
+  // ---- the tree's own rows: a unit of the last split ----
+  if (t.split == a.nsplit - 1 && a.tree_k) {
+    __syncthreads();  // s_wild, where there was no unit
+    if (wave == 0) s_anc[lane] = ancestors(tree_parent(a, t.r, t.tlen, lane), t.tlen, lane);
+    const int j = sub * 16 + i;
+    const uint16_t* row = (is_v ? a.tree_v : a.tree_k) + t.tree_base + min(j, t.tlen - 1) * t.tree_row + g * 32;
+    u32x4 y[8];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      y[q] = ldg16(row + 8 * q);
+      y[4 + q] = u32x4{0, 0, 0, 0};
+      if (j >= t.tlen) y[q] = y[4 + q];
+    }
+    if (is_v && take_wild(y)) s_wild = 1;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) put(0, q, y[q]);
+    __syncthreads();
+    if (team * 32 < t.tlen) attend(0, 16, 16, true);
+    __syncthreads();
+  }
+
+  // ---- merge the teams: the second one's rows through LDS, the sums back there ----
+  float(*s_o)[kPad] = reinterpret_cast<float(*)[kPad]>(s_buf);  // [row of the group]
+#pragma unroll
+  for (int v = 0; v < NT; ++v) m_neg[v] = -finish_row(m_neg[v], l_run[v]);
+  if (team == 1) {
+#pragma unroll
+    for (int v = 0; v < NT; ++v) {
+      const int row = (rt + v * kRowPlaces) * 16 + i;
+#pragma unroll
+      for (int dt = 0; dt < 8; ++dt) *reinterpret_cast<f32x4*>(&s_o[row][16 * dt + 4 * g]) = acc[v][dt];
+      if (g == 0) {
+        s_ml[0][row] = -m_neg[v];
+        s_ml[1][row] = l_run[v];
+      }
+    }
+  }
+  __syncthreads();
+  if (team == 0) {
+#pragma unroll
+    for (int v = 0; v < NT; ++v) {
+      const int row = (rt + v * kRowPlaces) * 16 + i;
+      const float m0 = -m_neg[v], m1 = s_ml[0][row], M = fmaxf(m0, m1);
+      const float f0 = m0 == -INFINITY ? 0.f : fast_exp2(m0 - M), f1 = m1 == -INFINITY ? 0.f : fast_exp2(m1 - M);
+      const float S = l_run[v] * f0 + s_ml[1][row] * f1;
+#pragma unroll
+      for (int dt = 0; dt < 8; ++dt) {
+        f32x4& o = *reinterpret_cast<f32x4*>(&s_o[row][16 * dt + 4 * g]);
+        o = acc[v][dt] * f0 + o * f1;
+      }
+      if (g == 0) {  // the row's other lanes have read them
+        s_ml[0][row] = M;
+        s_ml[1][row] = S;
+      }
+    }
+  }
+  __syncthreads();
+  const long long pbase = ((long long)t.rh * a.nsplit + t.split) * a.rows + t.row0;
+  const int last = min(min(t.tlen * a.G, a.rows) - t.row0, a.tiles * 16);  // rows of this group in use
+  for (int pos = threadIdx.x; pos < kRows * (kHeadDim / 4); pos += kRowsThreads) {
+    const int row = pos >> 5;
+    const int c4 = pos & 31;
+    if (row >= last) break;
+    f32x4 o = *reinterpret_cast<const f32x4*>(&s_o[row][c4 * 4]);
+    if (s_wild) add_wild(a, t, s_anc[a.by_g(t.row0 + row)], c4, o);
+    if (a.nsplit == 1) {
+      write_row(a, t.r, t.h, t.row0 + row, c4, o, s_ml[0][row], s_ml[1][row]);
+    } else {
+      *reinterpret_cast<f32x4*>(a.part_o + (pbase + row) * kHeadDim + c4 * 4) = o;
+      if (c4 == 0) *reinterpret_cast<float2*>(a.part_ml + (pbase + row) * 2) = make_float2(s_ml[0][row], s_ml[1][row]);
+    }
+  }
+}
+
 template <int BS, bool SELECT>
 void launch_bs_q4(const AttnQ4Args& a, hipStream_t s) {
   const long long runs = (long long)a.R * a.Hkv * a.nsplit;
   const dim3 grid((unsigned)(a.by_length ? (runs + 7) / 8 * 8 * a.groups : (runs * a.groups + 7) / 8 * 8));
   if (a.tiles == 1)
     hipLaunchKernelGGL((q4_attn_kernel<1, BS, SELECT>), grid, dim3(kQW * 64), 0, s, a);
-  else
+  else if (a.tiles == 2)
     hipLaunchKernelGGL((q4_attn_kernel<2, BS, SELECT>), grid, dim3(kQW * 64), 0, s, a);
+  else if (a.tiles <= kRowPlaces)
+    hipLaunchKernelGGL((q4_attn_rows_kernel<1, BS, SELECT>), grid, dim3(kRowsThreads), 0, s, a);
+  else
+    hipLaunchKernelGGL((q4_attn_rows_kernel<2, BS, SELECT>), grid, dim3(kRowsThreads), 0, s, a);
 }
 
 }  // namespace

@@ -10,7 +10,8 @@ namespace oasis {
 
 constexpr int kQ4Unit = 64;   // tokens
 constexpr int kQ4Waves = 4;   // of a workgroup
-constexpr int kQ4Tiles = 2;   // 16-row tiles of a workgroup at most
+constexpr int kQ4RegisterTiles = 2;  // 16-row tiles up to which a wave converts for itself
+constexpr int kQ4Tiles = 8;   // 16-row tiles of a workgroup at most
 
 inline TreePlan q4_plan(long long pairs, int G, int T, int units) {
   TreePlan p{};
@@ -20,7 +21,7 @@ inline TreePlan q4_plan(long long pairs, int G, int T, int units) {
   p.tiles = (tiles + p.groups - 1) / p.groups;
   p.units = units;
   const long long items = pairs * p.groups;
-  const long long slots = 512;
+  const long long slots = p.tiles > kQ4RegisterTiles ? 256 : 512;
   long long most = (units + kQ4Waves - 1) / kQ4Waves;
   if (most > kTreeMaxSplits) most = kTreeMaxSplits;
   p.nsplit = 1;

@@ -1,6 +1,6 @@
 // What the attention kernels of a drafted tree share, over bf16 caches and over the
-// 4-bit one: how work items lie on the chip, the tree's ancestors and wild values, and
-// the rows' ends.
+// 4-bit one: how work items lie on the chip, the online softmax, the tree's ancestors and
+// wild values, and the rows' ends.
 #pragma once
 
 #include "drafts_internal.h"
@@ -86,6 +86,61 @@ __device__ __forceinline__ bool take_wild(u32x4 (&v)[8]) {
       v[j][p] = x & ~(((((x & 0x7F807F80u) + 0x00800080u) & 0x80008000u) >> 15) * 0xFFFFu);
     }
   return true;
+}
+
+// A tile's scores of 32 tokens, 8 a lane; those of the lane's bits stay.
+__device__ __forceinline__ void mask_scores(f32x4 (&sc)[2], uint32_t bits) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) sc[e >> 2][e & 3] = bits >> e & 1 ? sc[e >> 2][e & 3] : -INFINITY;
+}
+
+// Online softmax of one tile's scores (scale > 0: load_q): probabilities in bf16
+// (the second product's operand; 2^-8 of each at most, unbiased, and the sum takes
+// them unrounded), the row's reference (negated: +inf before its first token) and
+// the lane's partial sum updated. A probability is 2^(score - reference), and the
+// reference follows the row's maximum only when a lane's eight probabilities pass
+// `top` together: that needs no maximum of every unit's scores, and values far
+// above the reference show as large, infinite or NaN sums. The accumulators are
+// rescaled then, in a branch that is rare after a wave's first unit. The reference
+// lies a lift above the maximum that it was taken from, and `top` as far below 2^8
+// (tree_lift): the sums of all the tokens that the call can attend stay below 1/2,
+// so that no finite value overflows in them.
+// (Taken from `top` where it is needed: with it as an argument of its own, live through
+// the loops, wide trees took 1 % more.)
+__device__ __forceinline__ float tree_lift_of(float top) { return (float)(9 - __builtin_amdgcn_frexp_expf(top)); }
+
+__device__ __forceinline__ float unit_exp(const f32x4 (&s)[2], float scale, float m_neg, float (&p)[8]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) p[e] = fast_exp2(__builtin_fmaf(s[e >> 2][e & 3], scale, m_neg));
+  return ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+}
+
+__device__ __forceinline__ bf16x8 unit_softmax(const f32x4 (&s)[2], float scale, float top, float& m_neg, float& l_part,
+                                               f32x4 (&acc)[8]) {
+  float p[8];
+  float psum = unit_exp(s, scale, m_neg, p);
+  const uint64_t past = __builtin_amdgcn_ballot_w64(!(psum <= top));
+  if (__builtin_expect(past != 0, 0)) {
+    // the rows that passed it in one of their four lanes; the others stay as they are
+    const uint64_t rows = past | past >> 16 | past >> 32 | past >> 48;
+    const bool mine = rows >> (threadIdx.x & 15) & 1;
+    const float lmax = scale * fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
+                                     fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
+    float m = fmaxf(lmax, __shfl_xor(lmax, 16));
+    m = fmaxf(fmaxf(m, __shfl_xor(m, 32)) + tree_lift_of(top), -m_neg);
+    m = mine ? m : -m_neg;
+    const float alpha = m == -INFINITY ? 1.f : fast_exp2(-m_neg - m);
+    l_part *= alpha;
+#pragma unroll
+    for (int dt = 0; dt < 8; ++dt) acc[dt] *= alpha;
+    m_neg = -m;
+    psum = unit_exp(s, scale, m == -INFINITY ? 0.f : m_neg, p);
+  }
+  bf16x8 pb;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) pb[e] = (__bf16)p[e];
+  l_part += psum;
+  return pb;
 }
 
 // A row's maximum and, in l, its sum, from its four lanes' parts.

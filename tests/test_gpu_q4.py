@@ -366,6 +366,51 @@ def test_dense_wide_rows():
     _attn_case(3501, 1, 64, 1, 64, 16, [100], "random", [63])
 
 
+@pytest.mark.parametrize("G,T", [(4, 9), (3, 13), (4, 16), (5, 13), (8, 16), (4, 33), (16, 16), (9, 63), (64, 5)])
+def test_rows_of_several_tiles(G, T):
+    """Three, four and more row tiles, in one group and in several, with rows left over."""
+    _attn_case(3510 + G * T, 2, G * 2, 2, T, 16, [777, 40], "random", [T, (T + 1) // 2])
+    _attn_case(3511 + G * T, 2, G * 2, 2, T, 32, [777, 40], "none", [T, (T + 1) // 2], k=7)
+
+
+@pytest.mark.parametrize("B", [16, 32])
+@pytest.mark.parametrize("ctx", [[0], [1], [15, 16, 17], [31, 32, 33], [63, 64, 65], [0, 1000, 64], [-4, 500, 333], [4097]])
+def test_rows_of_several_tiles_lengths(B, ctx):
+    _attn_case(3560 + B + len(ctx), len(ctx), 24, 2, 5, B, ctx)
+    _attn_case(3570 + B + len(ctx), len(ctx), 16, 2, 20, B, ctx, "beam")
+    _attn_case(3580 + B + len(ctx), len(ctx), 16, 2, 10, B, ctx, "none")
+
+
+@pytest.mark.parametrize("G,T", [(4, 3), (20, 2), (20, 4)])
+def test_long_contexts_in_one_split(G, T):
+    """So many pairs that they are hardly split, or not at all, two of them with thousands of blocks: lists of blocks in
+    several pieces."""
+    R, B, NB, NP = 1024, 32, 2205, 2300
+    ctx = np.zeros(R, np.int32)
+    ctx[[3, 700]] = 2060 * 32 + 5, NB * B - 40
+    rng = np.random.default_rng(G)
+    q = random_bf16(3590, (R, T, G, 128))
+    kp, vp = (Q.make_pages(rng.normal(size=(NP, 1, B, 128))) for _ in range(2))
+    table = np.broadcast_to(rng.permutation(NP)[:NB], (R, NB)).astype(np.int32)
+    sel = np.broadcast_to(np.arange(2100), (R, 1, 2100)).astype(np.int32)
+    d = P.dims(R, G, 1, 128, B, NB)
+    note(f"attention of long contexts G={G} T={T}")
+    for k in (0, 2100):
+        out, lse = torch.zeros((R, T, G, 128), dtype=torch.bfloat16, device="cuda"), torch.zeros((R, T, G), device="cuda")
+        ws = torch.zeros(P.oasis_tree_attn_q4_workspace_bytes(d, T, k), dtype=torch.uint8, device="cuda")
+        cnt = np.minimum(np.maximum(-(-ctx // B) - 1, 0), 2100)[:, None]
+        P.oasis_tree_attn_q4(d, dev_bf16(q), T, dev_u8(kp), dev_u8(vp), dev_i32(table), dev_i32(ctx), dev_i32(sel) if k else None,
+                             dev_i32(cnt) if k else None, k, None, None, None, None, None, out, lse, ws)
+        some = [3, 5, 700]
+        args = (q[some], Q.read_pages(kp, 1, B), Q.read_pages(vp, 1, B), table[some], ctx[some], sel[some] if k else None,
+                cnt[some] if k else None, None, None, None, [T] * 3, B)
+        ref, ref_lse = Q.attend(*args)
+        ref_abs, _ = Q.attend(*args, magnitude=True)
+        assert torch.all(lse[5] == -torch.inf) and not out[5].any()
+        keep = np.array([0, 2])
+        _check(out[some][keep], lse[some][keep], ref[keep], ref_abs[keep], ref_lse[keep], out[some][keep])
+
+
 def test_pages_outside_the_tier():
     for k in (None, 9):
         _attn_case(3600, 3, 8, 2, 4, 16, [300, 555, 90], bad=True, k=k)
