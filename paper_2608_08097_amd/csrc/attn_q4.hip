@@ -461,16 +461,16 @@ __global__ __launch_bounds__(kQW * 64) void q4_attn_kernel(AttnQ4Args a) {
 constexpr int kRowsThreads = 512;
 constexpr int kRowPlaces = 4;   // waves of a team
 constexpr int kListBlocks = 1024;
-constexpr int kAhead = 3;
 constexpr int kKeysBytes = 16 * 1024;
 constexpr int kValuesPart = 4 * 1024 + 16;  // 32 dims of the unit's tokens, and a skew for the writes
 constexpr int kUnitBytes = kKeysBytes + 4 * kValuesPart;
 
 template <int NT, int BS, bool SELECT>
-__global__ __launch_bounds__(kRowsThreads) void q4_attn_rows_kernel(AttnQ4Args a) {
+__global__ __launch_bounds__(kRowsThreads, NT == 1 ? 4 : 2) void q4_attn_rows_kernel(AttnQ4Args a) {
   constexpr int kRows = NT * kRowPlaces * 16;
   constexpr int kPad = kHeadDim + 4;
   constexpr int kPer = kUnitTokens / BS;
+  constexpr int kAhead = 3;
   constexpr int kMerge = (int)sizeof(float) * kRows * kPad;
   __shared__ __align__(16) char s_buf[2 * kUnitBytes > kMerge ? 2 * kUnitBytes : kMerge];
   __shared__ int2 s_list[kListBlocks];  // page and attended tokens of the segment's blocks
@@ -547,8 +547,7 @@ __global__ __launch_bounds__(kRowsThreads) void q4_attn_rows_kernel(AttnQ4Args a
     typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
     char* vb = s_buf + buf * kUnitBytes + kKeysBytes + (team * 32 + 4 * g + (i >> 2)) * 32 + (i & 3) * 8;
     u32x4 vf[8];
-#pragma unroll
-    for (int dt = 0; dt < 8; ++dt)
+    auto read_v = [&](int dt) __attribute__((always_inline)) {
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
         const u32x2 w = __builtin_bit_cast(
@@ -557,6 +556,12 @@ __global__ __launch_bounds__(kRowsThreads) void q4_attn_rows_kernel(AttnQ4Args a
         vf[dt][2 * q] = w[0];
         vf[dt][2 * q + 1] = w[1];
       }
+    };
+    __builtin_amdgcn_sched_barrier(0);  // no reads of values ahead of it, into more registers
+    if constexpr (NT > 1) {
+#pragma unroll
+      for (int dt = 0; dt < 8; ++dt) read_v(dt);
+    }
     if (keep0 < 16 || keep1 < 16 || tree) {
 #pragma unroll
       for (int v = 0; v < NT; ++v) {
@@ -575,8 +580,16 @@ __global__ __launch_bounds__(kRowsThreads) void q4_attn_rows_kernel(AttnQ4Args a
     for (int v = 0; v < NT; ++v) {
       const bf16x8 pb = unit_softmax(sc[v], a.scale_log2, a.top, m_neg[v], l_run[v], acc[v]);
 #pragma unroll
-      for (int dt = 0; dt < 8; ++dt)
-        acc[v][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(vf[dt]), pb, acc[v][dt], 0, 0, 0);
+      for (int half = 0; half < 2; ++half) {
+        if constexpr (NT == 1) {
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int dt = 4 * half; dt < 4 * half + 4; ++dt) read_v(dt);
+        }
+#pragma unroll
+        for (int dt = 4 * half; dt < 4 * half + 4; ++dt)
+          acc[v][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(vf[dt]), pb, acc[v][dt], 0, 0, 0);
+      }
     }
   };
 

@@ -21,7 +21,7 @@ inline TreePlan q4_plan(long long pairs, int G, int T, int units) {
   p.tiles = (tiles + p.groups - 1) / p.groups;
   p.units = units;
   const long long items = pairs * p.groups;
-  const long long slots = p.tiles > kQ4RegisterTiles ? 256 : 512;
+  const long long slots = p.tiles > 4 ? 256 : 512;
   long long most = (units + kQ4Waves - 1) / kQ4Waves;
   if (most > kTreeMaxSplits) most = kTreeMaxSplits;
   p.nsplit = 1;
