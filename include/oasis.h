@@ -571,8 +571,7 @@ OASIS_API oasis_status oasis_update_summaries_q4(const oasis_dims* dims, const u
  * and k = 0: every block. tree_k and tree_v both NULL: the T rows attend the cache
  * alone (parent is not looked at), each without a mask among them, as in
  * oasis_sparse_decode_attn. A row without an attended token gives out = 0, lse = -inf.
- * A NaN in the cache reaches the rows that attend its token. Values below 2^-96 lose
- * precision.
+ * A NaN in the cache reaches the rows that attend its token.
  * workspace: oasis_tree_attn_q4_workspace_bytes (0: may be NULL); calls that run at
  * the same time need separate workspaces.
  */

@@ -12,10 +12,8 @@
 // at a time; the queries are dealt to the same dims. The tokens are dealt to MFMA rows so
 // that lane (g, n) ends up with row n's scores of sub-block g's 16 tokens.
 //
-// Values need 16 tokens of one dim in a lane: their codes go through LDS, 4 KB a wave and
-// unit, and come back through the transposing read of 16 x 16 codes. Their powers differ
-// from token to token of a lane and cannot go into that conversion: the probabilities take
-// them up, once for each group of dims, which rounds nothing (a power of two).
+// Values need 8 tokens of one dim in a lane: turned into bf16 as the keys are, they go
+// through LDS, a part of it for each wave, and come back through the transposing read.
 //
 // The tree's rows, keys and values in bf16, are a unit of their own in the last split of
 // every pair.
@@ -196,38 +194,40 @@ __global__ __launch_bounds__(kQW * 64) void q4_attn_kernel(AttnQ4Args a) {
     live &= ~(((1ull << kPer) - 1) << p);
     return p;
   };
+  // Lane (g, i) holds, of each sub-block s = i / 4, tokens 4 q + i % 4 in tile q, dims 32 g ..
+  // +31, so that lane (g, n) gets row n's scores of sub-block g's tokens in order.
   struct Loaded {
-    u32x4 k[4], v[4];       // codes: keys of tile u, values of sub-block u
-    uint32_t k_pow, v_pow;
-    int keep;               // attended tokens of sub-block g
-    bool whole;             // of every sub-block
+    u32x4 k[4], v[4];        // codes
+    uint32_t k_pow, v_pow;   // tile q's power in byte q
+    int keep;                // attended tokens of sub-block s, in the lower half those of sub-block g
+    bool whole;              // all of every sub-block
   };
-  const long long codes_h = (long long)t.h * BS * kQ4Codes;
-  const long long powers_h = (long long)a.Hkv * BS * kQ4Codes + (long long)t.h * BS * kQ4Powers;
+  const int s_in = BS == 16 ? 0 : (i >> 2) & 1;  // sub-block s in its block
+  const uint32_t codes_at = t.h * BS * kQ4Codes + s_in * 1024 + (i & 3) * kQ4Codes + g * 16;
+  const uint32_t power_at = a.Hkv * BS * kQ4Codes + t.h * BS * kQ4Powers + s_in * 64 + ((i & 3) * 4 + g) * 4;
   Loaded u;
-  // (for a wave without a next unit the first unit's block 0 of page 0 stands in)
+  // (for a wave without a next unit the first bytes of page 0 stand in)
+  long long page_at = 0;
   auto load_k = [&](int p) __attribute__((always_inline)) {
-    const int s = i >> 2;  // the sub-block of this lane's tokens
-    const int pg = __shfl(place, p < 0 ? 0 : p + (BS == 16 ? s : s >> 1));
-    const uint8_t* at = a.k4 + (p < 0 ? 0 : pg) * a.page_bytes;
-    const int sub = BS == 16 ? 0 : s & 1;
-    const uint8_t* codes = at + codes_h + sub * 1024 + (i & 3) * 64 + g * 16;
+    const int from = p < 0 ? 0 : p + (BS == 16 ? i >> 2 : i >> 3);
+    page_at = p < 0 ? 0 : __shfl(place, from) * a.page_bytes;
+    const uint8_t* at = a.k4 + page_at;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) u.k[q] = ldg16(codes + q * 256);
-    u.k_pow = *reinterpret_cast<const uint32_t*>(at + powers_h + sub * 64 + ((i & 3) * 4 + g) * 4);
+    for (int q = 0; q < 4; ++q) u.k[q] = ldg16(at + codes_at + q * 256);
+    u.k_pow = *reinterpret_cast<const uint32_t*>(at + power_at);
+    auto keep_of = [&](int sub) __attribute__((always_inline)) {
+      const int n = __shfl(count, p < 0 ? 0 : p + (BS == 16 ? sub : sub >> 1)) - (BS == 16 ? 0 : (sub & 1) * 16);
+      return p < 0 || n < 0 ? 0 : (n > 16 ? 16 : n);
+    };
+    const int mine = keep_of(g);
+    u.whole = __builtin_amdgcn_ballot_w64(mine == 16) == ~0ull;
+    u.keep = u.whole ? 16 << 16 | 16 : keep_of(i >> 2) << 16 | mine;
   };
-  auto load_v = [&](int p) __attribute__((always_inline)) {
+  auto load_v = [&]() __attribute__((always_inline)) {
+    const uint8_t* at = a.v4 + page_at;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int pg = p < 0 ? 0 : __builtin_amdgcn_readlane(place, p + (BS == 16 ? q : q >> 1));
-      u.v[q] = ldg16(a.v4 + pg * a.page_bytes + codes_h + (BS == 16 ? 0 : q & 1) * 1024 + lane * 16);
-    }
-    const int from = p < 0 ? 0 : p + (BS == 16 ? g : g >> 1);
-    const int pg = p < 0 ? 0 : __shfl(place, from);
-    u.v_pow = *reinterpret_cast<const uint32_t*>(a.v4 + pg * a.page_bytes + powers_h + (BS == 16 ? 0 : g & 1) * 64 + i * 4);
-    const int n = p < 0 ? 0 : __shfl(count, from) - (BS == 16 ? 0 : (g & 1) * 16);
-    u.keep = n < 0 ? 0 : (n > 16 ? 16 : n);
-    u.whole = __builtin_amdgcn_ballot_w64(u.keep == 16) == ~0ull;
+    for (int q = 0; q < 4; ++q) u.v[q] = ldg16(at + codes_at + q * 256);
+    u.v_pow = *reinterpret_cast<const uint32_t*>(at + power_at);
   };
 
   bf16x8 qb[NT][4];
@@ -248,8 +248,12 @@ __global__ __launch_bounds__(kQW * 64) void q4_attn_kernel(AttnQ4Args a) {
   __shared__ uint64_t s_anc[kTreeMaxTokens];
   __shared__ int s_wild;
   // a wave's values of a unit, its part of the tree's, and its rows at the end
-  __shared__ __align__(16) float s_o[kQW][kRows][kPad];
-  static_assert(sizeof(float) * kRows * kPad >= 8192, "half the tree's values");
+  constexpr int kValues = kUnitTokens * kHeadDim * 2, kMerge = (int)sizeof(float) * kRows * kPad;
+  constexpr int kWaveBytes = kValues > kMerge ? kValues : kMerge;
+  __shared__ __align__(16) char s_wave[kQW][kWaveBytes];
+  auto s_o = [&](int w, int row, int dim) __attribute__((always_inline)) {
+    return reinterpret_cast<f32x4*>(&s_wave[w][(row * kPad + dim) * sizeof(float)]);
+  };
 
   // ---- the tree's own rows: one unit, of the last wave of the last split ----
   const bool tree_split = t.split == a.nsplit - 1 && a.tree_k != nullptr;
@@ -285,7 +289,7 @@ __global__ __launch_bounds__(kQW * 64) void q4_attn_kernel(AttnQ4Args a) {
         for (int e = 0; e < 4; ++e) sc[q][e] = bits >> (4 * q + e) & 1 ? sc[q][e] : -INFINITY;
       softmax16(sc, a.scale_log2, a.top, m_neg[v], l_run[v], acc[v], p[v]);
     }
-    u32x4* sv = reinterpret_cast<u32x4*>(&s_o[wave][0][0]);  // [dim][group of tokens], 8 tokens each
+    u32x4* sv = reinterpret_cast<u32x4*>(s_wave[wave]);  // [dim][group of tokens], 8 tokens each
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
       u32x4 tv[8];
@@ -318,29 +322,33 @@ __global__ __launch_bounds__(kQW * 64) void q4_attn_kernel(AttnQ4Args a) {
   if (threadIdx.x == (kQW - 1) * 64) s_wild = wild;
 
   // ---- the cache ----
-  typedef int i32x2 __attribute__((ext_vector_type(2)));
-  char* sw = reinterpret_cast<char*>(&s_o[wave][0][0]);  // codes [sub-block][32 dims][16 tokens][16 bytes], powers
-  char* s_pow = sw + 4096;
+  // Values in LDS: [32 dims][16 dims][tile q][lane i] of 32 bytes, the two halves of the
+  // lanes i >= 8 swapped, so that the lanes of a write meet no bank twice.
+  typedef short s16x4 __attribute__((ext_vector_type(4)));
+  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+  char* const put = s_wave[wave] + g * 4096 + i * 32;
+  char* const get = s_wave[wave] + (4 * g + (i >> 2)) * 32 + ((((i & 3) >> 1) ^ (g >> 1)) << 4) + (i & 1) * 8;
+  const int swap = i >> 3 << 4;
   chunk_set();
   int cur = next();
   load_k(cur);
-  load_v(cur);
+  load_v();
   while (cur >= 0) {
     const int nxt = next();
-    // values into LDS
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-      *reinterpret_cast<u32x4*>(sw + q * 1024 + (lane & 3) * 256 + (lane >> 2) * 16) = u.v[q];
     const int keep = u.keep;
     const bool whole = u.whole;
-    uint32_t v_pow = u.v_pow;
-    if (!whole) {  // token i / 4 + 4 u at byte u
-      uint32_t m = 0;
+    // values into LDS
 #pragma unroll
-      for (int q = 0; q < 4; ++q) m |= 4 * q + (i >> 2) < keep ? 0xFFu << (8 * q) : 0;
-      v_pow &= m;  // 0 times what an unused place holds stays 0
+    for (int q = 0; q < 4; ++q) {
+      float s = power_f32(u.v_pow, q);
+      if (!whole && 4 * q + (i & 3) >= keep >> 16) {  // 0 times what an unused place holds must stay 0
+        s = 1.f;
+        u.v[q] = u32x4{0, 0, 0, 0};
+      }
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        *reinterpret_cast<bf16x8*>(put + (c >> 1) * 2048 + q * 512 + (((c & 1) << 4) ^ swap)) = eight_bf16(u.v[q][c], s);
     }
-    *reinterpret_cast<uint32_t*>(s_pow + g * 64 + i * 4) = v_pow;
     // scores
     f32x4 sc[NT][4];
 #pragma unroll
@@ -357,45 +365,39 @@ __global__ __launch_bounds__(kQW * 64) void q4_attn_kernel(AttnQ4Args a) {
     }
     __builtin_amdgcn_sched_barrier(0);
     load_k(nxt);
-    load_v(nxt);
+    load_v();
     __builtin_amdgcn_sched_barrier(0);
-    float p[NT][16];
+    bf16x8 pb[NT][2];
 #pragma unroll
     for (int v = 0; v < NT; ++v) {
       if (!whole) {
 #pragma unroll
         for (int q = 0; q < 4; ++q)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) sc[v][q][e] = 4 * q + e < keep ? sc[v][q][e] : -INFINITY;
+          for (int e = 0; e < 4; ++e) sc[v][q][e] = 4 * q + e < (keep & 0xFFFF) ? sc[v][q][e] : -INFINITY;
       }
-      softmax16(sc[v], a.scale_log2, a.top, m_neg[v], l_run[v], acc[v], p[v]);
+      float p[16];
+      softmax16(sc[v], a.scale_log2, a.top, m_neg[v], l_run[v], acc[v], p);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) pb[v][e >> 3][e & 7] = (__bf16)p[e];
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    u32x4 pw[4];  // powers of tokens e + 4 u: group of dims, byte u
 #pragma unroll
-    for (int e = 0; e < 4; ++e) pw[e] = *reinterpret_cast<const u32x4*>(s_pow + g * 64 + e * 16);
+    for (int dt = 0; dt < 8; ++dt) {
+      u32x4 vf[2];
 #pragma unroll
-    for (int gd = 0; gd < 4; ++gd) {
-      bf16x8 pb[NT][2];
-#pragma unroll
-      for (int v = 0; v < NT; ++v)
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) pb[v][q >> 1][(q & 1) * 4 + e] = (__bf16)(p[v][4 * q + e] * power_f32(pw[e][gd], q));
-#pragma unroll
-      for (int d2 = 0; d2 < 2; ++d2) {
-        const int dt = 2 * gd + d2;
-        const i32x2 w = __builtin_amdgcn_ds_read_tr4_b64_v2i32(
-            (__attribute__((address_space(3))) i32x2*)(sw + g * 1024 + gd * 256 + i * 16 + d2 * 8));
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          const bf16x8 vb = eight_bf16((uint32_t)w[half], 1.f);
-#pragma unroll
-          for (int v = 0; v < NT; ++v)
-            acc[v][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vb, pb[v][half], acc[v][dt], 0, 0, 0);
-        }
+      for (int q = 0; q < 4; ++q) {
+        const u32x2 w = __builtin_bit_cast(
+            u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                       (__attribute__((address_space(3))) s16x4*)(get + (dt >> 1) * 4096 + (dt & 1) * 2048 + q * 512)));
+        vf[q >> 1][2 * (q & 1)] = w[0];
+        vf[q >> 1][2 * (q & 1) + 1] = w[1];
       }
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int v = 0; v < NT; ++v)
+          acc[v][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(vf[half]), pb[v][half], acc[v][dt], 0, 0, 0);
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     cur = nxt;
@@ -428,7 +430,7 @@ __global__ __launch_bounds__(kQW * 64) void q4_attn_kernel(AttnQ4Args a) {
       s_ml[1][row] = S;
     }
 #pragma unroll
-    for (int dt = 0; dt < 8; ++dt) *reinterpret_cast<f32x4*>(&s_o[wave][row][16 * dt + 4 * g]) = acc[v][dt] * f;
+    for (int dt = 0; dt < 8; ++dt) *s_o(wave, row, 16 * dt + 4 * g) = acc[v][dt] * f;
   }
   __syncthreads();
   const long long pbase = ((long long)t.rh * a.nsplit + t.split) * a.rows + t.row0;
@@ -437,9 +439,9 @@ __global__ __launch_bounds__(kQW * 64) void q4_attn_kernel(AttnQ4Args a) {
     const int row = pos >> 5;
     const int c4 = pos & 31;
     if (row >= last) break;
-    f32x4 o = *reinterpret_cast<const f32x4*>(&s_o[0][row][c4 * 4]);
+    f32x4 o = *s_o(0, row, c4 * 4);
 #pragma unroll
-    for (int w = 1; w < kQW; ++w) o += *reinterpret_cast<const f32x4*>(&s_o[w][row][c4 * 4]);
+    for (int w = 1; w < kQW; ++w) o += *s_o(w, row, c4 * 4);
     if (s_wild) add_wild(a, t, s_anc[a.by_g(t.row0 + row)], c4, o);
     if (a.nsplit == 1) {
       write_row(a, t.r, t.h, t.row0 + row, c4, o, s_ml[0][row], s_ml[1][row]);
