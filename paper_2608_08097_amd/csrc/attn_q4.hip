@@ -208,13 +208,9 @@ __global__ __launch_bounds__(kQW * 64) void q4_attn_kernel(AttnQ4Args a) {
   Loaded u;
   // (for a wave without a next unit the first bytes of page 0 stand in)
   long long page_at = 0;
-  auto load_k = [&](int p) __attribute__((always_inline)) {
+  auto find = [&](int p) __attribute__((always_inline)) {
     const int from = p < 0 ? 0 : p + (BS == 16 ? i >> 2 : i >> 3);
     page_at = p < 0 ? 0 : __shfl(place, from) * a.page_bytes;
-    const uint8_t* at = a.k4 + page_at;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) u.k[q] = ldg16(at + codes_at + q * 256);
-    u.k_pow = *reinterpret_cast<const uint32_t*>(at + power_at);
     auto keep_of = [&](int sub) __attribute__((always_inline)) {
       const int n = __shfl(count, p < 0 ? 0 : p + (BS == 16 ? sub : sub >> 1)) - (BS == 16 ? 0 : (sub & 1) * 16);
       return p < 0 || n < 0 ? 0 : (n > 16 ? 16 : n);
@@ -223,11 +219,10 @@ __global__ __launch_bounds__(kQW * 64) void q4_attn_kernel(AttnQ4Args a) {
     u.whole = __builtin_amdgcn_ballot_w64(mine == 16) == ~0ull;
     u.keep = u.whole ? 16 << 16 | 16 : keep_of(i >> 2) << 16 | mine;
   };
-  auto load_v = [&]() __attribute__((always_inline)) {
-    const uint8_t* at = a.v4 + page_at;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) u.v[q] = ldg16(at + codes_at + q * 256);
-    u.v_pow = *reinterpret_cast<const uint32_t*>(at + power_at);
+  auto load_k = [&](int q) __attribute__((always_inline)) { u.k[q] = ldg16(a.k4 + page_at + codes_at + q * 256); };
+  auto load_v = [&](int q) __attribute__((always_inline)) { u.v[q] = ldg16(a.v4 + page_at + codes_at + q * 256); };
+  auto load_pow = [&](const uint8_t* pages) __attribute__((always_inline)) {
+    return *reinterpret_cast<const uint32_t*>(pages + page_at + power_at);
   };
 
   bf16x8 qb[NT][4];
@@ -322,25 +317,34 @@ __global__ __launch_bounds__(kQW * 64) void q4_attn_kernel(AttnQ4Args a) {
   if (threadIdx.x == (kQW - 1) * 64) s_wild = wild;
 
   // ---- the cache ----
-  // Values in LDS: [32 dims][16 dims][tile q][lane i] of 32 bytes, the two halves of the
-  // lanes i >= 8 swapped, so that the lanes of a write meet no bank twice.
+  // Values in LDS: [32 dims][16 dims][tile q][lane i] of 32 bytes, the two halves swapped in
+  // every other four lanes, so that the lanes of a write meet no bank twice.
   typedef short s16x4 __attribute__((ext_vector_type(4)));
   typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
   char* const put = s_wave[wave] + g * 4096 + i * 32;
-  char* const get = s_wave[wave] + (4 * g + (i >> 2)) * 32 + ((((i & 3) >> 1) ^ (g >> 1)) << 4) + (i & 1) * 8;
-  const int swap = i >> 3 << 4;
+  char* const get = s_wave[wave] + (4 * g + (i >> 2)) * 32 + ((((i & 3) >> 1) ^ (g & 1)) << 4) + (i & 1) * 8;
+  const int swap = (i >> 2 & 1) << 4;
   chunk_set();
   int cur = next();
-  load_k(cur);
-  load_v();
+  find(cur);
+  u.v_pow = load_pow(a.v4);
+#pragma unroll
+  for (int q = 0; q < 4; ++q) load_v(q);
+  u.k_pow = load_pow(a.k4);
+#pragma unroll
+  for (int q = 0; q < 4; ++q) load_k(q);
   while (cur >= 0) {
+    // A tile's registers take the next unit's codes as soon as this one's are turned: the time
+    // to the next use is what hides the latency, 8.5 KB a wave on their way.
     const int nxt = next();
     const int keep = u.keep;
     const bool whole = u.whole;
+    const uint32_t v_pow = u.v_pow, k_pow = u.k_pow;
+    find(nxt);
     // values into LDS
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      float s = power_f32(u.v_pow, q);
+      float s = power_f32(v_pow, q);
       if (!whole && 4 * q + (i & 3) >= keep >> 16) {  // 0 times what an unused place holds must stay 0
         s = 1.f;
         u.v[q] = u32x4{0, 0, 0, 0};
@@ -348,12 +352,15 @@ __global__ __launch_bounds__(kQW * 64) void q4_attn_kernel(AttnQ4Args a) {
 #pragma unroll
       for (int c = 0; c < 4; ++c)
         *reinterpret_cast<bf16x8*>(put + (c >> 1) * 2048 + q * 512 + (((c & 1) << 4) ^ swap)) = eight_bf16(u.v[q][c], s);
+      __builtin_amdgcn_sched_barrier(0);
+      if (q == 0) u.v_pow = load_pow(a.v4);
+      load_v(q);
     }
     // scores
     f32x4 sc[NT][4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      const float s = power_f32(u.k_pow, q);
+      const float s = power_f32(k_pow, q);
 #pragma unroll
       for (int v = 0; v < NT; ++v) sc[v][q] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -362,11 +369,10 @@ __global__ __launch_bounds__(kQW * 64) void q4_attn_kernel(AttnQ4Args a) {
 #pragma unroll
         for (int v = 0; v < NT; ++v) sc[v][q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kb, qb[v][st], sc[v][q], 0, 0, 0);
       }
+      __builtin_amdgcn_sched_barrier(0);
+      if (q == 0) u.k_pow = load_pow(a.k4);
+      load_k(q);
     }
-    __builtin_amdgcn_sched_barrier(0);
-    load_k(nxt);
-    load_v();
-    __builtin_amdgcn_sched_barrier(0);
     bf16x8 pb[NT][2];
 #pragma unroll
     for (int v = 0; v < NT; ++v) {
@@ -456,7 +462,7 @@ __global__ __launch_bounds__(kQW * 64) void q4_attn_kernel(AttnQ4Args a) {
 // sixteenth of its codes, 16 tokens of keys or of values, into bf16 in LDS, and then attends
 // with its own one or two of the group's row tiles, team 0 the unit's first 32 tokens and
 // team 1 the others. Keys lie there as the first product's operand, values a token after the
-// other, 16 dims apart, for the transposing read.
+// other, 16 dims (32 bytes, the halves swapped as above) apart, for the transposing read.
 //
 // Loads of a unit's codes, 16 bytes a lane, go out kAhead units ahead of their conversion,
 // that one unit ahead of the products; two units are in LDS, one barrier a unit.
@@ -464,7 +470,7 @@ constexpr int kRowsThreads = 512;
 constexpr int kRowPlaces = 4;   // waves of a team
 constexpr int kListBlocks = 1024;
 constexpr int kKeysBytes = 16 * 1024;
-constexpr int kValuesPart = 4 * 1024 + 16;  // 32 dims of the unit's tokens, and a skew for the writes
+constexpr int kValuesPart = 4 * 1024;  // 32 dims of the unit's tokens
 constexpr int kUnitBytes = kKeysBytes + 4 * kValuesPart;
 
 template <int NT, int BS, bool SELECT>
@@ -520,7 +526,7 @@ __global__ __launch_bounds__(kRowsThreads, NT == 1 ? 4 : 2) void q4_attn_rows_ke
   // 32 dims of a token (quads of 8) to their place
   const uint32_t put_at = is_v ? kKeysBytes + g * kValuesPart + (sub * 16 + i) * 32 : sub * 4096 + g * 256 + i * 16;
   auto put = [&](int buf, int q, u32x4 x) __attribute__((always_inline)) {
-    *reinterpret_cast<u32x4*>(s_buf + buf * kUnitBytes + put_at + (is_v ? (q >> 1) * 2048 + (q & 1) * 16 : q * 1024)) = x;
+    *reinterpret_cast<u32x4*>(s_buf + buf * kUnitBytes + put_at + (is_v ? (q >> 1) * 2048 + ((q & 1) ^ (i >> 2 & 1)) * 16 : q * 1024)) = x;
   };
   struct Codes {
     u32x4 x;
@@ -547,7 +553,7 @@ __global__ __launch_bounds__(kRowsThreads, NT == 1 ? 4 : 2) void q4_attn_rows_ke
     }
     typedef short s16x4 __attribute__((ext_vector_type(4)));
     typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-    char* vb = s_buf + buf * kUnitBytes + kKeysBytes + (team * 32 + 4 * g + (i >> 2)) * 32 + (i & 3) * 8;
+    char* vb = s_buf + buf * kUnitBytes + kKeysBytes + (team * 32 + 4 * g + (i >> 2)) * 32 + ((((i & 3) >> 1) ^ (g & 1)) << 4) + (i & 1) * 8;
     u32x4 vf[8];
     auto read_v = [&](int dt) __attribute__((always_inline)) {
 #pragma unroll
