@@ -89,8 +89,6 @@ __device__ __forceinline__ void q4_block(const AttnQ4Args& a, const Q4Item& t, c
   count = ok ? (id == c.n_cand ? c.local_len : BS) : 0;
 }
 
-__device__ __forceinline__ float power_f32(uint32_t w, int u) { return __uint_as_float((w >> (8 * u) & 255u) << 23); }
-
 template <int SEL>
 __device__ __forceinline__ uint32_t two_bf16(uint32_t codes, float scale) {
   return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, SEL));
@@ -130,31 +128,42 @@ __device__ __forceinline__ float exp16(const f32x4 (&s)[4], float scale, float m
   }
   return (sum[0] + sum[1]) + (sum[2] + sum[3]);
 }
-__device__ __forceinline__ void softmax16(const f32x4 (&s)[4], float scale, float top, float& m_neg, float& l_part,
-                                          f32x4 (&acc)[8], float (&p)[16]) {
-  float psum = exp16(s, scale, m_neg, p);
-  const uint64_t past = __builtin_amdgcn_ballot_w64(!(psum <= top));
-  if (__builtin_expect(past != 0, 0)) {
-    const uint64_t rows = past | past >> 16 | past >> 32 | past >> 48;
-    const bool mine = rows >> (threadIdx.x & 15) & 1;
-    float m = -INFINITY;
+template <int NT>
+__device__ __forceinline__ void softmax16(const f32x4 (&s)[NT][4], float scale, float top, float (&m_neg)[NT],
+                                          float (&l_part)[NT], f32x4 (&acc)[NT][8], float (&p)[NT][16]) {
+  float psum[NT];
+  bool over = false;
 #pragma unroll
-    for (int u = 0; u < 4; ++u) m = fmaxf(m, fmaxf(fmaxf(s[u][0], s[u][1]), fmaxf(s[u][2], s[u][3])));
-    m *= scale;
-    m = fmaxf(m, __shfl_xor(m, 16));
-    m = fmaxf(fmaxf(m, __shfl_xor(m, 32)) + (float)(9 - __builtin_amdgcn_frexp_expf(top)), -m_neg);
-    m = mine ? m : -m_neg;
-    const float alpha = m == -INFINITY ? 1.f : fast_exp2(-m_neg - m);
-    l_part *= alpha;
-#pragma unroll
-    for (int dt = 0; dt < 8; ++dt) acc[dt] *= alpha;
-    m_neg = -m;
-    psum = exp16(s, scale, m == -INFINITY ? 0.f : m_neg, p);
+  for (int v = 0; v < NT; ++v) {
+    psum[v] = exp16(s[v], scale, m_neg[v], p[v]);
+    over |= !(psum[v] <= top);
   }
-  l_part += psum;
+  if (__builtin_expect(__builtin_amdgcn_ballot_w64(over) != 0, 0)) {
+#pragma unroll
+    for (int v = 0; v < NT; ++v) {
+      const uint64_t past = __builtin_amdgcn_ballot_w64(!(psum[v] <= top));
+      const uint64_t rows = past | past >> 16 | past >> 32 | past >> 48;
+      const bool mine = rows >> (threadIdx.x & 15) & 1;
+      float m = -INFINITY;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) m = fmaxf(m, fmaxf(fmaxf(s[v][u][0], s[v][u][1]), fmaxf(s[v][u][2], s[v][u][3])));
+      m *= scale;
+      m = fmaxf(m, __shfl_xor(m, 16));
+      m = fmaxf(fmaxf(m, __shfl_xor(m, 32)) + tree_lift_of(top), -m_neg[v]);
+      m = mine ? m : -m_neg[v];
+      const float alpha = m == -INFINITY ? 1.f : fast_exp2(-m_neg[v] - m);
+      l_part[v] *= alpha;
+#pragma unroll
+      for (int dt = 0; dt < 8; ++dt) acc[v][dt] *= alpha;
+      m_neg[v] = -m;
+      psum[v] = exp16(s[v], scale, m == -INFINITY ? 0.f : m_neg[v], p[v]);
+    }
+  }
+#pragma unroll
+  for (int v = 0; v < NT; ++v) l_part[v] += psum[v];
 }
 
-template <int NT, int BS, bool SELECT>
+template <int NT, int BS, bool SELECT, bool STREAM>
 __global__ __launch_bounds__(kQW * 64) void q4_attn_kernel(AttnQ4Args a) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
@@ -194,36 +203,36 @@ __global__ __launch_bounds__(kQW * 64) void q4_attn_kernel(AttnQ4Args a) {
     live &= ~(((1ull << kPer) - 1) << p);
     return p;
   };
-  // Lane (g, i) holds, of each sub-block s = i / 4, tokens 4 q + i % 4 in tile q, dims 32 g ..
-  // +31, so that lane (g, n) gets row n's scores of sub-block g's tokens in order.
+  // Of sub-block q lane (g, i) holds token i, dims 32 g .. +31: each load stays in a page, and
+  // lane (g, n) gets row n's scores of tokens 4 g .. 4 g + 3 of each.
   struct Loaded {
-    u32x4 k[4], v[4];        // codes
-    uint32_t k_pow, v_pow;   // tile q's power in byte q
-    int keep;                // attended tokens of sub-block s, in the lower half those of sub-block g
-    bool whole;              // all of every sub-block
+    u32x4 k[4], v[4];              // codes
+    uint32_t k_pow[4], v_pow[4];
   };
-  const int s_in = BS == 16 ? 0 : (i >> 2) & 1;  // sub-block s in its block
-  const uint32_t codes_at = t.h * BS * kQ4Codes + s_in * 1024 + (i & 3) * kQ4Codes + g * 16;
-  const uint32_t power_at = a.Hkv * BS * kQ4Codes + t.h * BS * kQ4Powers + s_in * 64 + ((i & 3) * 4 + g) * 4;
+  const uint32_t codes_at = t.h * BS * kQ4Codes, power_at = a.Hkv * BS * kQ4Codes + t.h * BS * kQ4Powers;
+  const uint32_t code_of = i * kQ4Codes + g * 16, power_of = ((i & 3) * 4 + g) * 4 + (i >> 2);
   Loaded u;
-  // (for a wave without a next unit the first bytes of page 0 stand in)
-  long long page_at = 0;
+  // where the next unit's sub-blocks are, and their attended tokens (for a wave without a next
+  // unit the first bytes of page 0 stand in)
+  long long page_at[kPer];
+  int keeps;  // five bits each
   auto find = [&](int p) __attribute__((always_inline)) {
-    const int from = p < 0 ? 0 : p + (BS == 16 ? i >> 2 : i >> 3);
-    page_at = p < 0 ? 0 : __shfl(place, from) * a.page_bytes;
-    auto keep_of = [&](int sub) __attribute__((always_inline)) {
-      const int n = __shfl(count, p < 0 ? 0 : p + (BS == 16 ? sub : sub >> 1)) - (BS == 16 ? 0 : (sub & 1) * 16);
-      return p < 0 || n < 0 ? 0 : (n > 16 ? 16 : n);
-    };
-    const int mine = keep_of(g);
-    u.whole = __builtin_amdgcn_ballot_w64(mine == 16) == ~0ull;
-    u.keep = u.whole ? 16 << 16 | 16 : keep_of(i >> 2) << 16 | mine;
+    keeps = 0;
+#pragma unroll
+    for (int b = 0; b < kPer; ++b) {
+      page_at[b] = p < 0 ? 0 : (long long)__builtin_amdgcn_readlane(place, p + b) * a.page_bytes;
+      const int n = p < 0 ? 0 : __builtin_amdgcn_readlane(count, p + b);
+      if constexpr (BS == 16) keeps |= n << (5 * b);
+      else keeps |= (n > 16 ? 16 | (n - 16) << 5 : n) << (10 * b);
+    }
   };
-  auto load_k = [&](int q) __attribute__((always_inline)) { u.k[q] = ldg16(a.k4 + page_at + codes_at + q * 256); };
-  auto load_v = [&](int q) __attribute__((always_inline)) { u.v[q] = ldg16(a.v4 + page_at + codes_at + q * 256); };
-  auto load_pow = [&](const uint8_t* pages) __attribute__((always_inline)) {
-    return *reinterpret_cast<const uint32_t*>(pages + page_at + power_at);
+  auto load = [&](const uint8_t* pages, int q, u32x4& codes, uint32_t& power) __attribute__((always_inline)) {
+    const uint8_t* at = pages + page_at[BS == 16 ? q : q >> 1] + (BS == 16 ? 0 : q & 1) * 1024;
+    codes = ldg16_once<STREAM>(at + codes_at + code_of);
+    at -= (BS == 16 ? 0 : q & 1) * (1024 - 64);
+    power = at[power_at + power_of];
   };
+  constexpr int kWhole = 16 | 16 << 5 | 16 << 10 | 16 << 15;
 
   bf16x8 qb[NT][4];
 #pragma unroll
@@ -257,45 +266,44 @@ __global__ __launch_bounds__(kQW * 64) void q4_attn_kernel(AttnQ4Args a) {
     u32x4 tk[4][4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      const int j = min(16 * (i >> 2) + 4 * q + (i & 3), t.tlen - 1);
+      const int j = min(16 * q + i, t.tlen - 1);
 #pragma unroll
       for (int st = 0; st < 4; ++st) tk[q][st] = ldg16(a.tree_k + t.tree_base + j * t.tree_row + g * 32 + st * 8);
     }
     const uint64_t anc = ancestors(tree_parent(a, t.r, t.tlen, lane), t.tlen, lane);
     s_anc[lane] = anc;
     float p[NT][16];
+    f32x4 sc[NT][4];
 #pragma unroll
     for (int v = 0; v < NT; ++v) {
-      f32x4 sc[4];
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        sc[q] = f32x4{0.f, 0.f, 0.f, 0.f};
+        sc[v][q] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int st = 0; st < 4; ++st)
-          sc[q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(tk[q][st]), qb[v][st], sc[q], 0, 0, 0);
+          sc[v][q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(tk[q][st]), qb[v][st], sc[v][q], 0, 0, 0);
       }
       const int row = t.row0 + v * 16 + i;
       const int tq = row < a.rows ? a.by_g(row) : 0;
       const uint32_t lo = __shfl((uint32_t)anc, tq), hi = __shfl((uint32_t)(anc >> 32), tq);
-      const uint32_t bits = (g < 2 ? lo : hi) >> (16 * (g & 1));
 #pragma unroll
       for (int q = 0; q < 4; ++q)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sc[q][e] = bits >> (4 * q + e) & 1 ? sc[q][e] : -INFINITY;
-      softmax16(sc, a.scale_log2, a.top, m_neg[v], l_run[v], acc[v], p[v]);
+        for (int e = 0; e < 4; ++e)
+          sc[v][q][e] = (q < 2 ? lo : hi) >> (16 * (q & 1) + 4 * g + e) & 1 ? sc[v][q][e] : -INFINITY;
     }
+    softmax16(sc, a.scale_log2, a.top, m_neg, l_run, acc, p);
     u32x4* sv = reinterpret_cast<u32x4*>(s_wave[wave]);  // [dim][group of tokens], 8 tokens each
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
       u32x4 tv[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const int j = min(16 * g + 8 * half + e, t.tlen - 1);
-        tv[e] = ldg16(a.tree_v + t.tree_base + j * t.tree_row + i * 8);
+        const int j = 32 * half + 16 * (e >> 2) + 4 * g + (e & 3);
+        tv[e] = ldg16(a.tree_v + t.tree_base + min(j, t.tlen - 1) * t.tree_row + i * 8);
+        if (j >= t.tlen) tv[e] = u32x4{0, 0, 0, 0};
       }
       transpose8(tv);
-      const int n = t.tlen - 16 * g - 8 * half;
-      clear_tokens(tv, n < 0 ? 0 : (n > 8 ? 8 : n));
       wild |= take_wild(tv);
 #pragma unroll
       for (int j = 0; j < 8; ++j) sv[(8 * i + j) * 4 + g] = tv[j];
@@ -327,66 +335,61 @@ __global__ __launch_bounds__(kQW * 64) void q4_attn_kernel(AttnQ4Args a) {
   chunk_set();
   int cur = next();
   find(cur);
-  u.v_pow = load_pow(a.v4);
 #pragma unroll
-  for (int q = 0; q < 4; ++q) load_v(q);
-  u.k_pow = load_pow(a.k4);
+  for (int q = 0; q < 4; ++q) load(a.v4, q, u.v[q], u.v_pow[q]);
 #pragma unroll
-  for (int q = 0; q < 4; ++q) load_k(q);
+  for (int q = 0; q < 4; ++q) load(a.k4, q, u.k[q], u.k_pow[q]);
   while (cur >= 0) {
-    // A tile's registers take the next unit's codes as soon as this one's are turned: the time
-    // to the next use is what hides the latency, 8.5 KB a wave on their way.
+    // A sub-block's registers take the next unit's codes as soon as this one's are turned: the
+    // time to the next use is what hides the latency, 8.5 KB a wave on their way.
     const int nxt = next();
-    const int keep = u.keep;
-    const bool whole = u.whole;
-    const uint32_t v_pow = u.v_pow, k_pow = u.k_pow;
+    const int keep = keeps;
     find(nxt);
-    // values into LDS
+    if (keep != kWhole) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      float s = power_f32(v_pow, q);
-      if (!whole && 4 * q + (i & 3) >= keep >> 16) {  // 0 times what an unused place holds must stay 0
-        s = 1.f;
-        u.v[q] = u32x4{0, 0, 0, 0};
-      }
-#pragma unroll
-      for (int c = 0; c < 4; ++c)
-        *reinterpret_cast<bf16x8*>(put + (c >> 1) * 2048 + q * 512 + (((c & 1) << 4) ^ swap)) = eight_bf16(u.v[q][c], s);
-      __builtin_amdgcn_sched_barrier(0);
-      if (q == 0) u.v_pow = load_pow(a.v4);
-      load_v(q);
+      for (int q = 0; q < 4; ++q)
+        if (i >= (keep >> (5 * q) & 31)) {  // 0 times what an unused place holds must stay 0
+          u.v_pow[q] = 127;
+          u.v[q] = u32x4{0, 0, 0, 0};
+        }
     }
-    // scores
     f32x4 sc[NT][4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      const float s = power_f32(k_pow, q);
+      // values into LDS
+      const float sv = __uint_as_float(u.v_pow[q] << 23);
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        *reinterpret_cast<bf16x8*>(put + (c >> 1) * 2048 + q * 512 + (((c & 1) << 4) ^ swap)) = eight_bf16(u.v[q][c], sv);
+      // scores
+      const float sk = __uint_as_float(u.k_pow[q] << 23);
 #pragma unroll
       for (int v = 0; v < NT; ++v) sc[v][q] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int st = 0; st < 4; ++st) {
-        const bf16x8 kb = eight_bf16(u.k[q][st], s);
+        const bf16x8 kb = eight_bf16(u.k[q][st], sk);
 #pragma unroll
         for (int v = 0; v < NT; ++v) sc[v][q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kb, qb[v][st], sc[v][q], 0, 0, 0);
       }
       __builtin_amdgcn_sched_barrier(0);
-      if (q == 0) u.k_pow = load_pow(a.k4);
-      load_k(q);
+      load(a.v4, q, u.v[q], u.v_pow[q]);
+      load(a.k4, q, u.k[q], u.k_pow[q]);
     }
-    bf16x8 pb[NT][2];
+    if (keep != kWhole) {
 #pragma unroll
-    for (int v = 0; v < NT; ++v) {
-      if (!whole) {
+      for (int v = 0; v < NT; ++v)
 #pragma unroll
         for (int q = 0; q < 4; ++q)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) sc[v][q][e] = 4 * q + e < (keep & 0xFFFF) ? sc[v][q][e] : -INFINITY;
-      }
-      float p[16];
-      softmax16(sc[v], a.scale_log2, a.top, m_neg[v], l_run[v], acc[v], p);
-#pragma unroll
-      for (int e = 0; e < 16; ++e) pb[v][e >> 3][e & 7] = (__bf16)p[e];
+          for (int e = 0; e < 4; ++e) sc[v][q][e] = 4 * g + e < (keep >> (5 * q) & 31) ? sc[v][q][e] : -INFINITY;
     }
+    float p[NT][16];
+    softmax16(sc, a.scale_log2, a.top, m_neg, l_run, acc, p);
+    bf16x8 pb[NT][2];
+#pragma unroll
+    for (int v = 0; v < NT; ++v)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) pb[v][e >> 3][e & 7] = (__bf16)p[v][e];
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
     for (int dt = 0; dt < 8; ++dt) {
@@ -736,10 +739,16 @@ template <int BS, bool SELECT>
 void launch_bs_q4(const AttnQ4Args& a, hipStream_t s) {
   const long long runs = (long long)a.R * a.Hkv * a.nsplit;
   const dim3 grid((unsigned)(a.by_length ? (runs + 7) / 8 * 8 * a.groups : (runs * a.groups + 7) / 8 * 8));
+  // What the tables and selections hold at most: past kStreamBytes the codes are read past
+  // the caches (whole lines a load).
+  const long long blocks = SELECT && a.k_sel + 1ll < a.NBmax ? a.k_sel + 1ll : a.NBmax;
+  const bool stream = (long long)a.R * a.Hkv * blocks * BS * 2 * (kQ4Codes + kQ4Powers) >= kStreamBytes;
   if (a.tiles == 1)
-    hipLaunchKernelGGL((q4_attn_kernel<1, BS, SELECT>), grid, dim3(kQW * 64), 0, s, a);
+    hipLaunchKernelGGL((stream ? q4_attn_kernel<1, BS, SELECT, true> : q4_attn_kernel<1, BS, SELECT, false>), grid,
+                       dim3(kQW * 64), 0, s, a);
   else if (a.tiles == 2)
-    hipLaunchKernelGGL((q4_attn_kernel<2, BS, SELECT>), grid, dim3(kQW * 64), 0, s, a);
+    hipLaunchKernelGGL((stream ? q4_attn_kernel<2, BS, SELECT, true> : q4_attn_kernel<2, BS, SELECT, false>), grid,
+                       dim3(kQW * 64), 0, s, a);
   else if (a.tiles <= kRowPlaces)
     hipLaunchKernelGGL((q4_attn_rows_kernel<1, BS, SELECT>), grid, dim3(kRowsThreads), 0, s, a);
   else
