@@ -117,25 +117,28 @@ __device__ __forceinline__ void load_q4_queries(const TreeAttnArgs& a, const Q4I
   }
 }
 
-// The online softmax of tree_attn.hip over a lane's 16 scores: probabilities not yet rounded.
-__device__ __forceinline__ float exp16(const f32x4 (&s)[4], float scale, float m_neg, float (&p)[16]) {
-  float sum[4];
+// The online softmax of tree_attn.hip over a lane's 4 U scores of each tile, with one branch
+// for all tiles: probabilities not yet rounded.
+template <int U>
+__device__ __forceinline__ float exp_of(const f32x4 (&s)[U], float scale, float m_neg, float (&p)[4 * U]) {
+  float sum[U];
 #pragma unroll
-  for (int u = 0; u < 4; ++u) {
+  for (int u = 0; u < U; ++u) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) p[4 * u + e] = fast_exp2(__builtin_fmaf(s[u][e], scale, m_neg));
     sum[u] = (p[4 * u] + p[4 * u + 1]) + (p[4 * u + 2] + p[4 * u + 3]);
   }
-  return (sum[0] + sum[1]) + (sum[2] + sum[3]);
+  if constexpr (U == 4) return (sum[0] + sum[1]) + (sum[2] + sum[3]);
+  else return sum[0] + sum[1];
 }
-template <int NT>
-__device__ __forceinline__ void softmax16(const f32x4 (&s)[NT][4], float scale, float top, float (&m_neg)[NT],
-                                          float (&l_part)[NT], f32x4 (&acc)[NT][8], float (&p)[NT][16]) {
+template <int NT, int U>
+__device__ __forceinline__ void softmax_of(const f32x4 (&s)[NT][U], float scale, float top, float (&m_neg)[NT],
+                                           float (&l_part)[NT], f32x4 (&acc)[NT][8], float (&p)[NT][4 * U]) {
   float psum[NT];
   bool over = false;
 #pragma unroll
   for (int v = 0; v < NT; ++v) {
-    psum[v] = exp16(s[v], scale, m_neg[v], p[v]);
+    psum[v] = exp_of(s[v], scale, m_neg[v], p[v]);
     over |= !(psum[v] <= top);
   }
   if (__builtin_expect(__builtin_amdgcn_ballot_w64(over) != 0, 0)) {
@@ -146,7 +149,7 @@ __device__ __forceinline__ void softmax16(const f32x4 (&s)[NT][4], float scale, 
       const bool mine = rows >> (threadIdx.x & 15) & 1;
       float m = -INFINITY;
 #pragma unroll
-      for (int u = 0; u < 4; ++u) m = fmaxf(m, fmaxf(fmaxf(s[v][u][0], s[v][u][1]), fmaxf(s[v][u][2], s[v][u][3])));
+      for (int u = 0; u < U; ++u) m = fmaxf(m, fmaxf(fmaxf(s[v][u][0], s[v][u][1]), fmaxf(s[v][u][2], s[v][u][3])));
       m *= scale;
       m = fmaxf(m, __shfl_xor(m, 16));
       m = fmaxf(fmaxf(m, __shfl_xor(m, 32)) + tree_lift_of(top), -m_neg[v]);
@@ -156,7 +159,7 @@ __device__ __forceinline__ void softmax16(const f32x4 (&s)[NT][4], float scale, 
 #pragma unroll
       for (int dt = 0; dt < 8; ++dt) acc[v][dt] *= alpha;
       m_neg[v] = -m;
-      psum[v] = exp16(s[v], scale, m == -INFINITY ? 0.f : m_neg[v], p[v]);
+      psum[v] = exp_of(s[v], scale, m == -INFINITY ? 0.f : m_neg[v], p[v]);
     }
   }
 #pragma unroll
@@ -292,7 +295,7 @@ __global__ __launch_bounds__(kQW * 64) void q4_attn_kernel(AttnQ4Args a) {
         for (int e = 0; e < 4; ++e)
           sc[v][q][e] = (q < 2 ? lo : hi) >> (16 * (q & 1) + 4 * g + e) & 1 ? sc[v][q][e] : -INFINITY;
     }
-    softmax16(sc, a.scale_log2, a.top, m_neg, l_run, acc, p);
+    softmax_of(sc, a.scale_log2, a.top, m_neg, l_run, acc, p);
     u32x4* sv = reinterpret_cast<u32x4*>(s_wave[wave]);  // [dim][group of tokens], 8 tokens each
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
@@ -384,7 +387,7 @@ __global__ __launch_bounds__(kQW * 64) void q4_attn_kernel(AttnQ4Args a) {
           for (int e = 0; e < 4; ++e) sc[v][q][e] = 4 * g + e < (keep >> (5 * q) & 31) ? sc[v][q][e] : -INFINITY;
     }
     float p[NT][16];
-    softmax16(sc, a.scale_log2, a.top, m_neg, l_run, acc, p);
+    softmax_of(sc, a.scale_log2, a.top, m_neg, l_run, acc, p);
     bf16x8 pb[NT][2];
 #pragma unroll
     for (int v = 0; v < NT; ++v)
@@ -481,9 +484,9 @@ __global__ __launch_bounds__(kRowsThreads, NT == 1 ? 4 : 2) void q4_attn_rows_ke
   constexpr int kRows = NT * kRowPlaces * 16;
   constexpr int kPad = kHeadDim + 4;
   constexpr int kPer = kUnitTokens / BS;
-  constexpr int kAhead = 3;
+  constexpr int kBuffers = NT == 1 ? 2 : 3;
   constexpr int kMerge = (int)sizeof(float) * kRows * kPad;
-  __shared__ __align__(16) char s_buf[2 * kUnitBytes > kMerge ? 2 * kUnitBytes : kMerge];
+  __shared__ __align__(16) char s_buf[kBuffers * kUnitBytes > kMerge ? kBuffers * kUnitBytes : kMerge];
   __shared__ int2 s_list[kListBlocks];  // page and attended tokens of the segment's blocks
   __shared__ uint64_t s_anc[kTreeMaxTokens];
   __shared__ float s_ml[2][kRows];
@@ -536,29 +539,22 @@ __global__ __launch_bounds__(kRowsThreads, NT == 1 ? 4 : 2) void q4_attn_rows_ke
     uint32_t power;
     int keep;  // attended tokens
   };
-  // ---- the products of one unit: `keep` attended tokens of the team's two sub-blocks (16: all)
-  auto attend = [&](int buf, int keep0, int keep1, bool tree) __attribute__((always_inline)) {
+  // ---- the products of one unit
+  typedef short s16x4 __attribute__((ext_vector_type(4)));
+  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+  u32x4 kf[2][4], vf[8];
+  auto read_k = [&](int buf) __attribute__((always_inline)) {
     const char* kb = s_buf + buf * kUnitBytes + team * 8192 + lane * 16;
-    u32x4 kf[2][4];
 #pragma unroll
     for (int tau = 0; tau < 2; ++tau)
 #pragma unroll
       for (int st = 0; st < 4; ++st) kf[tau][st] = *reinterpret_cast<const u32x4*>(kb + tau * 4096 + st * 1024);
-    f32x4 sc[NT][2];
+  };
+  auto read_v = [&](int buf) __attribute__((always_inline)) {
+    char* vb = s_buf + buf * kUnitBytes + kKeysBytes + (team * 32 + 4 * g + (i >> 2)) * 32 +
+               ((((i & 3) >> 1) ^ (g & 1)) << 4) + (i & 1) * 8;
 #pragma unroll
-    for (int v = 0; v < NT; ++v) {
-      sc[v][0] = sc[v][1] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int st = 0; st < 4; ++st)
-#pragma unroll
-        for (int tau = 0; tau < 2; ++tau)
-          sc[v][tau] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(kf[tau][st]), qb[v][st], sc[v][tau], 0, 0, 0);
-    }
-    typedef short s16x4 __attribute__((ext_vector_type(4)));
-    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-    char* vb = s_buf + buf * kUnitBytes + kKeysBytes + (team * 32 + 4 * g + (i >> 2)) * 32 + ((((i & 3) >> 1) ^ (g & 1)) << 4) + (i & 1) * 8;
-    u32x4 vf[8];
-    auto read_v = [&](int dt) __attribute__((always_inline)) {
+    for (int dt = 0; dt < 8; ++dt)
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
         const u32x2 w = __builtin_bit_cast(
@@ -567,41 +563,54 @@ __global__ __launch_bounds__(kRowsThreads, NT == 1 ? 4 : 2) void q4_attn_rows_ke
         vf[dt][2 * q] = w[0];
         vf[dt][2 * q + 1] = w[1];
       }
-    };
-    __builtin_amdgcn_sched_barrier(0);  // no reads of values ahead of it, into more registers
-    if constexpr (NT > 1) {
+  };
+  f32x4 sc[NT][2];
+  auto scores = [&]() __attribute__((always_inline)) {
 #pragma unroll
-      for (int dt = 0; dt < 8; ++dt) read_v(dt);
-    }
-    if (keep0 < 16 || keep1 < 16 || tree) {
+    for (int v = 0; v < NT; ++v) sc[v][0] = sc[v][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int v = 0; v < NT; ++v) {
-        const int k0 = keep0 - 4 * g, k1 = keep1 - 4 * g;
-        uint32_t bits = (k0 <= 0 ? 0u : k0 >= 4 ? 15u : (1u << k0) - 1) | (k1 <= 0 ? 0u : k1 >= 4 ? 15u : (1u << k1) - 1) << 4;
-        if (tree) {
-          const int row = t.row0 + (rt + v * kRowPlaces) * 16 + i;
-          const uint64_t anc = s_anc[row < a.rows ? a.by_g(row) : 0];
-          bits = (uint32_t)(anc >> (team * 32 + 4 * g)) & 15u;
-          bits |= ((uint32_t)(anc >> (team * 32 + 16 + 4 * g)) & 15u) << 4;
-        }
-        mask_scores(sc[v], bits);
-      }
-    }
+    for (int st = 0; st < 4; ++st)
+#pragma unroll
+      for (int v = 0; v < NT; ++v)
+#pragma unroll
+        for (int tau = 0; tau < 2; ++tau)
+          sc[v][tau] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(kf[tau][st]), qb[v][st], sc[v][tau], 0, 0, 0);
+  };
+  // `keep` attended tokens of the team's two sub-blocks (16: all), or the tree's rows
+  auto mask = [&](int keep0, int keep1, bool tree) __attribute__((always_inline)) {
+    if (keep0 >= 16 && keep1 >= 16 && !tree) return;
 #pragma unroll
     for (int v = 0; v < NT; ++v) {
-      const bf16x8 pb = unit_softmax(sc[v], a.scale_log2, a.top, m_neg[v], l_run[v], acc[v]);
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        if constexpr (NT == 1) {
-          __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-          for (int dt = 4 * half; dt < 4 * half + 4; ++dt) read_v(dt);
-        }
-#pragma unroll
-        for (int dt = 4 * half; dt < 4 * half + 4; ++dt)
-          acc[v][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(vf[dt]), pb, acc[v][dt], 0, 0, 0);
+      const int k0 = keep0 - 4 * g, k1 = keep1 - 4 * g;
+      uint32_t bits = (k0 <= 0 ? 0u : k0 >= 4 ? 15u : (1u << k0) - 1) | (k1 <= 0 ? 0u : k1 >= 4 ? 15u : (1u << k1) - 1) << 4;
+      if (tree) {
+        const int row = t.row0 + (rt + v * kRowPlaces) * 16 + i;
+        const uint64_t anc = s_anc[row < a.rows ? a.by_g(row) : 0];
+        bits = (uint32_t)(anc >> (team * 32 + 4 * g)) & 15u;
+        bits |= ((uint32_t)(anc >> (team * 32 + 16 + 4 * g)) & 15u) << 4;
       }
+      mask_scores(sc[v], bits);
     }
+  };
+  bf16x8 pb[NT];
+  auto softmax = [&]() __attribute__((always_inline)) {
+    float p[NT][8];
+    softmax_of(sc, a.scale_log2, a.top, m_neg, l_run, acc, p);
+#pragma unroll
+    for (int v = 0; v < NT; ++v)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) pb[v][e] = (__bf16)p[v][e];
+  };
+  auto values = [&](int dt) __attribute__((always_inline)) {
+#pragma unroll
+    for (int v = 0; v < NT; ++v)
+      acc[v][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(vf[dt]), pb[v], acc[v][dt], 0, 0, 0);
+  };
+  auto attend = [&]() __attribute__((always_inline)) {
+    softmax();
+#pragma unroll
+    for (int dt = 0; dt < 8; ++dt) values(dt);
+    __builtin_amdgcn_sched_barrier(0);
   };
 
   for (int seg = u_begin; seg < u_end; seg += kListBlocks / kPer) {
@@ -639,31 +648,65 @@ __global__ __launch_bounds__(kRowsThreads, NT == 1 ? 4 : 2) void q4_attn_rows_ke
       const int n = __builtin_amdgcn_readfirstlane(s_list[s * kPer + (BS == 16 ? b : b >> 1)].y) - (BS == 16 ? 0 : (b & 1) * 16);
       return n > 16 ? 16 : n;
     };
-    Codes x[kAhead];
+    if constexpr (NT == 1) {
+      // Two workgroups share a CU, and hide each other's waits: two units in LDS.
+      constexpr int kAhead = 3;
+      Codes x[kAhead];
 #pragma unroll
-    for (int p = 0; p < kAhead; ++p) x[p] = load(p);
-    convert(0, x[0]);
-    x[0] = load(kAhead);
-    __syncthreads();
-    for (int s0 = 0; s0 < units; s0 += kAhead) {
+      for (int p = 0; p < kAhead; ++p) x[p] = load(p);
+      convert(0, x[0]);
+      x[0] = load(kAhead);
+      __syncthreads();
+      for (int s0 = 0; s0 < units; s0 += kAhead) {
 #pragma unroll
-      for (int p = 0; p < kAhead; ++p) {
-        const int s = s0 + p;
-        if (s >= units) break;
-        Codes& nx = x[(p + 1) % kAhead];
-        if (s + 1 < units) {
-          convert((s + 1) & 1, nx);
-          nx = load(s + 1 + kAhead);
+        for (int p = 0; p < kAhead; ++p) {
+          const int s = s0 + p;
+          if (s >= units) break;
+          if (s + 1 < units) {
+            convert((s + 1) & 1, x[(p + 1) % kAhead]);
+            x[(p + 1) % kAhead] = load(s + 1 + kAhead);
+          }
+          read_k(s & 1);
+          scores();
+          mask(keep_of(s, 2 * team), keep_of(s, 2 * team + 1), false);
+          __builtin_amdgcn_sched_barrier(0);  // no reads of values ahead of it, into more registers
+          softmax();
+          __builtin_amdgcn_sched_barrier(0);
+          read_v(s & 1);
+#pragma unroll
+          for (int dt = 0; dt < 8; ++dt) values(dt);
+          __syncthreads();
         }
-        attend(s & 1, keep_of(s, 2 * team), keep_of(s, 2 * team + 1), false);
+      }
+    } else {
+      // One workgroup a CU: LDS reads run beside the products, V ahead of the scores and the
+      // next unit's K behind them, so three units are in LDS.
+      convert(0, load(0));
+      convert(1, load(1));
+      Codes x = load(2);
+      __syncthreads();
+      read_k(0);
+      int buf = 0;  // of unit s
+      for (int s = 0; s < units; ++s) {
+        const int next = buf < 2 ? buf + 1 : 0, after = next < 2 ? next + 1 : 0;
+        convert(after, x);
+        x = load(s + 3);
+        __builtin_amdgcn_sched_barrier(0);
+        read_v(buf);
+        scores();
+        __builtin_amdgcn_sched_barrier(0);
+        read_k(next);
+        mask(keep_of(s, 2 * team), keep_of(s, 2 * team + 1), false);
+        attend();
         __syncthreads();
+        buf = next;
       }
     }
   }
 
   // ---- the tree's own rows: a unit of the last split ----
+  __syncthreads();  // team 0's last unit is read, and s_wild is set where there was none
   if (t.split == a.nsplit - 1 && a.tree_k) {
-    __syncthreads();  // s_wild, where there was no unit
     if (wave == 0) s_anc[lane] = ancestors(tree_parent(a, t.r, t.tlen, lane), t.tlen, lane);
     const int j = sub * 16 + i;
     const uint16_t* row = (is_v ? a.tree_v : a.tree_k) + t.tree_base + min(j, t.tlen - 1) * t.tree_row + g * 32;
@@ -678,7 +721,13 @@ __global__ __launch_bounds__(kRowsThreads, NT == 1 ? 4 : 2) void q4_attn_rows_ke
 #pragma unroll
     for (int q = 0; q < 4; ++q) put(0, q, y[q]);
     __syncthreads();
-    if (team * 32 < t.tlen) attend(0, 16, 16, true);
+    if (team * 32 < t.tlen) {
+      read_k(0);
+      read_v(0);
+      scores();
+      mask(16, 16, true);
+      attend();
+    }
     __syncthreads();
   }
 

@@ -13,19 +13,38 @@ constexpr int kQ4Waves = 4;   // of a workgroup
 constexpr int kQ4RegisterTiles = 2;  // 16-row tiles up to which a wave converts for itself
 constexpr int kQ4Tiles = 8;   // 16-row tiles of a workgroup at most
 
+// Calls of more than four row tiles go two by two through the form for up to two all the
+// same where the row groups together read at most so many units. Measured, us with the form
+// for more rows and this one (8 heads, 128 rows: pairs x units): 8 x 8 17.9 and 14.8, 8 x 32
+// 18.5 and 15.6, 8 x 125 23.6 and 20.4, 16 x 125 27.5 and 29.0; 256 rows: 8 x 32 19.8 and
+// 18.0, 8 x 125 26.8 and 28.9.
+constexpr int kQ4SmallUnits = 4700;
+
+// `units`: 64-token units of the longest context or selection that the call can have.
+//
+// As many splits as fill the CUs, two workgroups each (one with more than four row tiles),
+// but the second one only with 16 units for each workgroup: a workgroup of a few units is
+// nearly all start and end. Measured, splits and us (pairs, rows, units): 64, 20, 33: 1 23.4,
+// 2 19.7, 4 16.7, 8 17.8; 8, 4, 31: 1 17.0, 2 14.2, 4 11.3, 8 9.7; 8, 20, 2,048: 8 120, 16
+// 68, 32 45, 64 43, 128 58; 64, 20, 2,048: 4 239, 8 197, 12 217, 16 210; 128, 72, 65: 1 84,
+// 2 55, 4 62; 16, 512, 1,024: 2 555, 4 291, 8 304.
 inline TreePlan q4_plan(long long pairs, int G, int T, int units) {
   TreePlan p{};
   p.rows = G * T;
-  const int tiles = (p.rows + 15) / 16;
-  p.groups = (tiles + kQ4Tiles - 1) / kQ4Tiles;
-  p.tiles = (tiles + p.groups - 1) / p.groups;
+  const int tiles = (p.rows + 15) / 16, twos = (tiles + 1) / 2;
+  const bool small = tiles > 4 && pairs * units * twos <= kQ4SmallUnits;
+  p.groups = small ? twos : (tiles + kQ4Tiles - 1) / kQ4Tiles;
+  p.tiles = small ? kQ4RegisterTiles : (tiles + p.groups - 1) / p.groups;
   p.units = units;
   const long long items = pairs * p.groups;
   const long long slots = p.tiles > 4 ? 256 : 512;
   long long most = (units + kQ4Waves - 1) / kQ4Waves;
   if (most > kTreeMaxSplits) most = kTreeMaxSplits;
   p.nsplit = 1;
-  while (items > 0 && p.nsplit * 2 <= most && items * p.nsplit < slots) p.nsplit *= 2;
+  while (items > 0 && p.nsplit * 2 <= most && items * p.nsplit < slots) {
+    if (items * p.nsplit * 2 > 256 && units < 16 * p.nsplit * 2) break;
+    p.nsplit *= 2;
+  }
   if (p.nsplit > 1) {
     p.part_o_floats = (std::size_t)pairs * p.nsplit * p.rows * 128;
     p.bytes = (std::size_t)pairs * p.nsplit * p.rows * 130 * sizeof(float);

@@ -1,8 +1,10 @@
 // Compressed keys of the 4-bit cache: per block and head the coordinate-wise maximum and
 // minimum of the keys as the cache holds them (summaries.hip), exact in bf16.
 //
-// Eight threads a (request, block, head), 16 dims each: a token's 8 bytes, two codes a
-// conversion with the token's power, then a maximum and a minimum a value.
+// A wave takes eight sub-blocks, 16 tokens of one head each: their codes come in whole lines,
+// a kilobyte a load, and pass through LDS to eight threads a sub-block, 16 dims each (8 of
+// the first 64 and 8 of the others, so that a row is written in whole lines): two codes a
+// conversion with their token's power, then a maximum and a minimum a value.
 #include <type_traits>
 
 #include "q4_internal.h"
@@ -12,33 +14,66 @@ namespace {
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
-template <int SEL>
-__device__ __forceinline__ f32x2 pair_of(uint32_t w, float scale) {
-  return __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, SEL);
+constexpr int kSubs = 8;             // sub-blocks of a wave
+constexpr int kSubStride = 1024 + 32;  // of a sub-block in LDS: the eight of a read meet no bank twice
+
+__device__ __forceinline__ void eight_f32(uint32_t w, float s, f32x2 (&v)[4]) {
+  v[0] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 0);
+  v[1] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 1);
+  v[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 2);
+  v[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 3);
+}
+__device__ __forceinline__ float across_eight(float x) {  // the value of the lane 8 further in its row of 16
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x128, 0xF, 0xF, false));
 }
 
 template <int BS>
 __global__ __launch_bounds__(256) void q4_summaries_kernel(SummaryQ4Args a) {
+  __shared__ __align__(16) char s_codes[4][kSubs * kSubStride];
+  __shared__ uint32_t s_powers[4][kSubs * 16];
+  constexpr int kPer = BS / 16;  // sub-blocks of an item (block, head)
   const int r = blockIdx.y;
-  const uint32_t item = blockIdx.x * 256 + threadIdx.x;  // below 2^31 (the entry point)
-  const int w = item & 7;
-  const int bh = item >> 3, at = a.by_hkv(bh), h = bh - at * a.Hkv;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const Ctx c = ctx_blocks(a.ctx_len[r], BS, a.NBmax);
   const int lo = a.prev_ctx_len ? ctx_blocks(a.prev_ctx_len[r], BS, a.NBmax).n_cand : 0;
-  if (a.prev_ctx_len && at >= a.max_new) return;
-  const long long b = (long long)lo + at;
-  if (b >= c.n_cand) return;
-  const int page = a.table[(long long)r * a.NBmax + b];
-  if (page < 0 || page >= a.num_pages) return;
-  const uint8_t* base = a.k + page * a.page_bytes;
-  const uint8_t* codes = base + h * BS * kQ4Codes + w * 8;
-  const uint32_t* powers = reinterpret_cast<const uint32_t*>(base + a.Hkv * BS * kQ4Codes + h * BS * kQ4Powers) + (w >> 1);
-  uint2 x[BS];
-  uint32_t p[BS / 4];
+  long long n = c.n_cand - lo;
+  if (a.prev_ctx_len && n > a.max_new) n = a.max_new;
+  const int item0 = (blockIdx.x * 4 + wave) * (kSubs / kPer);  // below 2^28 (the entry point)
+  if ((int)a.by_hkv(item0) >= n) return;
+  // this lane's item, in the lanes of its sub-block
+  const int sub = lane >> 3, w = lane & 7;
+  const int item = item0 + sub / kPer;
+  const int at = a.by_hkv(item), h = item - at * a.Hkv, b = lo + at;
+  int page = at < n ? a.table[(long long)r * a.NBmax + b] : -1;
+  const bool ok = page >= 0 && page < a.num_pages;
+  page = ok ? page : 0;
+  const long long from = page * a.page_bytes;
+  const int codes_at = (h * BS + sub % kPer * 16) * kQ4Codes;
+  const int powers_at = a.Hkv * BS * kQ4Codes + (h * BS + sub % kPer * 16) * kQ4Powers;
+  const bool stream = (long long)a.R * n * a.Hkv * (BS * (kQ4Codes + kQ4Powers)) >= kStreamBytes;
+  u32x4 x[kSubs];
+  auto load = [&](auto past) __attribute__((always_inline)) {
 #pragma unroll
-  for (int t = 0; t < BS; ++t) x[t] = *reinterpret_cast<const uint2*>(codes + t * kQ4Codes);
+    for (int q = 0; q < kSubs; ++q) {
+      const long long f = __shfl(from, 8 * q);
+      const int o = __shfl(codes_at, 8 * q);
+      x[q] = ldg16_once<decltype(past)::value>(a.k + f + o + lane * 16);
+    }
+  };
+  // (the marks keep the compiler from folding the two forms into one)
+  if (stream) {
+    asm volatile("; read past the caches");
+    load(std::true_type{});
+    asm volatile("; read past the caches");
+  } else {
+    load(std::false_type{});
+  }
+  const uint2 pw = *reinterpret_cast<const uint2*>(a.k + from + powers_at + w * 8);
+  char* const s = s_codes[wave];
 #pragma unroll
-  for (int q = 0; q < BS / 4; ++q) p[q] = powers[(q >> 2) * 16 + (q & 3) * 4];  // tokens q % 4 + 4 u of 16
+  for (int q = 0; q < kSubs; ++q) *reinterpret_cast<u32x4*>(s + q * kSubStride + lane * 16) = x[q];
+  *reinterpret_cast<uint2*>(&s_powers[wave][lane * 2]) = pw;
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   float mx[16], mn[16];
 #pragma unroll
   for (int j = 0; j < 16; ++j) {
@@ -46,28 +81,53 @@ __global__ __launch_bounds__(256) void q4_summaries_kernel(SummaryQ4Args a) {
     mn[j] = INFINITY;
   }
 #pragma unroll
-  for (int t = 0; t < BS; ++t) {
-    const float s = __uint_as_float((p[(t >> 4) * 4 + (t & 3)] >> (8 * ((t >> 2) & 3)) & 255u) << 23);
-    const f32x2 v[8] = {pair_of<0>(x[t].x, s), pair_of<1>(x[t].x, s), pair_of<2>(x[t].x, s), pair_of<3>(x[t].x, s),
-                        pair_of<0>(x[t].y, s), pair_of<1>(x[t].y, s), pair_of<2>(x[t].y, s), pair_of<3>(x[t].y, s)};
+  for (int e = 0; e < 4; ++e) {  // tokens e + 4 u
+    const uint32_t p0 = s_powers[wave][sub * 16 + e * 4 + (w >> 2)], p1 = s_powers[wave][sub * 16 + e * 4 + 2 + (w >> 2)];
 #pragma unroll
-    for (int j = 0; j < 16; ++j) {
-      mx[j] = fmaxf(mx[j], v[j >> 1][j & 1]);
-      mn[j] = fminf(mn[j], v[j >> 1][j & 1]);
+    for (int u = 0; u < 4; ++u) {
+      const char* row = s + sub * kSubStride + (e + 4 * u) * kQ4Codes + w * 4;
+      f32x2 v[2][4];
+      eight_f32(*reinterpret_cast<const uint32_t*>(row), __uint_as_float((p0 >> (8 * u) & 255u) << 23), v[0]);
+      eight_f32(*reinterpret_cast<const uint32_t*>(row + 32), __uint_as_float((p1 >> (8 * u) & 255u) << 23), v[1]);
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        mx[j] = fmaxf(mx[j], v[j >> 3][j >> 1 & 3][j & 1]);
+        mn[j] = fminf(mn[j], v[j >> 3][j >> 1 & 3][j & 1]);
+      }
     }
   }
-  const long long o = (((long long)r * a.Hkv + h) * a.NBmax + b) * kHeadDim + w * 16;
+  if constexpr (BS == 32) {  // the item's other sub-block
 #pragma unroll
-  for (int half = 0; half < 2; ++half) {
-    u32x4 omx, omn;
+    for (int j = 0; j < 16; ++j) {
+      mx[j] = fmaxf(mx[j], across_eight(mx[j]));
+      mn[j] = fminf(mn[j], across_eight(mn[j]));
+    }
+  }
+  if (!ok) return;
+  const long long o = (((long long)r * a.Hkv + h) * a.NBmax + b) * kHeadDim + w * 8;
+  u32x4 rows[2][2];  // kmax, kmin; the first and the other 64 dims
+#pragma unroll
+  for (int half = 0; half < 2; ++half)
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const int j = half * 8 + 2 * q;  // exact: the values are bf16
-      omx[q] = (__float_as_uint(mx[j]) >> 16) | (__float_as_uint(mx[j + 1]) & 0xFFFF0000u);
-      omn[q] = (__float_as_uint(mn[j]) >> 16) | (__float_as_uint(mn[j + 1]) & 0xFFFF0000u);
+      rows[0][half][q] = (__float_as_uint(mx[j]) >> 16) | (__float_as_uint(mx[j + 1]) & 0xFFFF0000u);
+      rows[1][half][q] = (__float_as_uint(mn[j]) >> 16) | (__float_as_uint(mn[j + 1]) & 0xFFFF0000u);
     }
-    *reinterpret_cast<u32x4*>(a.kmax + o + half * 8) = omx;
-    *reinterpret_cast<u32x4*>(a.kmin + o + half * 8) = omn;
+  auto store = [&](uint16_t* to, u32x4 v) __attribute__((always_inline)) {
+    if (stream) __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(to));
+    else *reinterpret_cast<u32x4*>(to) = v;
+  };
+  if constexpr (BS == 16) {
+    store(a.kmax + o, rows[0][0]);
+    store(a.kmax + o + 64, rows[0][1]);
+    store(a.kmin + o, rows[1][0]);
+    store(a.kmin + o + 64, rows[1][1]);
+  } else {  // a sub-block's lanes each write one of the two
+    const int which = sub & 1;
+    uint16_t* const to = which ? a.kmin : a.kmax;
+    store(to + o, which ? rows[1][0] : rows[0][0]);
+    store(to + o + 64, which ? rows[1][1] : rows[0][1]);
   }
 }
 
@@ -75,8 +135,8 @@ __global__ __launch_bounds__(256) void q4_summaries_kernel(SummaryQ4Args a) {
 
 hipError_t launch_summaries_q4(const SummaryQ4Args& a, hipStream_t s) {
   const long long blocks = a.prev_ctx_len ? (a.max_new < a.NBmax ? a.max_new : a.NBmax) : a.NBmax;
-  const long long items = blocks * a.Hkv * 8;
-  const dim3 grid((unsigned)((items + 255) / 256), (unsigned)a.R);
+  const long long per_group = 4 * kSubs / (a.B / 16);  // (block, head) items of a workgroup
+  const dim3 grid((unsigned)((blocks * a.Hkv + per_group - 1) / per_group), (unsigned)a.R);
   if (a.B == 16)
     hipLaunchKernelGGL(q4_summaries_kernel<16>, grid, dim3(256), 0, s, a);
   else
