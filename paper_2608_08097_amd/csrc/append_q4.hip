@@ -39,6 +39,7 @@ __device__ __forceinline__ uint32_t quad_max(uint32_t x) {
 template <bool ROTATE>
 __global__ __launch_bounds__(kQAThreads) void q4_append_kernel(AppendQ4Args a) {
   __shared__ double2 s_cs[ROTATE ? kQATokens : 1][kHeadDim / 2];
+  __shared__ int2 s_at[kQATokens];  // a token's row of the new ones (-1: it is not written) and its page
   const int r = blockIdx.y;
   const long long cap = (long long)a.NBmax * a.B;
   long long ctx = a.ctx_len[r];
@@ -50,31 +51,57 @@ __global__ __launch_bounds__(kQAThreads) void q4_append_kernel(AppendQ4Args a) {
   const int i0 = blockIdx.x * a.tokens;
   const int mine = min(n - i0, a.tokens);
   if (mine <= 0) return;
-  if constexpr (ROTATE) {
+  if ((int)threadIdx.x < mine) {
+    const int i = i0 + threadIdx.x;
+    const int row = a.path ? a.path[(long long)r * a.T + i] : i;
+    const int page = a.table[(long long)r * a.NBmax + ((ctx + i) >> (a.B == 16 ? 4 : 5))];
+    const bool ok = row >= 0 && row < a.T && page >= 0 && page < a.num_pages;
+    s_at[threadIdx.x] = make_int2(ok ? row : -1, page);
+  }
+  __syncthreads();
+  const int heads = 2 * a.Hkv;
+  const int w = threadIdx.x & 15, d0 = 8 * w;  // this lane's dims
+  // whole waves stay together: the quads exchange their maxima
+  const int end = (mine * heads + 3) / 4 * 4;
+  struct Entry {
+    int t, h, row, page;
+    bool is_v;
+    const uint16_t* src;
+    u32x4 x;
+  };
+  auto fetch = [&](int e) __attribute__((always_inline)) {
+    Entry y;
+    const bool in = e < mine * heads;
+    y.t = in ? a.by_heads(e) : 0;
+    const int hh = in ? e - y.t * heads : 0;
+    const bool upper = hh >= a.Hkv;
+    y.is_v = upper != (bool)(y.t & 1);  // in turn, so that every SIMD has its share of the rotations
+    y.h = upper ? hh - a.Hkv : hh;
+    const int2 at = s_at[y.t];
+    y.row = in ? at.x : -1;
+    y.page = at.y;
+    const long long from = (long long)r * a.T + (y.row < 0 ? 0 : y.row);
+    y.src = (y.is_v ? a.new_v + from * a.v_stride : a.new_k + from * a.k_stride) + y.h * kHeadDim;
+    y.x = ldg16(y.src + d0);
+    return y;
+  };
+  Entry ahead{};
+  if ((int)threadIdx.x >> 4 < end) ahead = fetch(threadIdx.x >> 4);
+  if constexpr (ROTATE) {  // behind the first loads
     for (int e = threadIdx.x; e < mine * 64; e += kQAThreads) {
       const int t = e >> 6, pair = e & 63;
       if (pair < a.rot.half) s_cs[t][pair] = rotary_cos_sin(a.rot, ctx + i0 + t, pair);
     }
     __syncthreads();
   }
-  const int heads = 2 * a.Hkv;
-  const int w = threadIdx.x & 15, d0 = 8 * w;  // this lane's dims
-  // whole waves stay together: the quads exchange their maxima
-  for (int e = threadIdx.x >> 4; e < (mine * heads + 3) / 4 * 4; e += kQAThreads / 16) {
-    const bool in = e < mine * heads;
-    const int t = in ? a.by_heads(e) : 0, hh = in ? e - t * heads : 0;
-    const bool is_v = hh >= a.Hkv;
-    const int h = is_v ? hh - a.Hkv : hh, i = i0 + t;
-    const int row = a.path ? a.path[(long long)r * a.T + i] : i;
-    const long long pos = ctx + i;
-    const int block = (int)(pos >> (a.B == 16 ? 4 : 5)), tok = (int)(pos & (a.B - 1));
-    const int page = a.table[(long long)r * a.NBmax + block];
-    const bool ok = in && row >= 0 && row < a.T && page >= 0 && page < a.num_pages;
-    const long long from = (long long)r * a.T + (ok ? row : 0);
-    const uint16_t* src = (is_v ? a.new_v + from * a.v_stride : a.new_k + from * a.k_stride) + h * kHeadDim;
-    const u32x4 x = ldg16(src + d0);
+  for (int e = threadIdx.x >> 4; e < end; e += kQAThreads / 16) {
+    const Entry cur = ahead;
+    if (e + kQAThreads / 16 < end) ahead = fetch(e + kQAThreads / 16);
+    const int t = cur.t, h = cur.h, i = i0 + t, tok = (int)((ctx + i) & (a.B - 1));
+    const bool is_v = cur.is_v, ok = cur.row >= 0;
+    const uint16_t* src = cur.src;
+    const u32x4 x = cur.x;
     float f[8];
-    bool wild = false;
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
       f[2 * p] = bf16_bits_to_f32(x[p] & 0xFFFFu);
@@ -132,7 +159,7 @@ __global__ __launch_bounds__(kQAThreads) void q4_append_kernel(AppendQ4Args a) {
       top = top > b ? top : b;
     }
     top = quad_max(top);
-    wild = top >= 0x7F800000u;
+    const bool wild = top >= 0x7F800000u;
     // exponent of the largest value, one more past 1.75 of its power, less 2
     int byte = (int)((top + 0x1FFFFFu) >> 23) - 2;
     byte = wild ? kQ4NaN : (byte < 1 ? 1 : (byte > 252 ? 252 : byte));
@@ -144,7 +171,7 @@ __global__ __launch_bounds__(kQAThreads) void q4_append_kernel(AppendQ4Args a) {
     codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, f[6], f[7], scale, 3);
     codes = wild ? 0 : codes;
     if (!ok) continue;
-    uint8_t* dst = (is_v ? a.v : a.k) + page * a.page_bytes;
+    uint8_t* dst = (is_v ? a.v : a.k) + cur.page * a.page_bytes;
     *reinterpret_cast<uint32_t*>(dst + (h * a.B + tok) * kQ4Codes + 4 * w) = codes;
     if ((w & 3) == 0) dst[a.Hkv * a.B * kQ4Codes + q4_power_at(h, a.B, tok, w >> 2)] = (uint8_t)byte;
     uint16_t* read = is_v ? a.read_v : a.read_k;
@@ -154,7 +181,8 @@ __global__ __launch_bounds__(kQAThreads) void q4_append_kernel(AppendQ4Args a) {
       y[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1));
       y[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2));
       y[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3));
-      *reinterpret_cast<u32x4*>(read + (((long long)r * a.T + i) * a.Hkv + h) * kHeadDim + d0) = y;
+      // whole lines, which nothing reads soon where they are many
+      __builtin_nontemporal_store(y, reinterpret_cast<u32x4*>(read + (((long long)r * a.T + i) * a.Hkv + h) * kHeadDim + d0));
     }
   }
 }

@@ -28,7 +28,7 @@ __device__ __forceinline__ float across_eight(float x) {  // the value of the la
 }
 
 template <int BS>
-__global__ __launch_bounds__(256) void q4_summaries_kernel(SummaryQ4Args a) {
+__global__ __launch_bounds__(256, 4) void q4_summaries_kernel(SummaryQ4Args a) {
   __shared__ __align__(16) char s_codes[4][kSubs * kSubStride];
   __shared__ uint32_t s_powers[4][kSubs * 16];
   constexpr int kPer = BS / 16;  // sub-blocks of an item (block, head)
