@@ -10,7 +10,7 @@ namespace oasis {
 namespace {
 
 constexpr int kRotThreads = 256;
-constexpr int kRotTokens = 8;  // rows of a workgroup at most
+constexpr int kRotTokens = 2;  // rows of a workgroup at most
 
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
@@ -63,17 +63,18 @@ __global__ __launch_bounds__(kRotThreads) void rotate_kernel(RotateArgs a) {
         dst[j] = src[j];
       }
     } else if (a.rot.interleaved) {
-      u32x4 v[2] = {ldg16(src + 16 * w), ldg16(src + 16 * w + 8)};
+      u32x4 v[2] = {ldg16(src + 8 * w), ldg16(src + 64 + 8 * w)};
 #pragma unroll
       for (int p = 0; p < 8; ++p) {
+        const int pair = (p >> 2) * 32 + 4 * w + (p & 3);
         const uint32_t x = v[p >> 2][p & 3];
-        const float2 c = cs[8 * w + p];  // (past the pairs: not used)
+        const float2 c = cs[pair];  // (past the pairs: not used)
         const float lo = bf16_lo(x), hi = bf16_hi(x);
         const uint32_t y = pack_bf16(lo * c.x - hi * c.y, hi * c.x + lo * c.y);
-        v[p >> 2][p & 3] = 8 * w + p < half ? y : x;
+        v[p >> 2][p & 3] = pair < half ? y : x;
       }
-      *reinterpret_cast<u32x4*>(dst + 16 * w) = v[0];
-      *reinterpret_cast<u32x4*>(dst + 16 * w + 8) = v[1];
+      *reinterpret_cast<u32x4*>(dst + 8 * w) = v[0];
+      *reinterpret_cast<u32x4*>(dst + 64 + 8 * w) = v[1];
     } else {
       const bool turns = 8 * w < half;
       const int i = turns ? 8 * w : 16 * w, j = turns ? i + half : i + 8;
