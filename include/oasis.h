@@ -567,8 +567,8 @@ OASIS_API oasis_status oasis_update_summaries_q4(const oasis_dims* dims, const u
  * Attention over the 4-bit cache: oasis_tree_attn, over the values that the pages stand
  * for. sel, sel_count and k (the output of oasis_select_topk, 1 <= k <= 65536): of the
  * cache each KV head attends the blocks sel[r][h][0..sel_count) and the local block,
- * read from the pages; ids outside [0, n_cand_r) are left out. sel and sel_count NULL
- * and k = 0: every block. tree_k and tree_v both NULL: the T rows attend the cache
+ * read from the pages; ids outside [0, n_cand_r) are left out, one listed twice is
+ * attended twice. sel and sel_count NULL and k = 0: every block. tree_k and tree_v both NULL: the T rows attend the cache
  * alone (parent is not looked at), each without a mask among them, as in
  * oasis_sparse_decode_attn. A row without an attended token gives out = 0, lse = -inf.
  * A NaN in the cache reaches the rows that attend its token.

@@ -35,7 +35,7 @@ inline TreePlan q4_plan(long long pairs, int G, int T, int units) {
   const bool small = tiles > 4 && pairs * units * twos <= kQ4SmallUnits;
   p.groups = small ? twos : (tiles + kQ4Tiles - 1) / kQ4Tiles;
   p.tiles = small ? kQ4RegisterTiles : (tiles + p.groups - 1) / p.groups;
-  p.units = units;
+  p.units = 2 * units;  // of 32 tokens (tree_lift)
   const long long items = pairs * p.groups;
   const long long slots = p.tiles > 4 ? 256 : 512;
   long long most = (units + kQ4Waves - 1) / kQ4Waves;

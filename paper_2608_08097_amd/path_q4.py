@@ -71,10 +71,8 @@ class Q4Path:
         self._summaries(st, ctx_len, new_ctx_len, n, stream)
 
     def _summaries(self, st: Q4Layer, ctx_len, new_ctx_len, n: int, stream):
-        # n tokens complete at most so many blocks; the first one may have been the local block, full already
-        most = -(-n // self.dims.block_size) + 1
-        L.oasis_update_summaries_q4(self.dims, st.k_pages, self.block_table, ctx_len, new_ctx_len, most, st.kmax, st.kmin,
-                                    stream)
+        L.oasis_update_summaries_q4(self.dims, st.k_pages, self.block_table, ctx_len, new_ctx_len,
+                                    -(-n // self.dims.block_size), st.kmax, st.kmin, stream)
 
     def rotate(self, q: torch.Tensor, k: torch.Tensor, ctx_len: torch.Tensor, positions: torch.Tensor | None = None,
                stream=None) -> tuple[torch.Tensor, torch.Tensor]:

@@ -107,6 +107,20 @@ def test_tree_rows_off_the_path_have_no_influence(form):
     assert torch.equal(b[..., keep], o0[hit][:, G:][..., keep])
 
 
+# Tables and selections of more than 96 MiB, whose codes are read past the caches: one and two row tiles, few tokens
+STREAM = [(4, 3, 16, 24000, 0), (4, 3, 32, 12000, 0), (4, 6, 16, 24000, 0), (4, 6, 32, 12000, 0), (4, 3, 16, 24000, 23500),
+          (4, 3, 32, 12000, 11800), (4, 6, 16, 24000, 23500), (4, 6, 32, 12000, 11800)]
+
+
+@pytest.mark.parametrize("form", STREAM)
+def test_loads_past_the_caches(form):
+    G, T, B, spare, k = form
+    assert H * min(spare, k or spare) * B * 136 >= 96 << 20
+    _, q, tk, tv, parent, _ = _inputs(920, 1, G * H, H, T, "random", None)
+    _Call(form, q, *_pages(10, B), tk, tv, parent).check()
+    _Call(form, q, *_pages(11, B)).check()
+
+
 @pytest.mark.parametrize("form", FORMS)
 @pytest.mark.parametrize("signs", ["same", "mixed"])
 def test_the_largest_values(form, signs):
