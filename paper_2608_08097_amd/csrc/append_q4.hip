@@ -10,6 +10,11 @@
 // Turned keys are held in 64 bits up to their code: with 32, one value in some 10^7 lies
 // close enough to a border between two codes to fall on the other side. On the way to the
 // conversion, which takes 32 bits, they are rounded to odd, which keeps them on their side.
+//
+// Four chunks of 8,192 tokens (306 MB with the rows read back): 77 us, 65 without the
+// rotation, 60 at the rate of a copy. Heads of keys and values alternate between the waves:
+// with all keys in two of the four, on two of the SIMDs, 87; with the pages looked up row by
+// row 100. A batch's accepted rows take the time of a launch (4.3 us).
 #include "rotary.h"
 
 namespace oasis {
@@ -181,7 +186,7 @@ __global__ __launch_bounds__(kQAThreads) void q4_append_kernel(AppendQ4Args a) {
       y[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1));
       y[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2));
       y[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3));
-      // whole lines, which nothing reads soon where they are many
+      // past the caches: whole lines (92 -> 87 us)
       __builtin_nontemporal_store(y, reinterpret_cast<u32x4*>(read + (((long long)r * a.T + i) * a.Hkv + h) * kHeadDim + d0));
     }
   }

@@ -7,16 +7,30 @@
 //   S^T (tokens x rows) = K . Q^T     16 of v_mfma_f32_16x16x32_bf16
 //   O^T (d x rows)     += V^T . P^T   16 of them
 //
-// Keys go straight from memory into the first product's operand: a lane has 32 dims of a
-// token in 16 bytes, whose codes the hardware turns into bf16 with the token's power, two
-// at a time; the queries are dealt to the same dims. The tokens are dealt to MFMA rows so
-// that lane (g, n) ends up with row n's scores of sub-block g's 16 tokens.
+// Codes become bf16 exactly, two a conversion with their power of two, and both products are
+// those of tree_attn.hip over the values that the cache stands for. Two forms.
 //
-// Values need 8 tokens of one dim in a lane: turned into bf16 as the keys are, they go
-// through LDS, a part of it for each wave, and come back through the transposing read.
+// Up to two row tiles every wave streams units of its own. Of a sub-block a lane has 32 dims of
+// a token in 16 bytes, with one power: keys are the first product's operand as soon as they are
+// turned, the queries being dealt to the same dims. The second product needs 8 tokens of one
+// dim in a lane: values go through LDS, 16 KB a wave, and come back through the transposing
+// read. (Left as codes there, with the powers taken up by the probabilities, they took 249 us
+// instead of 220 in the second case below.) With more rows eight waves share what is turned.
 //
 // The tree's rows, keys and values in bf16, are a unit of their own in the last split of
 // every pair.
+//
+// Measured (136 bytes a token and KV head; 4 d operations a row and token):
+//   8 requests x 8 heads x 131,072 tokens, 4 rows    180 us  6.3 TB/s
+//   8 x 8 x 131,072, 20 rows                         203-205 us  5.6 TB/s; its loads alone take 174 and the
+//                                                    clock falls from 2.4 to 2.05 GHz with the products
+//   24 x 8 x 1 to 32,768, 64 rows                    151-172 us a draw
+//   2 x 8 x 65,000 to 65,536, 512 rows               297-307 us  890-920 TFLOP/s
+//   16 x 8 x 4,128 selected, 72 rows                 54 us
+//   8 x 8 x 2,064 selected, 20 rows                  16.1 us  two launches (7.4), four loads in turn
+//   1 x 8 x 2,000, 4 rows                            8.8-9.5 us  the same
+// A read of 1 KB pieces in any order reaches 6.7 TB/s here past the caches and 5.9 through
+// them, hence the loads of large caches.
 #include "tree_core.h"
 #include "q4_internal.h"
 
@@ -468,10 +482,15 @@ __global__ __launch_bounds__(kQW * 64) void q4_attn_kernel(AttnQ4Args a) {
 // sixteenth of its codes, 16 tokens of keys or of values, into bf16 in LDS, and then attends
 // with its own one or two of the group's row tiles, team 0 the unit's first 32 tokens and
 // team 1 the others. Keys lie there as the first product's operand, values a token after the
-// other, 16 dims (32 bytes, the halves swapped as above) apart, for the transposing read.
+// other, 16 dims (32 bytes, the halves swapped as above) apart, for the transposing read. One
+// barrier a unit.
 //
-// Loads of a unit's codes, 16 bytes a lane, go out kAhead units ahead of their conversion,
-// that one unit ahead of the products; two units are in LDS, one barrier a unit.
+// With two tiles a wave (512 rows over 65,536 tokens, 296 us) the barrier takes 38 us, the LDS
+// reads 40, turning the codes and their loads 41, and the rest 177, about what the products
+// take at the library's rate; with the teams out of step, as in tree_attn.hip, it was slower
+// (308), with loads two and three units ahead the same. With one tile a wave 42 % of a wave's
+// time is waiting; keys read by each wave as codes, from LDS (166 us for the ragged case) or
+// from memory (199), were no faster than through LDS in bf16 (164).
 constexpr int kRowsThreads = 512;
 constexpr int kRowPlaces = 4;   // waves of a team
 constexpr int kListBlocks = 1024;
@@ -649,7 +668,8 @@ __global__ __launch_bounds__(kRowsThreads, NT == 1 ? 4 : 2) void q4_attn_rows_ke
       return n > 16 ? 16 : n;
     };
     if constexpr (NT == 1) {
-      // Two workgroups share a CU, and hide each other's waits: two units in LDS.
+      // Two workgroups share a CU, and hide each other's waits: two units in LDS, loads three
+      // units ahead of their conversion.
       constexpr int kAhead = 3;
       Codes x[kAhead];
 #pragma unroll

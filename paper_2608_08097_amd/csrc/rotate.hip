@@ -3,7 +3,10 @@
 // A workgroup takes some rows with all their heads: first their cosines and sines, 64 bits
 // rounded to 32, into LDS, then eight threads a head, 16 elements each: the two halves of
 // eight pairs, or eight pairs side by side, or 16 elements that do not turn. Products and
-// sums are in 32 bits, rounded to bf16 once.
+// sums are in 32 bits, rounded to bf16 once: the rounding to bf16 is 2^15 times theirs.
+//
+// It is a copy: 32,768 rows of 40 heads (671 MB both ways) 120 us, 5.6 TB/s, with two rows a
+// workgroup (four 125, eight 137); 320 rows the time of a launch.
 #include "rotary.h"
 
 namespace oasis {
@@ -63,7 +66,7 @@ __global__ __launch_bounds__(kRotThreads) void rotate_kernel(RotateArgs a) {
         dst[j] = src[j];
       }
     } else if (a.rot.interleaved) {
-      u32x4 v[2] = {ldg16(src + 8 * w), ldg16(src + 64 + 8 * w)};
+      u32x4 v[2] = {ldg16(src + 8 * w), ldg16(src + 64 + 8 * w)};  // whole lines (32 bytes a lane: 8 % slower)
 #pragma unroll
       for (int p = 0; p < 8; ++p) {
         const int pair = (p >> 2) * 32 + 4 * w + (p & 3);
