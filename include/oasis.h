@@ -525,7 +525,7 @@ OASIS_API oasis_status oasis_rotary_turns(int32_t rotary_dim, double base, int32
  * same address and stride); outputs and inputs of one stride may lie side by side.
  * inverse != 0 turns back, by the negative angle and with the same amplitude: the
  * gradient of the rows from that of the turned ones. Sines and cosines are rounded to
- * 32 bits, products and sums in 32 bits, to bf16 once.
+ * 32 bits, products and sums in 32 bits, to bf16 once. At most 2^24 rows a call.
  */
 OASIS_API oasis_status oasis_rotate(const oasis_dims* dims, const oasis_rotary* rotary, int32_t num_tokens,
                                     const int32_t* positions, const int32_t* ctx_len, int32_t inverse,

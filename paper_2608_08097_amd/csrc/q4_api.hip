@@ -147,7 +147,8 @@ oasis_status oasis_rotate(const oasis_dims* dims, const oasis_rotary* rotary, in
   oasis::RotateArgs a{};
   if ((st = oasis::make_rotary(rotary, inverse != 0, &a.rot, fn)) != OASIS_OK) return st;
   const long long rows = (long long)dims->num_reqs * num_tokens;
-  if (rows > INT32_MAX || (long long)dims->num_q_heads + dims->num_kv_heads > 65536)
+  // (a launch has fewer than 2^32 threads: 256 for every two rows)
+  if (rows > 1 << 24 || (long long)dims->num_q_heads + dims->num_kv_heads > 65536)
     return fail(OASIS_ERR_UNSUPPORTED, "%s: %lld rows of %d and %d heads", fn, rows, dims->num_q_heads,
                 dims->num_kv_heads);
   if (dims->num_reqs == 0) return ok();

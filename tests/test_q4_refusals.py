@@ -124,6 +124,12 @@ def test_rotations():
     assert rotate(rot=False)[0] == INVALID
 
 
+def test_rotate_more_rows_than_a_launch_has_threads_for():
+    for d, tokens in ((_d(), (1 << 24) // R + 1), (_d(num_reqs=1), (1 << 24) + 1), (_d(num_reqs=1), 1 << 25)):
+        st, error = rotate(d, tokens=tokens)
+        assert st == UNSUPPORTED and "rows" in error, tokens
+
+
 def test_strides():
     for bad in (HQ * 128 - 8, HQ * 128 + 4, 0, -HQ * 128, 1 << 62):
         for n in ("qs", "qos"):
