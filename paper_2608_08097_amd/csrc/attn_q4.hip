@@ -488,7 +488,8 @@ __global__ __launch_bounds__(kQW * 64) void q4_attn_kernel(AttnQ4Args a) {
 // With two tiles a wave (512 rows over 65,536 tokens, 296 us) the barrier takes 38 us, the LDS
 // reads 40, turning the codes and their loads 41, and the rest 177, about what the products
 // take at the library's rate; with the teams out of step, as in tree_attn.hip, it was slower
-// (308), with loads two and three units ahead the same. With one tile a wave 42 % of a wave's
+// (308), with a barrier for every two units in four buffers too (303), with loads two and
+// three units ahead the same. With one tile a wave 42 % of a wave's
 // time is waiting; keys read by each wave as codes, from LDS (166 us for the ragged case) or
 // from memory (199), were no faster than through LDS in bf16 (164).
 constexpr int kRowsThreads = 512;
