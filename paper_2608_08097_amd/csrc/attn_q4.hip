@@ -26,7 +26,7 @@
 //                                                    clock falls from 2.4 to 2.05 GHz with the products
 //   24 x 8 x 1 to 32,768, 64 rows                    151-172 us a draw
 //   2 x 8 x 65,000 to 65,536, 512 rows               297-307 us  890-920 TFLOP/s
-//   16 x 8 x 4,128 selected, 72 rows                 54 us
+//   16 x 8 x 4,128 selected, 72 rows                 52 us
 //   8 x 8 x 2,064 selected, 20 rows                  16.1 us  two launches (7.4), four loads in turn
 //   1 x 8 x 2,000, 4 rows                            8.8-9.5 us  the same
 // A read of 1 KB pieces in any order reaches 6.7 TB/s here past the caches and 5.9 through
@@ -131,8 +131,8 @@ __device__ __forceinline__ void load_q4_queries(const TreeAttnArgs& a, const Q4I
   }
 }
 
-// The online softmax of tree_attn.hip over a lane's 4 U scores of each tile, with one branch
-// for all tiles: probabilities not yet rounded.
+// The online softmax of tree_attn.hip over a lane's 4 U scores of the first `used` tiles, with
+// one branch for all: probabilities not yet rounded.
 template <int U>
 __device__ __forceinline__ float exp_of(const f32x4 (&s)[U], float scale, float m_neg, float (&p)[4 * U]) {
   float sum[U];
@@ -147,17 +147,19 @@ __device__ __forceinline__ float exp_of(const f32x4 (&s)[U], float scale, float 
 }
 template <int NT, int U>
 __device__ __forceinline__ void softmax_of(const f32x4 (&s)[NT][U], float scale, float top, float (&m_neg)[NT],
-                                           float (&l_part)[NT], f32x4 (&acc)[NT][8], float (&p)[NT][4 * U]) {
+                                           float (&l_part)[NT], f32x4 (&acc)[NT][8], float (&p)[NT][4 * U], int used = NT) {
   float psum[NT];
   bool over = false;
 #pragma unroll
   for (int v = 0; v < NT; ++v) {
+    if (v >= used) continue;
     psum[v] = exp_of(s[v], scale, m_neg[v], p[v]);
     over |= !(psum[v] <= top);
   }
   if (__builtin_expect(__builtin_amdgcn_ballot_w64(over) != 0, 0)) {
 #pragma unroll
     for (int v = 0; v < NT; ++v) {
+      if (v >= used) continue;
       const uint64_t past = __builtin_amdgcn_ballot_w64(!(psum[v] <= top));
       const uint64_t rows = past | past >> 16 | past >> 32 | past >> 48;
       const bool mine = rows >> (threadIdx.x & 15) & 1;
@@ -177,7 +179,8 @@ __device__ __forceinline__ void softmax_of(const f32x4 (&s)[NT][U], float scale,
     }
   }
 #pragma unroll
-  for (int v = 0; v < NT; ++v) l_part[v] += psum[v];
+  for (int v = 0; v < NT; ++v)
+    if (v < used) l_part[v] += psum[v];
 }
 
 template <int NT, int BS, bool SELECT, bool STREAM>
@@ -494,12 +497,17 @@ __global__ __launch_bounds__(kQW * 64) void q4_attn_kernel(AttnQ4Args a) {
 // from memory (199), were no faster than through LDS in bf16 (164).
 constexpr int kRowsThreads = 512;
 constexpr int kRowPlaces = 4;   // waves of a team
+// Groups of five or six tiles leave out the products and exponentials of the places without a
+// second one, tile by tile (FULL false). Measured, us with and without, 512 pairs over 2,064
+// selected tokens: five tiles 95 and 102, six 100 and 105, seven 110 and 108; 16 pairs over
+// 65,536: 85 and 87, 87 and 89, 96 and 90.
+constexpr int kUnevenTiles = 6;
 constexpr int kListBlocks = 1024;
 constexpr int kKeysBytes = 16 * 1024;
 constexpr int kValuesPart = 4 * 1024;  // 32 dims of the unit's tokens
 constexpr int kUnitBytes = kKeysBytes + 4 * kValuesPart;
 
-template <int NT, int BS, bool SELECT>
+template <int NT, int BS, bool SELECT, bool FULL>
 __global__ __launch_bounds__(kRowsThreads, NT == 1 ? 4 : 2) void q4_attn_rows_kernel(AttnQ4Args a) {
   constexpr int kRows = NT * kRowPlaces * 16;
   constexpr int kPad = kHeadDim + 4;
@@ -516,7 +524,10 @@ __global__ __launch_bounds__(kRowsThreads, NT == 1 ? 4 : 2) void q4_attn_rows_ke
   const int g = lane >> 4;
   const int i = lane & 15;
   const int team = wave / kRowPlaces;
-  const int rt = wave % kRowPlaces;  // this wave's tiles: rt and rt + 4 of the group's
+  // this wave's tiles: rt and rt + 4 of the group's; not FULL: the second one may be none of
+  // the group's (the waves with two tiles of the teams are on different SIMDs)
+  const int rt = (wave + (FULL ? 0 : 2 * team)) % kRowPlaces;
+  const int used = FULL ? NT : (rt + kRowPlaces < a.tiles ? 2 : 1);
   Q4Item t;
   if (!q4_setup<SELECT>(a, a.tiles * 16, t)) return;
   const Ctx c = ctx_blocks(t.ctx, BS, a.NBmax);
@@ -586,21 +597,35 @@ __global__ __launch_bounds__(kRowsThreads, NT == 1 ? 4 : 2) void q4_attn_rows_ke
   };
   f32x4 sc[NT][2];
   auto scores = [&]() __attribute__((always_inline)) {
+    if constexpr (FULL) {
 #pragma unroll
-    for (int v = 0; v < NT; ++v) sc[v][0] = sc[v][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int v = 0; v < NT; ++v) sc[v][0] = sc[v][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int st = 0; st < 4; ++st)
+      for (int st = 0; st < 4; ++st)
 #pragma unroll
-      for (int v = 0; v < NT; ++v)
+        for (int v = 0; v < NT; ++v)
 #pragma unroll
-        for (int tau = 0; tau < 2; ++tau)
-          sc[v][tau] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(kf[tau][st]), qb[v][st], sc[v][tau], 0, 0, 0);
+          for (int tau = 0; tau < 2; ++tau)
+            sc[v][tau] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(kf[tau][st]), qb[v][st], sc[v][tau], 0, 0, 0);
+    } else {
+#pragma unroll
+      for (int v = 0; v < NT; ++v) {
+        if (v >= used) continue;
+        sc[v][0] = sc[v][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int st = 0; st < 4; ++st)
+#pragma unroll
+          for (int tau = 0; tau < 2; ++tau)
+            sc[v][tau] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(kf[tau][st]), qb[v][st], sc[v][tau], 0, 0, 0);
+      }
+    }
   };
   // `keep` attended tokens of the team's two sub-blocks (16: all), or the tree's rows
   auto mask = [&](int keep0, int keep1, bool tree) __attribute__((always_inline)) {
     if (keep0 >= 16 && keep1 >= 16 && !tree) return;
 #pragma unroll
     for (int v = 0; v < NT; ++v) {
+      if (v >= used) continue;
       const int k0 = keep0 - 4 * g, k1 = keep1 - 4 * g;
       uint32_t bits = (k0 <= 0 ? 0u : k0 >= 4 ? 15u : (1u << k0) - 1) | (k1 <= 0 ? 0u : k1 >= 4 ? 15u : (1u << k1) - 1) << 4;
       if (tree) {
@@ -615,11 +640,13 @@ __global__ __launch_bounds__(kRowsThreads, NT == 1 ? 4 : 2) void q4_attn_rows_ke
   bf16x8 pb[NT];
   auto softmax = [&]() __attribute__((always_inline)) {
     float p[NT][8];
-    softmax_of(sc, a.scale_log2, a.top, m_neg, l_run, acc, p);
+    softmax_of(sc, a.scale_log2, a.top, m_neg, l_run, acc, p, used);
 #pragma unroll
-    for (int v = 0; v < NT; ++v)
+    for (int v = 0; v < NT; ++v) {
+      if (v >= used) continue;
 #pragma unroll
       for (int e = 0; e < 8; ++e) pb[v][e] = (__bf16)p[v][e];
+    }
   };
   auto values = [&](int dt) __attribute__((always_inline)) {
 #pragma unroll
@@ -628,8 +655,18 @@ __global__ __launch_bounds__(kRowsThreads, NT == 1 ? 4 : 2) void q4_attn_rows_ke
   };
   auto attend = [&]() __attribute__((always_inline)) {
     softmax();
+    if constexpr (FULL) {
 #pragma unroll
-    for (int dt = 0; dt < 8; ++dt) values(dt);
+      for (int dt = 0; dt < 8; ++dt) values(dt);
+    } else {
+#pragma unroll
+      for (int v = 0; v < NT; ++v) {
+        if (v >= used) continue;
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt)
+          acc[v][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(vf[dt]), pb[v], acc[v][dt], 0, 0, 0);
+      }
+    }
     __builtin_amdgcn_sched_barrier(0);
   };
 
@@ -820,9 +857,11 @@ void launch_bs_q4(const AttnQ4Args& a, hipStream_t s) {
     hipLaunchKernelGGL((stream ? q4_attn_kernel<2, BS, SELECT, true> : q4_attn_kernel<2, BS, SELECT, false>), grid,
                        dim3(kQW * 64), 0, s, a);
   else if (a.tiles <= kRowPlaces)
-    hipLaunchKernelGGL((q4_attn_rows_kernel<1, BS, SELECT>), grid, dim3(kRowsThreads), 0, s, a);
+    hipLaunchKernelGGL((q4_attn_rows_kernel<1, BS, SELECT, true>), grid, dim3(kRowsThreads), 0, s, a);
+  else if (a.tiles <= kUnevenTiles)
+    hipLaunchKernelGGL((q4_attn_rows_kernel<2, BS, SELECT, false>), grid, dim3(kRowsThreads), 0, s, a);
   else
-    hipLaunchKernelGGL((q4_attn_rows_kernel<2, BS, SELECT>), grid, dim3(kRowsThreads), 0, s, a);
+    hipLaunchKernelGGL((q4_attn_rows_kernel<2, BS, SELECT, true>), grid, dim3(kRowsThreads), 0, s, a);
 }
 
 }  // namespace

@@ -381,6 +381,16 @@ def test_rows_of_several_tiles_lengths(B, ctx):
     _attn_case(3580 + B + len(ctx), len(ctx), 16, 2, 10, B, ctx, "none")
 
 
+@pytest.mark.parametrize("G,T", [(5, 13), (5, 16), (6, 15), (3, 32), (7, 15), (8, 14), (11, 11), (8, 16)])
+def test_five_to_eight_tiles_over_long_tables(G, T):
+    """One group of so many row tiles (a table of many units), with a last tile that is full or not, and trees that leave
+    whole tiles unused."""
+    for k in (None, 3000):
+        _attn_case(3700 + G * T, 3, G * 2, 2, T, 16, [300, 20, 0], "random", [T, T // 2, T - 1], spare=7000, k=k)
+        _attn_case(3800 + G * T, 2, G * 2, 2, T, 32, [77, 1100], "beam", [3, T], spare=4000, k=k)
+        _attn_case(3900 + G * T, 2, G * 2, 2, T, 16, [65, 1000], "none", spare=7000, k=k)
+
+
 @pytest.mark.parametrize("G,T", [(4, 3), (20, 2), (20, 4)])
 def test_long_contexts_in_one_split(G, T):
     """So many pairs that they are hardly split, or not at all, two of them with thousands of blocks: lists of blocks in

@@ -16,9 +16,10 @@ pytestmark = pytest.mark.gpu
 
 H, L = 2, 300
 # G, T, B, blocks of the table past the context, selected blocks: one and two row tiles a wave for itself, one and two of
-# the form that shares a unit, each in one split and in several, and over a selection
+# the form that shares a unit (not every place with two, and every one), each in one split and in several, and over a selection
 FORMS = [(4, 3, 16, 0, 0), (4, 3, 32, 3000, 0), (4, 6, 16, 3000, 0), (4, 6, 32, 0, 0), (4, 13, 16, 0, 0), (4, 13, 32, 3000, 0),
-         (8, 12, 16, 6000, 0), (8, 12, 32, 6000, 0), (4, 3, 16, 0, 30), (4, 6, 32, 0, 30), (4, 13, 16, 0, 30), (8, 12, 32, 6000, 2000)]
+         (8, 12, 16, 6000, 0), (8, 12, 32, 6000, 0), (4, 3, 16, 0, 30), (4, 6, 32, 0, 30), (4, 13, 16, 0, 30), (8, 12, 32, 6000, 2000),
+         (8, 16, 16, 6000, 0), (8, 16, 32, 6000, 2000)]
 
 
 class _Call:

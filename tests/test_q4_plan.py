@@ -75,4 +75,4 @@ def test_the_kernels_keep_their_values_in_registers(kernels):  # noqa: F811
             two = n.startswith("q4_attn_rows_kernel<1")
             assert waves >= (4 if two else 2) and (2 if two else 1) * lds <= LDS, (n, k[".vgpr_count"], lds)
     assert {n: len(v) for n, v in seen.items()} == {
-        "q4_attn_kernel": 16, "q4_attn_rows_kernel": 8, "q4_append_kernel": 2, "q4_summaries_kernel": 2, "rotate_kernel": 2}, seen
+        "q4_attn_kernel": 16, "q4_attn_rows_kernel": 12, "q4_append_kernel": 2, "q4_summaries_kernel": 2, "rotate_kernel": 2}, seen
