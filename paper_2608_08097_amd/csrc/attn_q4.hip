@@ -494,7 +494,9 @@ __global__ __launch_bounds__(kQW * 64) void q4_attn_kernel(AttnQ4Args a) {
 // (308), with a barrier for every two units in four buffers too (303), with loads two and
 // three units ahead the same. With one tile a wave 42 % of a wave's
 // time is waiting; keys read by each wave as codes, from LDS (166 us for the ragged case) or
-// from memory (199), were no faster than through LDS in bf16 (164).
+// from memory (199), were no faster than through LDS in bf16 (164), nor were two tiles a wave
+// in four teams over 128 tokens a step, with 0.6 of the LDS traffic and one workgroup a CU
+// (407 and 382 us for 8 x 8 x 131,072 tokens with 64 rows, 43 and 41 for 16 x 8 x 4,128).
 constexpr int kRowsThreads = 512;
 constexpr int kRowPlaces = 4;   // waves of a team
 // Groups of five or six tiles leave out the products and exponentials of the places without a
