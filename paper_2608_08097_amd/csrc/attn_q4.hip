@@ -874,7 +874,7 @@ hipError_t launch_attn_q4(const AttnQ4Args& a, hipStream_t s) {
   else
     a.sel ? launch_bs_q4<32, true>(a, s) : launch_bs_q4<32, false>(a, s);
   const hipError_t e = hipGetLastError();
-  return e != hipSuccess ? e : launch_tree_finish(a, s);
+  return e != hipSuccess ? e : launch_tree_finish(a, CacheSelection{a.sel, a.sel_count, a.k_sel}, s);
 }
 
 }  // namespace oasis

@@ -31,8 +31,15 @@ struct TreeAttnArgs {
   FastDiv by_groups, by_nsplit, by_hkv, by_g;
 };
 hipError_t launch_tree_attn(const TreeAttnArgs& a, bool paged, hipStream_t s);
-// What follows an attention kernel: the merge of its splits, and the rows of wild queries under a scale of 0.
-hipError_t launch_tree_finish(const TreeAttnArgs& a, hipStream_t s);
+// The blocks of the paged cache that each KV head attends beside the local one.
+struct CacheSelection {
+  const int32_t* ids = nullptr;    // [R][Hkv][k]; NULL: every block
+  const int32_t* count = nullptr;  // [R][Hkv]
+  int k = 0;
+};
+// What follows an attention kernel: the merge of its splits, and the rows of wild queries under a scale of 0 (without a
+// tree by the pages that the selection and table name).
+hipError_t launch_tree_finish(const TreeAttnArgs& a, const CacheSelection& sel, hipStream_t s);
 
 constexpr int kVerifyBlocks = 256;  // blocks of a row at most
 struct VerifyCut {

@@ -819,17 +819,50 @@ __global__ __launch_bounds__(kTreeMergeRows * 32) void tree_merge_kernel(TreeAtt
 // times which is a NaN score of every token: the rows of such queries, after the others.
 // (Looked at where the queries are read, or where rows are written, every call of wide
 // trees paid 1 to 3 % for it.)
-__global__ __launch_bounds__(kTreeMergeRows * 32) void wild_queries_kernel(TreeAttnArgs a) {
+//
+// A row that attends nothing keeps its 0 and -infinity. With a tree it attends itself;
+// without one (the 4-bit cache) it attends a token where a block of the context, or of the
+// selection and the local one, has a page of the tier: its 32 lanes look at as many blocks
+// at a time.
+__device__ __forceinline__ uint32_t of_row(bool x) {
+  return (uint32_t)(__builtin_amdgcn_ballot_w64(x) >> (threadIdx.x & 32));
+}
+__device__ bool cache_attended(const TreeAttnArgs& a, const CacheSelection& sel, int r, int h) {
+  const Ctx c = ctx_blocks(a.ctx_len[r], a.B, a.NBmax);
+  if (c.nb == 0) return false;
+  int selected = c.n_cand;
+  const int32_t* ids = nullptr;
+  if (sel.ids) {
+    const long long rh = (long long)r * a.Hkv + h;
+    selected = min(max(sel.count[rh], 0), sel.k);
+    ids = sel.ids + rh * sel.k;
+  }
+  const int32_t* table = a.table + (long long)r * a.NBmax;
+  for (int b0 = 0; b0 <= selected; b0 += 32) {  // the local block last
+    const int b = b0 + (threadIdx.x & 31);
+    int id = c.n_cand;
+    bool in = b <= selected;
+    if (ids && b < selected) {
+      id = ids[b];
+      in = id >= 0 && id < c.n_cand;
+    } else if (b < selected) {
+      id = b;
+    }
+    const int page = in ? table[id] : -1;
+    if (of_row(page >= 0 && page < a.num_pages)) return true;
+  }
+  return false;
+}
+
+__global__ __launch_bounds__(kTreeMergeRows * 32) void wild_queries_kernel(TreeAttnArgs a, CacheSelection sel) {
   const int row = blockIdx.x * kTreeMergeRows + (threadIdx.x >> 5);  // of R x T x Hq
   const int rt = row / a.Hq, r = rt / a.T;
   if (r >= a.R || rt - r * a.T >= tree_length(a, r)) return;
-  if (!a.tree_k && a.ctx_len[r] <= 0) return;  // nothing attended
   const int c4 = threadIdx.x & 31;
   const long long at = (long long)row * kHeadDim + c4 * 4;
   const uint2 w = *reinterpret_cast<const uint2*>(a.q + at);
-  const uint64_t wild =
-      __builtin_amdgcn_ballot_w64(wild_bf16(w.x) || wild_bf16(w.x >> 16) || wild_bf16(w.y) || wild_bf16(w.y >> 16));
-  if (!(wild >> (threadIdx.x & 32) & 0xFFFFFFFFu)) return;
+  if (!of_row(wild_bf16(w.x) || wild_bf16(w.x >> 16) || wild_bf16(w.y) || wild_bf16(w.y >> 16))) return;
+  if (!a.tree_k && !cache_attended(a, sel, r, a.by_g(row - rt * a.Hq))) return;
   *reinterpret_cast<uint2*>(a.out + at) = make_uint2(0x7FC07FC0u, 0x7FC07FC0u);
   if (c4 == 0 && a.lse) a.lse[row] = __builtin_nanf("");
 }
@@ -860,7 +893,7 @@ void launch_bs(const TreeAttnArgs& a, hipStream_t s) {
 
 }  // namespace
 
-hipError_t launch_tree_finish(const TreeAttnArgs& a, hipStream_t s) {
+hipError_t launch_tree_finish(const TreeAttnArgs& a, const CacheSelection& sel, hipStream_t s) {
   hipError_t e = hipSuccess;
   if (a.nsplit > 1) {
     TreeAttnArgs m = a;
@@ -873,7 +906,7 @@ hipError_t launch_tree_finish(const TreeAttnArgs& a, hipStream_t s) {
   if (a.q_and != 0) return e;
   const long long rows = (long long)a.R * a.T * a.Hq;  // below 2^28
   hipLaunchKernelGGL(wild_queries_kernel, dim3((unsigned)((rows + kTreeMergeRows - 1) / kTreeMergeRows)),
-                     dim3(kTreeMergeRows * 32), 0, s, a);
+                     dim3(kTreeMergeRows * 32), 0, s, a, sel);
   return hipGetLastError();
 }
 
@@ -883,7 +916,7 @@ hipError_t launch_tree_attn(const TreeAttnArgs& a, bool paged, hipStream_t s) {
   else
     paged ? launch_bs<32, true>(a, s) : launch_bs<32, false>(a, s);
   const hipError_t e = hipGetLastError();
-  return e != hipSuccess ? e : launch_tree_finish(a, s);
+  return e != hipSuccess ? e : launch_tree_finish(a, CacheSelection{}, s);
 }
 
 }  // namespace oasis

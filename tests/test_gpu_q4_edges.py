@@ -1,0 +1,101 @@
+"""Attention over the 4-bit cache in the corners of its contract: wild queries where nothing is attended, in every
+form of the kernel."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2608_08097_amd as P
+from oracle import q4 as Q
+from tests.gpu_util import dev_bf16, dev_i32, note
+from tests.test_gpu_drafts import INF, NAN
+from tests.test_gpu_q4 import dev_u8
+from workloads import random_bf16
+
+pytestmark = pytest.mark.gpu
+
+H = 2
+# G, T, B, blocks of the table past the context: one and two row tiles a wave for itself, one and two of the form that
+# shares a unit, each in one split and in several
+FORMS = [(4, 3, 16, 0), (4, 3, 32, 3000), (4, 6, 16, 3000), (4, 6, 32, 0), (4, 13, 16, 0), (4, 13, 32, 3000), (8, 12, 16, 6000),
+         (8, 16, 32, 6000)]
+
+
+def _call(form, q, kp, vp, table, ctx, sel=None, cnt=None, scale=None, lse=True):
+    G, T, B, _ = form
+    R, NB, k = len(table), table.shape[1], 0 if sel is None else sel.shape[2]
+    d = P.dims(R, G * H, H, 128, B, NB)
+    note(f"4-bit corners G={G} T={T} B={B} NB={NB} k={k} ctx={list(ctx)[:4]}")
+    ws = torch.full((P.oasis_tree_attn_q4_workspace_bytes(d, T, k),), 255, dtype=torch.uint8, device="cuda")
+    out = torch.full(q.shape, 7.0, dtype=torch.bfloat16, device="cuda")
+    lse = torch.full(q.shape[:3], 7.0, device="cuda") if lse else None
+    P.oasis_tree_attn_q4(d, dev_bf16(q), T, dev_u8(kp), dev_u8(vp), dev_i32(table), dev_i32(ctx),
+                         None if sel is None else dev_i32(sel), None if cnt is None else dev_i32(cnt), k, None, None, None, None,
+                         scale, out, lse, ws)
+    torch.cuda.synchronize()
+    return out, lse
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("selected", [False, True])
+def test_wild_queries_that_attend_nothing_under_a_scale_of_0(form, selected):
+    """Request 0 has pages, request 1 none for its whole context, request 2 only one that the selection of its head 1
+    names (every block: the one of its last token). A row without an attended token is 0 and -infinity whatever its query
+    holds; one with a token is NaN."""
+    G, T, B, spare = form
+    L, n = 5 * B - 3, 4
+    rng = np.random.default_rng(T)
+    kp, vp = (Q.make_pages(rng.normal(size=(6, H, B, 128))) for _ in range(2))
+    table = np.full((3, 5 + spare), -1, np.int32)
+    table[0, :5] = [3, 1, 0, 2, 4]
+    table[1, :5] = [6, -7, 2 ** 31 - 1, -2 ** 31, -1]
+    table[2, 2 if selected else 4] = 5
+    sel = cnt = None
+    if selected:
+        sel = np.full((3, H, 3), -1, np.int32)
+        sel[:, 0], sel[:, 1] = [1, 3, -1], [n, 0, 2]  # (n is the local block's id: no candidate)
+        cnt = np.array([[2, 3], [2, 3], [3, 99]], np.int32)
+    q = random_bf16(40 + T, (3, T, G * H, 128))
+    q[:, 0, :, 3], q[:, T - 1, :, 120] = NAN, INF
+    some = np.zeros((3, H), bool)
+    some[0] = True
+    some[2] = [False, True] if selected else True
+    for lse in (True, False):
+        out, got_lse = _call(form, q, kp, vp, table, [L] * 3, sel, cnt, 0.0, lse)
+        out = out.cpu().view(3, T, H, G, 128)
+        for r in range(3):
+            for h in range(H):
+                at = out[r, :, h]
+                if not some[r, h]:
+                    assert not at.view(torch.int16).any(), (r, h)
+                else:
+                    assert torch.isnan(at[[0, T - 1]]).all() and torch.isfinite(at[1:T - 1]).all(), (r, h)
+                if lse:
+                    x = got_lse.cpu().view(3, T, H, G)[r, :, h]
+                    if not some[r, h]:
+                        assert torch.all(x == -torch.inf), (r, h)
+                    else:
+                        assert torch.isnan(x[[0, T - 1]]).all() and torch.isfinite(x[1:T - 1]).all(), (r, h)
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("last", [31, 32, 33, 63, 64, 70])
+def test_wild_queries_whose_only_page_is_far_along(form, last):
+    """Block `last` of the context, or entry `last` of the selection, is the only one with a page; with none at all the rows
+    are 0."""
+    G, T, B, spare = form
+    L, NB = 80 * B, 80
+    rng = np.random.default_rng(last)
+    kp, vp = (Q.make_pages(rng.normal(size=(2, H, B, 128))) for _ in range(2))
+    q = random_bf16(60 + T, (1, T, G * H, 128))
+    q[:, :, :, 9] = NAN
+    sel = np.broadcast_to(rng.permutation(NB - 1)[:75], (1, H, 75)).astype(np.int32).copy()
+    for some in (True, False):
+        for ids in (None, sel):
+            table = np.full((1, NB + spare), -1, np.int32)
+            if some:
+                table[0, last if ids is None else sel[0, 0, last]] = 1
+            out, lse = _call(form, q, kp, vp, table, [L], ids, None if ids is None else np.full((1, H), 75, np.int32), 0.0)
+            if some:
+                assert torch.isnan(out).all() and torch.isnan(lse).all()
+            else:
+                assert not out.view(torch.int16).any() and torch.all(lse == -torch.inf)
