@@ -854,17 +854,19 @@ __device__ bool cache_attended(const TreeAttnArgs& a, const CacheSelection& sel,
   return false;
 }
 
-__global__ __launch_bounds__(kTreeMergeRows * 32) void wild_queries_kernel(TreeAttnArgs a, CacheSelection sel) {
-  const int row = blockIdx.x * kTreeMergeRows + (threadIdx.x >> 5);  // of R x T x Hq
-  const int rt = row / a.Hq, r = rt / a.T;
-  if (r >= a.R || rt - r * a.T >= tree_length(a, r)) return;
+__global__ __launch_bounds__(kTreeWildRows * 32) void wild_queries_kernel(TreeAttnArgs a, CacheSelection sel) {
   const int c4 = threadIdx.x & 31;
-  const long long at = (long long)row * kHeadDim + c4 * 4;
-  const uint2 w = *reinterpret_cast<const uint2*>(a.q + at);
-  if (!of_row(wild_bf16(w.x) || wild_bf16(w.x >> 16) || wild_bf16(w.y) || wild_bf16(w.y >> 16))) return;
-  if (!a.tree_k && !cache_attended(a, sel, r, a.by_g(row - rt * a.Hq))) return;
-  *reinterpret_cast<uint2*>(a.out + at) = make_uint2(0x7FC07FC0u, 0x7FC07FC0u);
-  if (c4 == 0 && a.lse) a.lse[row] = __builtin_nanf("");
+  const int rows = a.R * a.T * a.Hq;  // at most 2^28
+  for (int row = blockIdx.x * kTreeWildRows + (threadIdx.x >> 5); row < rows; row += gridDim.x * kTreeWildRows) {
+    const int rt = row / a.Hq, r = rt / a.T;
+    if (rt - r * a.T >= tree_length(a, r)) continue;
+    const long long at = (long long)row * kHeadDim + c4 * 4;
+    const uint2 w = *reinterpret_cast<const uint2*>(a.q + at);
+    if (!of_row(wild_bf16(w.x) || wild_bf16(w.x >> 16) || wild_bf16(w.y) || wild_bf16(w.y >> 16))) continue;
+    if (!a.tree_k && !cache_attended(a, sel, r, a.by_g(row - rt * a.Hq))) continue;
+    *reinterpret_cast<uint2*>(a.out + at) = make_uint2(0x7FC07FC0u, 0x7FC07FC0u);
+    if (c4 == 0 && a.lse) a.lse[row] = __builtin_nanf("");
+  }
 }
 
 template <int BS, bool PAGED>
@@ -904,9 +906,8 @@ hipError_t launch_tree_finish(const TreeAttnArgs& a, const CacheSelection& sel, 
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   if (a.q_and != 0) return e;
-  const long long rows = (long long)a.R * a.T * a.Hq;  // below 2^28
-  hipLaunchKernelGGL(wild_queries_kernel, dim3((unsigned)((rows + kTreeMergeRows - 1) / kTreeMergeRows)),
-                     dim3(kTreeMergeRows * 32), 0, s, a, sel);
+  hipLaunchKernelGGL(wild_queries_kernel, dim3(tree_wild_groups((long long)a.R * a.T * a.Hq)), dim3(kTreeWildRows * 32), 0, s,
+                     a, sel);
   return hipGetLastError();
 }
 

@@ -134,6 +134,15 @@ inline TreePlan tree_plan(long long pairs, int G, int T, int units, bool ragged)
   return p;
 }
 
+// Workgroups of the pass over the rows of wild queries, kTreeWildRows rows each at a time.
+// Calls may have 2^28 rows, of which a workgroup for every eight would be 2^33 threads: a
+// launch has fewer than 2^32.
+constexpr int kTreeWildRows = 8;
+inline unsigned tree_wild_groups(long long rows) {
+  const long long groups = (rows + kTreeWildRows - 1) / kTreeWildRows;
+  return (unsigned)(groups < 1 << 14 ? groups : 1 << 14);
+}
+
 // Whether a paged call takes its requests by length, the longest first: a call of more
 // workgroups than the CUs hold at once ends with the last ones it starts, so these had
 // better be short. Up to 64 requests, one a lane. Measured, 64 rows, 24 requests of 1 to

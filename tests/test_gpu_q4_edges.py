@@ -99,3 +99,25 @@ def test_wild_queries_whose_only_page_is_far_along(form, last):
                 assert torch.isnan(out).all() and torch.isnan(lse).all()
             else:
                 assert not out.view(torch.int16).any() and torch.all(lse == -torch.inf)
+
+
+@pytest.mark.parametrize("tree", [False, True])
+def test_wild_queries_among_more_rows_than_one_launch_takes_at_once(tree):
+    R, T, G, B = 20, 64, 64, 16  # 163,840 rows
+    rng = np.random.default_rng(3)
+    d = P.dims(R, G * H, H, 128, B, 1)
+    note(f"4-bit wild queries of many rows tree={tree}")
+    q = torch.zeros((R, T, G * H, 128), dtype=torch.bfloat16, device="cuda")
+    wild = rng.choice(R * T * G * H, 50, replace=False)
+    wild[:4] = [0, R * T * G * H - 1, 1 << 17, (1 << 17) - 1]
+    q.view(-1, 128)[torch.from_numpy(wild).cuda(), torch.from_numpy(rng.integers(0, 128, 50)).cuda()] = float("nan")
+    pages = [dev_u8(Q.make_pages(rng.normal(size=(1, H, B, 128)))) for _ in range(2)]
+    rows = torch.ones((R, T, H, 128), dtype=torch.bfloat16, device="cuda") if tree else None
+    out, lse = torch.full(q.shape, 7.0, dtype=torch.bfloat16, device="cuda"), torch.full(q.shape[:3], 7.0, device="cuda")
+    ws = torch.zeros(P.oasis_tree_attn_q4_workspace_bytes(d, T, 0), dtype=torch.uint8, device="cuda")
+    P.oasis_tree_attn_q4(d, q, T, *pages, dev_i32(np.zeros((R, 1))), dev_i32(np.full(R, 5)), None, None, 0, rows, rows, None, None,
+                         0.0, out, lse, ws)
+    want = torch.zeros(R * T * G * H, dtype=torch.bool)
+    want[wild] = True
+    assert torch.equal(torch.isnan(out).all(-1).view(-1).cpu(), want) and torch.equal(torch.isnan(lse).view(-1).cpu(), want)
+    assert torch.isfinite(out.view(-1, 128)[(~want).cuda()]).all()
