@@ -73,10 +73,11 @@ oasis_status check_attn_q4(const oasis_dims* d, int32_t T, int32_t k, const char
 }
 
 TreePlan attn_q4_plan(const oasis_dims* d, int32_t T, int32_t k) {
-  long long blocks = d->max_blocks;
-  if (k > 0 && k + 1 < blocks) blocks = k + 1;
-  return q4_plan((long long)d->num_reqs * d->num_kv_heads, d->num_q_heads / d->num_kv_heads, T,
-                 (int)((blocks * d->block_size + kQ4Unit - 1) / kQ4Unit));
+  const long long attended = k > 0 ? k + 1 : d->max_blocks;
+  const long long blocks = attended < d->max_blocks ? attended : d->max_blocks;
+  auto units = [&](long long n) { return (int)((n * d->block_size + kQ4Unit - 1) / kQ4Unit); };
+  return q4_plan((long long)d->num_reqs * d->num_kv_heads, d->num_q_heads / d->num_kv_heads, T, units(blocks),
+                 units(attended));
 }
 
 }  // namespace

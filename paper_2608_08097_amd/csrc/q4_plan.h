@@ -20,7 +20,10 @@ constexpr int kQ4Tiles = 8;   // 16-row tiles of a workgroup at most
 // 18.0, 8 x 125 26.8 and 28.9.
 constexpr int kQ4SmallUnits = 4700;
 
-// `units`: 64-token units of the longest context or selection that the call can have.
+// `units`: 64-token units of the longest context, or of the most different blocks that a
+// selection can hold. `attended`: of the most tokens that a row attends, a block as often as
+// the selection lists it; the rows' references lie as far above their scores as those need
+// (tree_lift).
 //
 // As many splits as fill the CUs, two workgroups each (one with more than four row tiles),
 // but the second one only with 16 units for each workgroup: a workgroup of a few units is
@@ -28,14 +31,14 @@ constexpr int kQ4SmallUnits = 4700;
 // 2 19.7, 4 16.7, 8 17.8; 8, 4, 31: 1 17.0, 2 14.2, 4 11.3, 8 9.7; 8, 20, 2,048: 8 120, 16
 // 68, 32 45, 64 43, 128 58; 64, 20, 2,048: 4 239, 8 197, 12 217, 16 210; 128, 72, 65: 1 84,
 // 2 55, 4 62; 16, 512, 1,024: 2 555, 4 291, 8 304.
-inline TreePlan q4_plan(long long pairs, int G, int T, int units) {
+inline TreePlan q4_plan(long long pairs, int G, int T, int units, int attended) {
   TreePlan p{};
   p.rows = G * T;
   const int tiles = (p.rows + 15) / 16, twos = (tiles + 1) / 2;
   const bool small = tiles > 4 && pairs * units * twos <= kQ4SmallUnits;
   p.groups = small ? twos : (tiles + kQ4Tiles - 1) / kQ4Tiles;
   p.tiles = small ? kQ4RegisterTiles : (tiles + p.groups - 1) / p.groups;
-  p.units = 2 * units;  // of 32 tokens (tree_lift)
+  p.units = 2 * attended;  // of 32 tokens
   const long long items = pairs * p.groups;
   const long long slots = p.tiles > 4 ? 256 : 512;
   long long most = (units + kQ4Waves - 1) / kQ4Waves;
@@ -51,5 +54,6 @@ inline TreePlan q4_plan(long long pairs, int G, int T, int units) {
   }
   return p;
 }
+inline TreePlan q4_plan(long long pairs, int G, int T, int units) { return q4_plan(pairs, G, T, units, units); }
 
 }  // namespace oasis

@@ -1,13 +1,14 @@
-"""Attention over the 4-bit cache in the corners of its contract: wild queries where nothing is attended, in every
-form of the kernel."""
+"""Attention over the 4-bit cache in the corners of its contract: wild queries where nothing is attended, selections that
+repeat blocks, in every form of the kernel."""
 import numpy as np
 import pytest
 import torch
 
 import paper_2608_08097_amd as P
+from oracle import oasis_oracle as O
 from oracle import q4 as Q
-from tests.gpu_util import dev_bf16, dev_i32, note
-from tests.test_gpu_drafts import INF, NAN
+from tests.gpu_util import dev_bf16, dev_i32, host_bits, note
+from tests.test_gpu_drafts import INF, NAN, _check
 from tests.test_gpu_q4 import dev_u8
 from workloads import random_bf16
 
@@ -121,3 +122,25 @@ def test_wild_queries_among_more_rows_than_one_launch_takes_at_once(tree):
     want[wild] = True
     assert torch.equal(torch.isnan(out).all(-1).view(-1).cpu(), want) and torch.equal(torch.isnan(lse).view(-1).cpu(), want)
     assert torch.isfinite(out.view(-1, 128)[(~want).cuda()]).all()
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("times", [40, 2048])
+def test_a_selection_that_repeats_its_blocks(form, times):
+    """More selected ids than the table has blocks, each attended as often as it is listed: the largest finite values keep
+    finite means, and others are those of the oracle."""
+    G, T, B, _ = form
+    NB, L = 4, 4 * B - 5
+    rng = np.random.default_rng(T + times)
+    table = rng.permutation(5)[:NB].reshape(1, NB).astype(np.int32)
+    sel = np.tile(np.array([[[0, 2]], [[1, 0]]], np.int32).reshape(1, H, 2), (1, 1, times))
+    cnt = np.full((1, H), 2 * times, np.int32)
+    kp, vp = (Q.make_pages(rng.normal(size=(5, H, B, 128))) for _ in range(2))
+    big = Q.make_pages(np.full((5, H, B, 128), 6.0 * 2.0 ** 125))
+    for q, values in ((random_bf16(50 + T, (1, T, G * H, 128)), vp), (random_bf16(51 + T, (1, T, G * H, 128)), big),
+                      (np.zeros((1, T, G * H, 128), np.uint16), big)):
+        out, lse = _call(form, q, kp, values, table, [L], sel, cnt)
+        args = (q, Q.read_pages(kp, H, B), Q.read_pages(values, H, B), table, [L], sel, cnt, None, None, None, [T], B)
+        ref, ref_lse = Q.attend(*args)
+        ref_abs, _ = Q.attend(*args, magnitude=True)
+        _check(out, lse, ref, ref_abs, ref_lse, out)
