@@ -466,8 +466,10 @@ OASIS_API oasis_status oasis_append_tokens(const oasis_dims* dims, const uint16_
  *   codes         dims 2j and 2j + 1 of a token in the low and high half of its byte j;
  *                 bit 3 a sign, bits 0..2 one of 0, 0.5, 1, 1.5, 2, 3, 4, 6
  *   powers        a byte s for 32 dims of a token, at [t / 16][t % 4][dim / 32]
- *                 [t % 16 / 4] for token t of the page: they are code * 2^(s - 127).
- *                 255, with codes of 0: 32 NaN.
+ *                 [t % 16 / 4] for token t of the page: they are code * 2^(s - 127),
+ *                 s from 0 to 252 (the append writes 1 to 252). 255, with codes of 0: 32
+ *                 NaN. 253 and 254, whose larger codes pass the largest bf16, stand for
+ *                 nothing: what attends such a token may be any value, infinite or NaN.
  *
  * A step over it: oasis_rotate (queries, and keys that a tree's rows attend),
  * oasis_score_blocks and oasis_select_topk as for any cache, oasis_tree_attn_q4,

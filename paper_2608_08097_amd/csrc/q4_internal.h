@@ -4,7 +4,8 @@
 // A page holds, for B tokens of every KV head, codes [Hkv][B][64] and then powers of two
 // [Hkv][B / 16][4][4][4], a byte each. A code is a sign and one of 0, 0.5, 1, 1.5, 2, 3, 4,
 // 6 (dims 2 j and 2 j + 1 of a token in the low and high half of its byte j); the power of
-// 32 dims, byte s, is 2^(s - 127). The powers of 16 tokens are indexed by t % 4, the group
+// 32 dims, byte s, is 2^(s - 127), s up to 252 (the conversions read the exponent of a float
+// whose bits are s << 23, 2^-127 for 0). The powers of 16 tokens are indexed by t % 4, the group
 // of dims and t / 4: a lane of the attention has tokens 4 apart, and finds their powers in
 // one dword.
 #pragma once

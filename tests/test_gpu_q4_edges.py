@@ -1,5 +1,5 @@
-"""Attention over the 4-bit cache in the corners of its contract: wild queries where nothing is attended, selections that
-repeat blocks, in every form of the kernel."""
+"""The 4-bit cache in the corners of its contract: wild queries where nothing is attended, selections that repeat blocks,
+powers that no append writes; attention in every form of the kernel."""
 import numpy as np
 import pytest
 import torch
@@ -144,3 +144,44 @@ def test_a_selection_that_repeats_its_blocks(form, times):
         ref, ref_lse = Q.attend(*args)
         ref_abs, _ = Q.attend(*args, magnitude=True)
         _check(out, lse, ref, ref_abs, ref_lse, out)
+
+
+def _with_powers(rng, n, B, powers):
+    """Pages of any codes with powers among the given ones."""
+    pages = rng.integers(0, 256, (n, Q.page_bytes(H, B))).astype(np.uint8)
+    pages[:, H * B * 64:] = rng.choice(powers, (n, H * B * 4))
+    return pages
+
+
+@pytest.mark.parametrize("B", [16, 32])
+def test_the_smallest_and_largest_powers_in_compressed_keys(B):
+    rng = np.random.default_rng(B)
+    for powers in ([0], [0, 1, 2], [252], [0, 252, 255], list(range(253))):
+        pages = _with_powers(rng, 6, B, powers)
+        table = np.array([[4, 0, 5, 1, 3, 2]], np.int32)
+        out = [torch.zeros((1, H, 6, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+        want = [np.zeros((1, H, 6, 128)) for _ in range(2)]
+        note(f"powers {powers[:3]} in compressed keys B={B}")
+        P.oasis_update_summaries_q4(P.dims(1, H, H, 128, B, 6), dev_u8(pages), dev_i32(table), None, dev_i32([6 * B]), 0, *out)
+        Q.update_summaries(pages, table, None, [6 * B], B, *want)
+        for got, w in zip(out, want):
+            assert np.array_equal(O.bf16_to_f64(host_bits(got)), w), powers[:3]
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("power,size", [(0, 124), (1, 123), (2, 122), (252, -126), (251, -125)])
+def test_the_smallest_and_largest_powers_in_attention(form, power, size):
+    """Keys and queries at opposite ends of the range, whose products are logits of a few units; values of any power."""
+    G, T, B, spare = form
+    NB = 5
+    rng = np.random.default_rng(power + T)
+    q = rng.normal(size=(1, T, G * H, 128)) * 2.0 ** size
+    q = (q.astype(np.float32).view(np.uint32) >> 16).astype(np.uint16)
+    kp, vp = _with_powers(rng, NB, B, [power]), _with_powers(rng, NB, B, [0, 1, 100, 127, 129, 252])
+    table = np.array([[*rng.permutation(NB), *[-1] * spare]], np.int32)
+    L, scale = NB * B - 3, 0.1  # sums of scale |q k| below 16
+    out, lse = _call(form, q, kp, vp, table, [L], scale=scale)
+    args = (q, Q.read_pages(kp, H, B), Q.read_pages(vp, H, B), table, [L], None, None, None, None, None, [T], B, scale)
+    ref, ref_lse = Q.attend(*args)
+    ref_abs, _ = Q.attend(*args, magnitude=True)
+    _check(out, lse, ref, ref_abs, ref_lse, out)
