@@ -37,17 +37,20 @@ class Q4Path:
 
     ``block_table`` is the device page table ``[R][NBmax]`` of every layer; two requests may share pages that neither
     appends to. ``rotary`` (None: keys and queries come with their positions) turns the keys that ``append`` writes and the
-    rows that ``rotate`` is given. The layers' calls share one workspace and one pair of rotated rows, so they must run
-    in order, on one stream or behind each other's events.
+    rows that ``rotate`` is given. ``predict`` ranks blocks from the ``num_draft`` rows from ``first_draft`` on: by default
+    from all but the first, or a step's only one, as many as the scorer takes (64 with the heads that share a KV head). The
+    layers' calls share one workspace and one pair of rotated rows, so they must run in order, on one stream or behind
+    each other's events.
     """
 
     def __init__(self, d: L.OasisDims, num_q_tokens: int, k: int, num_pages: int, block_table: torch.Tensor,
-                 rotary: L.Rotary | None = None, first_draft: int = 1, num_draft: int | None = None,
+                 rotary: L.Rotary | None = None, first_draft: int | None = None, num_draft: int | None = None,
                  scale: float | None = None):
         self.dims, self.T, self.k, self.num_pages = d, int(num_q_tokens), int(k), int(num_pages)
         self.block_table, self.rotary = block_table, rotary
-        self.first_draft = int(first_draft)
-        self.num_draft = int(num_draft if num_draft is not None else self.T - self.first_draft)
+        self.first_draft = int(first_draft if first_draft is not None else self.T > 1)
+        most = max(1, 64 // (d.num_q_heads // d.num_kv_heads))  # (more heads: the scorer says so)
+        self.num_draft = int(num_draft if num_draft is not None else min(self.T - self.first_draft, most))
         self.scale = scale if scale is not None else 1.0 / math.sqrt(d.head_dim)
         dev = block_table.device
         need = max(L.oasis_tree_attn_q4_workspace_bytes(d, self.T, self.k), L.oasis_tree_attn_q4_workspace_bytes(d, self.T, 0))
