@@ -500,13 +500,15 @@ typedef struct {
  * the frequencies base^(-2i / rotary_dim) / (2 pi), scaled for long contexts:
  *   PLAIN      as they are
  *   LINEAR     divided by factor
- *   STRETCHED  of the base base * factor^(rotary_dim / (rotary_dim - 2))
+ *   STRETCHED  of the base base * factor^(rotary_dim / (rotary_dim - 2)), which is
+ *              known as NTK-aware scaling
  *   BY_TURNS   divided by factor where a pair makes at most `low` turns in first_len
  *              positions, as they are from `high` turns on, between them in proportion
- *              to the turns
+ *              to the turns (1 and 4 are usual)
  *   BY_INDEX   the same in proportion to the pair's index, from the pair (rounded down)
- *              that makes `high` turns to the one (rounded up) that makes `low`; the
- *              amplitude is 0.1 ln(factor) + 1 where factor > 1, else 1 (as in the others)
+ *              that makes `high` turns to the one (rounded up) that makes `low` (32 and 1
+ *              are usual); the amplitude is 0.1 ln(factor) + 1 where factor > 1, else 1 (as
+ *              in the others). Known as YaRN
  * Arguments that a scaling does not name are not looked at.
  */
 #define OASIS_ROTARY_PLAIN 0

@@ -668,7 +668,8 @@ ROTARY_BY_INDEX = 4   # OASIS_ROTARY_BY_INDEX
 
 def oasis_rotary_turns(rotary_dim: int, base: float = 10000.0, scaling: int = ROTARY_PLAIN, factor: float = 1.0,
                        first_len: float = 0.0, low: float = 1.0, high: float = 32.0) -> tuple[list[float], float]:
-    """Turns of each pair a position, and the amplitude, of rotary positions scaled for long contexts."""
+    """Turns of each pair a position, and the amplitude, of rotary positions scaled for long contexts. ``low`` and ``high``
+    are by default those usual for ROTARY_BY_INDEX; ROTARY_BY_TURNS usually takes 1 and 4."""
     n = int(rotary_dim)
     turns, amplitude = (ctypes.c_double * max(1, n // 2))(), ctypes.c_double()
     _check("oasis_rotary_turns", lib().oasis_rotary_turns(n, base, int(scaling), factor, first_len, low, high, turns,

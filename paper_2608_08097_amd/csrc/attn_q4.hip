@@ -8,7 +8,9 @@
 //   O^T (d x rows)     += V^T . P^T   16 of them
 //
 // Codes become bf16 exactly, two a conversion with their power of two, and both products are
-// those of tree_attn.hip over the values that the cache stands for. Two forms.
+// those of tree_attn.hip over the values that the cache stands for. The probabilities are
+// rounded to bf16 for the second one, their sums are not (unit_softmax in tree_core.h). Two
+// forms.
 //
 // Up to two row tiles every wave streams units of its own. Of a sub-block a lane has 32 dims of
 // a token in 16 bytes, with one power: keys are the first product's operand as soon as they are
@@ -22,9 +24,10 @@
 //
 // Measured (136 bytes a token and KV head; 4 d operations a row and token):
 //   8 requests x 8 heads x 131,072 tokens, 4 rows    180 us  6.3 TB/s
-//   8 x 8 x 131,072, 20 rows                         203-205 us  5.6 TB/s; its loads alone take 174 and the
-//                                                    clock falls from 2.4 to 2.05 GHz with the products
-//   24 x 8 x 1 to 32,768, 64 rows                    151-172 us a draw
+//   8 x 8 x 131,072, 20 rows                         201-208 us  5.6 TB/s; its loads alone take 174 and the
+//                                                    clock falls from 2.4 to 2.2 GHz with the products
+//   24 x 8 x 1 to 32,768, 64 rows                    151-173 us a draw; of its 768 workgroups on 512 places
+//                                                    the last ends at 1.3 times a place's share of the units
 //   2 x 8 x 65,000 to 65,536, 512 rows               297-307 us  890-920 TFLOP/s
 //   16 x 8 x 4,128 selected, 72 rows                 52 us
 //   8 x 8 x 2,064 selected, 20 rows                  16.1 us  two launches (7.4), four loads in turn

@@ -17,7 +17,8 @@ constexpr int kQ4Tiles = 8;   // 16-row tiles of a workgroup at most
 // same where the row groups together read at most so many units. Measured, us with the form
 // for more rows and this one (8 heads, 128 rows: pairs x units): 8 x 8 17.9 and 14.8, 8 x 32
 // 18.5 and 15.6, 8 x 125 23.6 and 20.4, 16 x 125 27.5 and 29.0; 256 rows: 8 x 32 19.8 and
-// 18.0, 8 x 125 26.8 and 28.9.
+// 18.0, 8 x 125 26.8 and 28.9. Not measured: hundreds of pairs with a few units each, of which
+// the small form's workgroups are more than the CUs hold at once.
 constexpr int kQ4SmallUnits = 4700;
 
 // `units`: 64-token units of the longest context, or of the most different blocks that a
@@ -30,7 +31,10 @@ constexpr int kQ4SmallUnits = 4700;
 // nearly all start and end. Measured, splits and us (pairs, rows, units): 64, 20, 33: 1 23.4,
 // 2 19.7, 4 16.7, 8 17.8; 8, 4, 31: 1 17.0, 2 14.2, 4 11.3, 8 9.7; 8, 20, 2,048: 8 120, 16
 // 68, 32 45, 64 43, 128 58; 64, 20, 2,048: 4 239, 8 197, 12 217, 16 210; 128, 72, 65: 1 84,
-// 2 55, 4 62; 16, 512, 1,024: 2 555, 4 291, 8 304.
+// 2 55, 4 62; 16, 512, 1,024: 2 555, 4 291, 8 304. Counts are powers of two, and these pairs
+// divide the places evenly: where they do not (72 pairs of 128 rows: 288 workgroups on 256),
+// the last round is hardly filled, and another count might end sooner. Nor are ragged
+// contexts looked at: a split is a share of its own request's tokens.
 inline TreePlan q4_plan(long long pairs, int G, int T, int units, int attended) {
   TreePlan p{};
   p.rows = G * T;
